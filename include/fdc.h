@@ -405,6 +405,160 @@ fdc_status fdc_adam_step(float *p, const float *g, float *m, float *v, int64_t n
                          float beta1, float beta2, float eps, float weight_decay, hipStream_t stream);
 
 /* ------------------------------------------------------------------------ */
+/* Sequence operators                                                       */
+/* ------------------------------------------------------------------------ */
+/* The block of a sequence network (tokens of D channels, for example the pixels of an
+ * FDCNN's last planes) and the loss it is trained with: a causal convolution of each
+ * channel with its own short kernel, a selective state space scan, the norms, gate and
+ * residual scale around them, and distillation from a teacher's top logits.
+ *
+ * Types.     Activations (and their gradients) are of one of the types below;
+ *            parameters, their gradients, states h and losses are float32.  Every sum
+ *            is formed in float32 and each output is rounded once.
+ * Tokens.    fdc_tokens is a [B][L][width] tensor: element (b, t, c) is at
+ *            p[b * batch_stride + t * token_stride + c] (strides in elements, >= 0,
+ *            token_stride below 2^26).  p == NULL: the tensor is absent, where that is
+ *            allowed.  Input strides may be 0 (one row for every token); the elements
+ *            of an output must not overlap.  No alignment beyond the type's own is
+ *            asked for.
+ * Lengths.   lengths [B] int32 (device memory; NULL: every sequence has L tokens):
+ *            sequence b has the tokens t < lengths[b] (a value outside [0, L] is taken
+ *            as 0 or L).  What inputs hold at the other tokens is never used, NaN
+ *            included; outputs and gradients are 0 there, and states are those after the
+ *            last token (after no token: the given state).
+ * States.    A state carries the tokens of an earlier call on; no gradient is formed
+ *            for it. */
+typedef enum { FDC_F32 = 0, FDC_BF16 = 1, FDC_F16 = 2 } fdc_dtype;
+
+typedef struct {
+  void *p;
+  int64_t batch_stride;
+  int64_t token_stride;
+} fdc_tokens;
+
+/* Causal convolution (each channel with its own kernel of n taps, 1 <= n <= 8):
+ *   p[b][t][d] = bias[d] + sum_{j<n} w[d][j] x[b][t - n + 1 + j][d];  y = silu ? p / (1 + exp(-p)) : p.
+ * x[b][t] for t < 0 is state[b][t + n - 1] (state [B][n-1][D] dense, of the activations'
+ * type; NULL: zeros).  w [D][n], bias [D] (NULL: none).  new_state [B][n-1][D] (NULL: not
+ * wanted): the last n - 1 tokens of each sequence, those of `state` among them where it is
+ * shorter; it may be `state` itself.  A single token is a call with L = 1. */
+typedef struct {
+  int dtype, B, L, D, n, silu;
+  fdc_tokens x, y;
+  const float *w, *bias;
+  const void *state;
+  void *new_state;
+  const int32_t *lengths;
+} fdc_causal_conv_args;
+fdc_status fdc_causal_conv_forward(const fdc_causal_conv_args *a, hipStream_t stream);
+/* From gy: gx (p NULL: skipped), gw [D][n] and gbias [D] (NULL: skipped), summed over
+ * tokens and sequences in a fixed order.  a->y and a->new_state are not used.
+ * ws: fdc_causal_conv_workspace_size bytes (0 when gw and gbias are both NULL). */
+fdc_status fdc_causal_conv_workspace_size(int dtype, int B, int L, int D, int n, size_t *bytes);
+fdc_status fdc_causal_conv_backward(const fdc_causal_conv_args *a, fdc_tokens gy, fdc_tokens gx, float *gw,
+                                    float *gbias, void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* Selective state space scan of each channel d with N states (1 <= N <= 64); the channels
+ * are G equal groups, group g = d / (D / G) sharing Bm and Cm:
+ *   delta = softplus ? log(1 + exp(dt + dt_bias[d])) : dt + dt_bias[d]
+ *   h[t][n] = exp(delta A[d][n]) h[t-1][n] + delta x[t] Bm[t][g][n]
+ *   y[t] = (sum_n Cm[t][g][n] h[t][n] + skip[d] x[t]) silu(gate[t])
+ * x, dt, gate, y: [B][L][D]; Bm, Cm: [B][L][G N]; A [D][N]; skip, dt_bias [D] (NULL: 0);
+ * gate absent: no factor.  h0 [B][D][N] (NULL: zeros) is the state before the first token,
+ * h_last [B][D][N] (NULL: not wanted; not h0) the one after the last.
+ * saved (NULL: no backward follows): fdc_scan_saved_size bytes, 16-byte aligned, for the
+ * backward: the states at every 16th token. */
+typedef struct {
+  int dtype, B, L, D, N, G, softplus;
+  fdc_tokens x, dt, gate, Bm, Cm, y;
+  const float *A, *skip, *dt_bias, *h0;
+  float *h_last;
+  const int32_t *lengths;
+} fdc_scan_args;
+fdc_status fdc_scan_saved_size(int B, int L, int D, int N, size_t *bytes);
+fdc_status fdc_scan_workspace_size(int B, int L, int D, int N, int G, size_t *fwd_ws, size_t *bwd_ws);
+fdc_status fdc_scan_forward(const fdc_scan_args *a, float *saved, void *ws, size_t ws_bytes, hipStream_t stream);
+/* From gy, the forward's inputs and what it saved (a->y, a->h0 and a->h_last are not used):
+ * gradients of x, dt, gate, Bm, Cm (type of the activations; gx, gdt, gBm and gCm are
+ * required, ggate where a gate is given), gA [D][N], gskip [D] and gdt_bias [D] (required
+ * where the parameter is given, else NULL).  Sums run in a fixed order. */
+typedef struct {
+  fdc_tokens gy, gx, gdt, ggate, gBm, gCm;
+  float *gA, *gskip, *gdt_bias;
+} fdc_scan_grads;
+fdc_status fdc_scan_backward(const fdc_scan_args *a, const float *saved, const fdc_scan_grads *g, void *ws,
+                             size_t ws_bytes, hipStream_t stream);
+/* One token of every sequence: a with L = 1 (lengths NULL), the state h0 in, h_last out
+ * (both required, dense [B][D][N]; h_last may be h0).  No workspace. */
+fdc_status fdc_scan_step(const fdc_scan_args *a, hipStream_t stream);
+
+/* The end of a block and the start of the next: with rms(v; w) = w v / sqrt(mean(v^2) + eps),
+ *   out = x + scale act(gate) rms(f; w_post);   n = rms(out; w_pre)
+ * over R rows of D channels, row strides in elements (inputs' may be 0).  Any part may be
+ * absent: f NULL: out = x (then gate, scale and w_post are NULL too); gate NULL: act is 1;
+ * scale NULL: 1; w_post NULL: f itself, not normed; w_pre NULL: no n.  scale, w_post and w_pre
+ * are [D] float32.  act: 0 the gate itself, 1 1 / (1 + exp(-g)), 2 g / (1 + exp(-g)).
+ * out NULL: not wanted.  stats [R][2] float32 (NULL: no backward follows): the reciprocal root
+ * mean squares of f and of out.  D at most 8192.  n is formed from out before its rounding. */
+typedef struct {
+  int dtype, D, act;
+  int64_t R;
+  float eps;
+  const void *x, *f, *gate;
+  int64_t x_stride, f_stride, gate_stride;
+  const float *scale, *w_post, *w_pre;
+} fdc_block_norm_args;
+fdc_status fdc_block_norm_forward(const fdc_block_norm_args *a, void *out, int64_t out_stride, void *n,
+                                  int64_t n_stride, float *stats, hipStream_t stream);
+/* From gout (gradient of out; NULL: zero) and gn (of n; NULL: zero): gx, gf, ggate (type of the
+ * activations, NULL: skipped) and gscale, gw_post, gw_pre [D] (NULL: skipped), summed over the
+ * rows in a fixed order.  ws: fdc_block_norm_workspace_size bytes. */
+typedef struct {
+  const void *gout, *gn;
+  void *gx, *gf, *ggate;
+  int64_t gout_stride, gn_stride, gx_stride, gf_stride, ggate_stride;
+  float *gscale, *gw_post, *gw_pre;
+} fdc_block_norm_grads;
+fdc_status fdc_block_norm_workspace_size(int64_t R, int D, size_t *bytes);
+fdc_status fdc_block_norm_backward(const fdc_block_norm_args *a, const float *stats, const fdc_block_norm_grads *g,
+                                   void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* Loss of R rows of V logits z against a teacher's K best logits of each row (1 <= K <= 1024),
+ * and against labels:
+ *   loss[r] = weight[r] ((1 - alpha) (-log softmax(z)[label]) +
+ *                        alpha tau^2 sum_k q_k (log q_k - log softmax(z / tau)[idx_k])),
+ *   q = softmax(teacher / tau) over the row's K entries.
+ * z [R][V] with row stride z_stride; idx [R][K] int32; teacher [R][K], of z's type; both dense.  An
+ * entry with idx < 0 is absent; a row without an entry (or with teacher logits of -inf alone)
+ * has no second term.  labels [R] int32 (NULL: no first term); a row with label < 0 has no
+ * first term.  weight [R] float32 (NULL: 1); a row of weight 0 has loss 0 and gradient 0,
+ * whatever it holds.  An index or label >= V gives a NaN loss and NaN gradients in its row.
+ * An index given twice counts twice.  tau > 0, 0 <= alpha <= 1.
+ * stats [R][4] float32 holds what the backward needs of the row: the largest logit, the sums
+ * of exp(z - max) and of exp((z - max) / tau), and the logsumexp of teacher / tau. */
+typedef struct {
+  int dtype, V, K;
+  int64_t R;
+  float tau, alpha;
+  const void *z;
+  int64_t z_stride;
+  const int32_t *idx;
+  const void *teacher;
+  const int32_t *labels;
+  const float *weight;
+} fdc_distill_args;
+fdc_status fdc_distill_workspace_size(int dtype, int64_t R, int V, size_t *bytes);
+fdc_status fdc_distill_forward(const fdc_distill_args *a, float *loss, float *stats, void *ws, size_t ws_bytes,
+                               hipStream_t stream);
+/* gz[r][v] = gloss[r] dloss[r]/dz[r][v] (gloss [R] float32), from the forward's stats; gz, of z's type,
+ * may be z itself. */
+fdc_status fdc_distill_backward(const fdc_distill_args *a, const float *stats, const float *gloss, void *gz,
+                                int64_t gz_stride, hipStream_t stream);
+/* Both in one call, for a gloss that is known beforehand (the mean over a batch): z is read once. */
+fdc_status fdc_distill_forward_backward(const fdc_distill_args *a, const float *gloss, float *loss, float *stats,
+                                        void *gz, int64_t gz_stride, void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------------------------ */
 /* Kernel timing (measurement support, off by default)                      */
 /* ------------------------------------------------------------------------ */
 /* While enabled, every kernel the library launches (only those named

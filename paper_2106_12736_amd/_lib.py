@@ -24,6 +24,40 @@ _I64 = ctypes.c_int64
 _SZ = ctypes.c_size_t
 _PP = ctypes.POINTER(ctypes.c_void_p)
 
+DTYPE_F32, DTYPE_BF16, DTYPE_F16 = range(3)
+
+
+class Tokens(ctypes.Structure):
+    """fdc_tokens: a [B][L][width] tensor by its strides in elements."""
+
+    _fields_ = [("p", _P), ("batch_stride", _I64), ("token_stride", _I64)]
+
+
+def _struct(name, doc, *fields):
+    return type(name, (ctypes.Structure,), {"__doc__": doc, "_fields_": list(fields)})
+
+
+def _named(kind, names):
+    return [(n, kind) for n in names.split()]
+
+
+ConvArgs = _struct("ConvArgs", "fdc_causal_conv_args", *_named(_I, "dtype B L D n silu"), *_named(Tokens, "x y"),
+                   *_named(_P, "w bias state new_state lengths"))
+ScanArgs = _struct("ScanArgs", "fdc_scan_args", *_named(_I, "dtype B L D N G softplus"),
+                   *_named(Tokens, "x dt gate Bm Cm y"), *_named(_P, "A skip dt_bias h0 h_last lengths"))
+ScanGrads = _struct("ScanGrads", "fdc_scan_grads", *_named(Tokens, "gy gx gdt ggate gBm gCm"),
+                    *_named(_P, "gA gskip gdt_bias"))
+NormArgs = _struct("NormArgs", "fdc_block_norm_args", *_named(_I, "dtype D act"), ("R", _I64),
+                   ("eps", ctypes.c_float), *_named(_P, "x f gate"), *_named(_I64, "x_stride f_stride gate_stride"),
+                   *_named(_P, "scale w_post w_pre"))
+NormGrads = _struct("NormGrads", "fdc_block_norm_grads", *_named(_P, "gout gn gx gf ggate"),
+                    *_named(_I64, "gout_stride gn_stride gx_stride gf_stride ggate_stride"),
+                    *_named(_P, "gscale gw_post gw_pre"))
+DistillArgs = _struct("DistillArgs", "fdc_distill_args", *_named(_I, "dtype V K"), ("R", _I64),
+                      *_named(ctypes.c_float, "tau alpha"), ("z", _P), ("z_stride", _I64),
+                      *_named(_P, "idx teacher labels weight"))
+_SZP = ctypes.POINTER(_SZ)
+
 # name -> argtypes (restype is int status unless listed in _RESTYPES)
 _SIGS = {
     "fdc_status_string": [_I],
@@ -85,6 +119,21 @@ _SIGS = {
     "fdc_cic_layer_one_launch": [_P, ctypes.POINTER(_I), ctypes.POINTER(_I)],
     "fdc_cic_stack_dk_ranges": [_P, _I, ctypes.POINTER(_I)],
     "fdc_cic_stack_tail": [_P, ctypes.POINTER(_I)],
+    "fdc_causal_conv_forward": [ctypes.POINTER(ConvArgs), _P],
+    "fdc_causal_conv_workspace_size": [_I, _I, _I, _I, _I, _SZP],
+    "fdc_causal_conv_backward": [ctypes.POINTER(ConvArgs), Tokens, Tokens, _P, _P, _P, _SZ, _P],
+    "fdc_scan_saved_size": [_I, _I, _I, _I, _SZP],
+    "fdc_scan_workspace_size": [_I, _I, _I, _I, _I, _SZP, _SZP],
+    "fdc_scan_forward": [ctypes.POINTER(ScanArgs), _P, _P, _SZ, _P],
+    "fdc_scan_backward": [ctypes.POINTER(ScanArgs), _P, ctypes.POINTER(ScanGrads), _P, _SZ, _P],
+    "fdc_scan_step": [ctypes.POINTER(ScanArgs), _P],
+    "fdc_block_norm_forward": [ctypes.POINTER(NormArgs), _P, _I64, _P, _I64, _P, _P],
+    "fdc_block_norm_workspace_size": [_I64, _I, _SZP],
+    "fdc_block_norm_backward": [ctypes.POINTER(NormArgs), _P, ctypes.POINTER(NormGrads), _P, _SZ, _P],
+    "fdc_distill_workspace_size": [_I, _I64, _I, _SZP],
+    "fdc_distill_forward": [ctypes.POINTER(DistillArgs), _P, _P, _P, _SZ, _P],
+    "fdc_distill_backward": [ctypes.POINTER(DistillArgs), _P, _P, _P, _I64, _P],
+    "fdc_distill_forward_backward": [ctypes.POINTER(DistillArgs), _P, _P, _P, _P, _I64, _P, _SZ, _P],
 }
 _RESTYPES = {"fdc_status_string": ctypes.c_char_p, "fdc_last_error": ctypes.c_char_p, "fdc_version": _I}
 

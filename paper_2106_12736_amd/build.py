@@ -58,7 +58,7 @@ def build(verbose=True):
     return LIB
 
 
-# Host sanitizers for the C ABI's host code (api.cpp only: argument validation, plan
+# Host sanitizers for the C ABI's host code (api*.cpp only: argument validation, plan
 # registry, workspace layout).  The device objects are the ones build() made; the
 # sanitizer flags reach the host compilation only.
 SAN_LIB = os.path.join(BUILD, "libfdc_hostsan.so")
@@ -82,7 +82,7 @@ def asan_runtime():
 
 
 def build_host_sanitized(verbose=True):
-    """SAN_LIB: the library with api.cpp compiled under AddressSanitizer and
+    """SAN_LIB: the library with its host sources compiled under AddressSanitizer and
     UndefinedBehaviorSanitizer (undefined behaviour traps), linked with the device
     objects of build() (made first if missing)."""
     os.makedirs(BUILD, exist_ok=True)
@@ -99,14 +99,15 @@ def build_host_sanitized(verbose=True):
     if missing:
         with ThreadPoolExecutor(max_workers=min(8, len(missing))) as ex:
             list(ex.map(_compile, missing))
-    api = os.path.join(CSRC, "api.cpp")
-    api_obj = os.path.join(BUILD, "api_hostsan.o")
-    cmd = [HIPCC] + COMMON + SAN_FLAGS + ["-c", api, "-o", api_obj]
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError(f"compile failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
+    api_objs = []
+    for api in (s for s in sources() if s.endswith(".cpp")):
+        api_objs.append(os.path.join(BUILD, os.path.basename(api)[:-4] + "_hostsan.o"))
+        cmd = [HIPCC] + COMMON + SAN_FLAGS + ["-c", api, "-o", api_objs[-1]]
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        if r.returncode != 0:
+            raise RuntimeError(f"compile failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
     rt = asan_runtime()
-    cmd = [HIPCC, "-shared", f"--offload-arch={ARCH}", "-fPIC", "-Wl,-z,defs", "-o", SAN_LIB, api_obj] + objs + [
+    cmd = [HIPCC, "-shared", f"--offload-arch={ARCH}", "-fPIC", "-Wl,-z,defs", "-o", SAN_LIB] + api_objs + objs + [
         rt, "-Wl,-rpath," + os.path.dirname(rt)]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:

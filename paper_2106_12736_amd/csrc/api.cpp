@@ -3,6 +3,7 @@
 // before enqueuing anything when an argument is wrong.
 #include "fdc.h"
 #include "internal.h"
+#include "status.h"
 
 #include <cmath>
 #include <cstdlib>
@@ -18,10 +19,10 @@
 #include <vector>
 
 namespace {
-
 thread_local std::string g_last_error;
+}  // namespace
 
-fdc_status fail(fdc_status st, const char *fmt, ...) {
+fdc_status fdc::fail(fdc_status st, const char *fmt, ...) {
   char buf[512];
   va_list ap;
   va_start(ap, fmt);
@@ -31,10 +32,15 @@ fdc_status fail(fdc_status st, const char *fmt, ...) {
   return st;
 }
 
-fdc_status check_hip(hipError_t e, const char *what) {
+fdc_status fdc::check_hip(hipError_t e, const char *what) {
   if (e == hipSuccess) return FDC_OK;
   return fail(FDC_EHIP, "%s: %s", what, hipGetErrorString(e));
 }
+
+using fdc::check_hip;
+using fdc::fail;
+
+namespace {
 
 bool even_pos(long long v) { return v > 0 && v % 2 == 0; }
 

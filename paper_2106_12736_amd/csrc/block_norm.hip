@@ -1,0 +1,340 @@
+// The end of a block and the start of the next in one pass over the row: norm of the block's output,
+// gate, residual scale and residual, and the norm of the sum.
+//
+//   fh = f rf, rf = 1 / sqrt(mean(f^2) + eps);  post = fh w_post;  out = x + scale act(gate) post
+//   n = out ro w_pre, ro = 1 / sqrt(mean(out^2) + eps)
+// Backward, from gout and gn:
+//   v = gn w_pre;  go = gout + v ro - out ro^3 mean(v out) = gx;  gw_pre = sum gn out ro
+//   gscale = sum go act post;  ggate = go scale post act'(gate);  gpost = go scale act
+//   u = gpost w_post;  gf = u rf - f rf^3 mean(u f);  gw_post = sum gpost fh
+//
+// A row is in the registers of the threads that share it, so everything is read and written once;
+// both directions are bound by HBM.  The sums over a row are formed in float32, across the wave
+// by lane moves and across waves through LDS.
+#include <algorithm>
+
+#include "sequence.h"
+
+namespace fdc {
+
+template <class T>
+constexpr int kNormV = 16 / (int)sizeof(T);  // 16 bytes a lane
+constexpr int kBwdV = 4;
+// Rows a workgroup takes at once: several only where a row is one wave's (no barrier in between).
+template <int TPR>
+constexpr int kRows = TPR == 64 ? 4 : 1;
+
+// Sum of v over the TPR threads of a row; every one of them gets it.  red: two halves used in turn,
+// so that one barrier a sum is enough.
+template <int TPR>
+__device__ __forceinline__ float row_sum(float v, float *red, int &turn) {
+  v = wave_sum(v);
+  if constexpr (TPR > 64) {
+    constexpr int W = TPR / 64;
+    float *r = red + turn * W;
+    turn ^= 1;
+    if ((threadIdx.x & 63) == 0) r[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = r[0];
+#pragma unroll
+    for (int i = 1; i < W; ++i) v += r[i];
+  }
+  return v;
+}
+
+__device__ __forceinline__ float gate_act(int act, float g, float sg) { return act == 0 ? g : act == 1 ? sg : g * sg; }
+__device__ __forceinline__ float gate_slope(int act, float g, float sg) {
+  return act == 0 ? 1.f : act == 1 ? sg * (1.f - sg) : sg * (1.f + g * (1.f - sg));
+}
+
+template <int V>
+__device__ __forceinline__ void params(float (&w)[V], const float *p, int c, int nc) {
+#pragma unroll
+  for (int i = 0; i < V; ++i) w[i] = 1.f;
+  if (p != nullptr && nc > 0) {
+    const Pack<float, V> x = load_some<float, V>(p + c, nc);
+#pragma unroll
+    for (int i = 0; i < V; ++i) w[i] = x.v[i];
+  }
+}
+template <class T, int V>
+__device__ __forceinline__ Pack<T, V> row_part(const T *p, int c, int nc) {
+  if (p != nullptr && nc > 0) return load_some<T, V>(p + c, nc);
+  Pack<T, V> x;
+#pragma unroll
+  for (int i = 0; i < V; ++i) x.v[i] = (T)0.f;
+  return x;
+}
+
+struct NormOut {
+  void *out, *n;
+  int64_t out_stride, n_stride;
+  float *stats;
+};
+
+template <class T, int TPR, int NV>
+__global__ __launch_bounds__(TPR * kRows<TPR>) void k_block_norm_fwd(fdc_block_norm_args a, NormOut o) {
+  constexpr int V = kNormV<T>, RPB = kRows<TPR>;
+  __shared__ float red[2 * (TPR / 64)];
+  int turn = 0;
+  const int tid = threadIdx.x % TPR;
+  const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * RPB + threadIdx.x / TPR;
+  if (row >= a.R) return;  // whole waves, and no barrier follows where a workgroup has several rows
+  const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
+  const T *f = a.f ? static_cast<const T *>(a.f) + row * a.f_stride : nullptr;
+  const T *gate = a.gate ? static_cast<const T *>(a.gate) + row * a.gate_stride : nullptr;
+  Pack<T, V> xr[NV], fr[NV], gr[NV];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int c = (k * TPR + tid) * V, nc = a.D - c;
+    xr[k] = row_part<T, V>(x, c, nc);
+    fr[k] = row_part<T, V>(f, c, nc);
+    gr[k] = row_part<T, V>(gate, c, nc);
+  }
+  const float invD = 1.f / (float)a.D;
+  float rf = 1.f, ro = 1.f;
+  if (f != nullptr && a.w_post != nullptr) {
+    float s = 0.f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int i = 0; i < V; ++i) s = fmaf((float)fr[k].v[i], (float)fr[k].v[i], s);
+    rf = 1.f / sqrtf(row_sum<TPR>(s, red, turn) * invD + a.eps);
+  }
+  float out[NV][V], s = 0.f;
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int c = (k * TPR + tid) * V, nc = a.D - c;
+    float wp[V], sc[V];
+    params<V>(wp, a.w_post, c, nc);
+    params<V>(sc, a.scale, c, nc);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const float g = (float)gr[k].v[i];
+      const float act = gate ? gate_act(a.act, g, sigmoid(g)) : 1.f;
+      const float post = (float)fr[k].v[i] * rf * wp[i];
+      out[k][i] = fmaf(sc[i] * act, post, (float)xr[k].v[i]);
+      s = fmaf(out[k][i], out[k][i], s);
+    }
+    if (o.out != nullptr && nc > 0) store_some<T, V>(static_cast<T *>(o.out) + row * o.out_stride + c, out[k], nc);
+  }
+  if (a.w_pre != nullptr) {
+    ro = 1.f / sqrtf(row_sum<TPR>(s, red, turn) * invD + a.eps);
+    T *n = static_cast<T *>(o.n) + row * o.n_stride;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int c = (k * TPR + tid) * V, nc = a.D - c;
+      float w[V];
+      params<V>(w, a.w_pre, c, nc);
+#pragma unroll
+      for (int i = 0; i < V; ++i) w[i] *= out[k][i] * ro;
+      if (nc > 0) store_some<T, V>(n + c, w, nc);
+    }
+  }
+  if (o.stats != nullptr && tid == 0) {
+    o.stats[2 * row] = rf;
+    o.stats[2 * row + 1] = ro;
+  }
+}
+
+// What a norm's backward leaves of the gradient u of (v r w) by w: u r - v c, c = r^3 mean(u v).  Of a
+// single channel that is u r (1 - v^2 r^2) = u eps r^3, which the difference would lose.
+__device__ __forceinline__ float norm_grad(float u, float v, float r, float c, int D, float eps) {
+  return D == 1 ? u * (eps * r * r * r) : u * r - v * c;
+}
+
+// Rows first, first + step, ...: the sums of the parameters' gradients stay in registers and go to
+// part [sharers of a row][3][D] (gscale, gw_post, gw_pre) at the end.
+template <class T, int TPR, int NV>
+__global__ __launch_bounds__(TPR * kRows<TPR>) void k_block_norm_bwd(fdc_block_norm_args a,
+                                                                          fdc_block_norm_grads g,
+                                                                          const float *__restrict__ stats,
+                                                                          float *__restrict__ part) {
+  constexpr int V = kBwdV, RPB = kRows<TPR>;
+  __shared__ float red[2 * (TPR / 64)];
+  int turn = 0;
+  const int tid = threadIdx.x % TPR;
+  const int64_t first = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR, step = (int64_t)gridDim.x * RPB;
+  const bool has_f = a.f != nullptr, has_gate = a.gate != nullptr, normed = a.w_post != nullptr;
+  const bool has_n = g.gn != nullptr && a.w_pre != nullptr;
+  const float invD = 1.f / (float)a.D;
+  float gscale[NV][V], gpost_w[NV][V], gpre_w[NV][V];
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+#pragma unroll
+    for (int i = 0; i < V; ++i) gscale[k][i] = gpost_w[k][i] = gpre_w[k][i] = 0.f;
+  for (int64_t row = first; row < a.R; row += step) {
+    Pack<T, V> xr[NV], fr[NV], ar[NV], go_r[NV], gn_r[NV];
+    const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
+    const T *f = has_f ? static_cast<const T *>(a.f) + row * a.f_stride : nullptr;
+    const T *gate = has_gate ? static_cast<const T *>(a.gate) + row * a.gate_stride : nullptr;
+    const T *gout = g.gout ? static_cast<const T *>(g.gout) + row * g.gout_stride : nullptr;
+    const T *gn = has_n ? static_cast<const T *>(g.gn) + row * g.gn_stride : nullptr;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int c = (k * TPR + tid) * V, nc = a.D - c;
+      xr[k] = row_part<T, V>(x, c, nc);
+      fr[k] = row_part<T, V>(f, c, nc);
+      ar[k] = row_part<T, V>(gate, c, nc);
+      go_r[k] = row_part<T, V>(gout, c, nc);
+      gn_r[k] = row_part<T, V>(gn, c, nc);
+    }
+    const float rf = stats[2 * row], ro = stats[2 * row + 1];
+    float s = 0.f, go[NV][V];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int c = (k * TPR + tid) * V, nc = a.D - c;
+      float wp[V], sc[V], w[V];
+      params<V>(wp, a.w_post, c, nc);
+      params<V>(sc, a.scale, c, nc);
+      params<V>(w, a.w_pre, c, nc);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const float gv = (float)ar[k].v[i];
+        const float act = has_gate ? gate_act(a.act, gv, sigmoid(gv)) : 1.f;
+        const float out = fmaf(sc[i] * act, (float)fr[k].v[i] * rf * wp[i], (float)xr[k].v[i]);
+        go[k][i] = out;
+        s = fmaf((float)gn_r[k].v[i] * w[i], out, s);
+      }
+    }
+    const float c1 = has_n ? ro * ro * ro * invD * row_sum<TPR>(s, red, turn) : 0.f;
+    float u[NV][V];
+    s = 0.f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int c = (k * TPR + tid) * V, nc = a.D - c;
+      float wp[V], sc[V], w[V], gg[V];
+      params<V>(wp, a.w_post, c, nc);
+      params<V>(sc, a.scale, c, nc);
+      params<V>(w, a.w_pre, c, nc);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const float out = go[k][i], gnv = (float)gn_r[k].v[i], gv = (float)ar[k].v[i];
+        const float sg = sigmoid(gv), act = has_gate ? gate_act(a.act, gv, sg) : 1.f;
+        gpre_w[k][i] = fmaf(gnv, out * ro, gpre_w[k][i]);
+        const float t = (float)go_r[k].v[i] + (has_n ? norm_grad(gnv * w[i], out, ro, c1, a.D, a.eps) : 0.f);
+        const float fh = (float)fr[k].v[i] * rf, post = fh * wp[i], gpost = t * sc[i] * act;
+        go[k][i] = t;
+        gscale[k][i] = fmaf(t, act * post, gscale[k][i]);
+        gpost_w[k][i] = fmaf(gpost, fh, gpost_w[k][i]);
+        gg[i] = t * sc[i] * post * gate_slope(a.act, gv, sg);
+        u[k][i] = gpost * wp[i];
+        s = fmaf(u[k][i], (float)fr[k].v[i], s);
+      }
+      if (nc > 0) {
+        if (g.gx) store_some<T, V>(static_cast<T *>(g.gx) + row * g.gx_stride + c, go[k], nc);
+        if (g.ggate) store_some<T, V>(static_cast<T *>(g.ggate) + row * g.ggate_stride + c, gg, nc);
+      }
+    }
+    if (g.gf) {
+      const float c2 = normed ? rf * rf * rf * invD * row_sum<TPR>(s, red, turn) : 0.f;
+      T *gf = static_cast<T *>(g.gf) + row * g.gf_stride;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        const int c = (k * TPR + tid) * V, nc = a.D - c;
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+          if (normed) u[k][i] = norm_grad(u[k][i], (float)fr[k].v[i], rf, c2, a.D, a.eps);
+        if (nc > 0) store_some<T, V>(gf + c, u[k], nc);
+      }
+    }
+  }
+  if (part == nullptr) return;
+  float *p = part + first * 3 * a.D;
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int c = (k * TPR + tid) * V, nc = a.D - c;
+    if (nc <= 0) continue;
+    store_some<float, V>(p + c, gscale[k], nc);
+    store_some<float, V>(p + a.D + c, gpost_w[k], nc);
+    store_some<float, V>(p + 2 * a.D + c, gpre_w[k], nc);
+  }
+}
+
+namespace {
+
+// f(threads a row, vectors a thread) for rows of `vecs` vectors: as few threads as hold the row.
+template <class F>
+hipError_t by_fwd_row(int vecs, F &&f) {
+  using std::integral_constant;
+#define FDC_ROW(TPR, NV) \
+  if (vecs <= TPR * NV) return f(integral_constant<int, TPR>{}, integral_constant<int, NV>{});
+  FDC_ROW(64, 1)
+  FDC_ROW(64, 2)
+  FDC_ROW(64, 4)
+  FDC_ROW(256, 2)
+  FDC_ROW(256, 4)
+  return f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+}
+// The backward has five rows, three rows of parameters and their sums in registers: four channels a
+// thread up to 4096 channels, eight beyond.
+template <class F>
+hipError_t by_bwd_row(int vecs, F &&f) {
+  using std::integral_constant;
+  FDC_ROW(64, 1)
+  FDC_ROW(128, 1)
+  FDC_ROW(256, 1)
+  FDC_ROW(512, 1)
+  FDC_ROW(1024, 1)
+  return f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+#undef FDC_ROW
+}
+
+template <class T>
+int fwd_vecs(int D) {
+  return (int)ceil_div(D, kNormV<T>);
+}
+int bwd_vecs(int D) { return (int)ceil_div(D, kBwdV); }
+// Workgroups of the backward: enough to fill the chip, few enough that their sums of the parameters'
+// gradients are little next to the rows.
+long long bwd_blocks(int64_t R, int rows_per_block) { return std::min<long long>(ceil_div(R, rows_per_block), 1024); }
+
+}  // namespace
+
+hipError_t launch_block_norm_fwd(const fdc_block_norm_args &a, void *out, int64_t out_stride, void *n,
+                                 int64_t n_stride, float *stats, hipStream_t s) {
+  const NormOut o{out, n, out_stride, n_stride, stats};
+  return by_dtype(a.dtype, [&](auto tag) {
+    using T = decltype(tag);
+    return by_fwd_row(fwd_vecs<T>(a.D), [&](auto tpr, auto nv) {
+      constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value, RPB = kRows<TPR>;
+      const long long blocks = ceil_div(a.R, RPB), x = std::min<long long>(blocks, 1 << 20);
+      return timed_launch("block_norm_fwd", k_block_norm_fwd<T, TPR, NV>, dim3((unsigned)x, (unsigned)ceil_div(blocks, x)),
+                          dim3(TPR * RPB), 0, s, a, o);
+    });
+  });
+}
+
+size_t block_norm_bwd_ws_floats(int64_t R, int D) {
+  size_t n = 0;
+  (void)by_bwd_row(bwd_vecs(D), [&](auto tpr, auto) {
+    constexpr int TPR = decltype(tpr)::value, RPB = kRows<TPR>;
+    n = (size_t)bwd_blocks(R, RPB) * RPB * 3 * D;
+    return hipSuccess;
+  });
+  return n;
+}
+
+hipError_t launch_block_norm_bwd(const fdc_block_norm_args &a, const float *stats, const fdc_block_norm_grads &g,
+                                 float *part, hipStream_t s) {
+  float *p = g.gscale || g.gw_post || g.gw_pre ? part : nullptr;
+  long long sharers = 0;
+  const hipError_t e = by_dtype(a.dtype, [&](auto tag) {
+    using T = decltype(tag);
+    return by_bwd_row(bwd_vecs(a.D), [&](auto tpr, auto nv) {
+      constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value, RPB = kRows<TPR>;
+      const long long blocks = bwd_blocks(a.R, RPB);
+      sharers = blocks * RPB;
+      return timed_launch("block_norm_bwd", k_block_norm_bwd<T, TPR, NV>, dim3((unsigned)blocks), dim3(TPR * RPB), 0, s,
+                          a, g, stats, p);
+    });
+  });
+  if (e != hipSuccess || p == nullptr) return e;
+  ColSegments segs{};
+  segs.count = 3;
+  float *outs[3] = {g.gscale, g.gw_post, g.gw_pre};
+  for (int i = 0; i < 3; ++i) segs.seg[i] = ColSegment{outs[i], a.D, a.D, 1};
+  return launch_col_sums(p, sharers, 3LL * a.D, segs, s);
+}
+
+}  // namespace fdc
