@@ -534,8 +534,9 @@ fdc_status fdc_block_norm_backward(const fdc_block_norm_args *a, const float *st
  * first term.  weight [R] float32 (NULL: 1); a row of weight 0 has loss 0 and gradient 0,
  * whatever it holds.  An index or label >= V gives a NaN loss and NaN gradients in its row.
  * An index given twice counts twice.  tau > 0, 0 <= alpha <= 1.
- * stats [R][4] float32 holds what the backward needs of the row: the largest logit, the sums
- * of exp(z - max) and of exp((z - max) / tau), and the logsumexp of teacher / tau. */
+ * stats [R][5] float32 holds what the backward needs of the row: the largest logit m, the sums of
+ * exp(z - m) and of exp((z - m) / tau) (0 where the row has no use of one), the teacher's largest logit and
+ * its sum. */
 typedef struct {
   int dtype, V, K;
   int64_t R;

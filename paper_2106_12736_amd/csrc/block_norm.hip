@@ -54,16 +54,13 @@ __device__ __forceinline__ void params(float (&w)[V], const float *p, int c, int
   if (p != nullptr && nc > 0) {
     const Pack<float, V> x = load_some<float, V>(p + c, nc);
 #pragma unroll
-    for (int i = 0; i < V; ++i) w[i] = x.v[i];
+    for (int i = 0; i < V; ++i) w[i] = x.at(i);
   }
 }
 template <class T, int V>
 __device__ __forceinline__ Pack<T, V> row_part(const T *p, int c, int nc) {
   if (p != nullptr && nc > 0) return load_some<T, V>(p + c, nc);
-  Pack<T, V> x;
-#pragma unroll
-  for (int i = 0; i < V; ++i) x.v[i] = (T)0.f;
-  return x;
+  return Pack<T, V>{};
 }
 
 struct NormOut {
@@ -98,7 +95,7 @@ __global__ __launch_bounds__(TPR * kRows<TPR>) void k_block_norm_fwd(fdc_block_n
 #pragma unroll
     for (int k = 0; k < NV; ++k)
 #pragma unroll
-      for (int i = 0; i < V; ++i) s = fmaf((float)fr[k].v[i], (float)fr[k].v[i], s);
+      for (int i = 0; i < V; ++i) s = fmaf(fr[k].at(i), fr[k].at(i), s);
     rf = 1.f / sqrtf(row_sum<TPR>(s, red, turn) * invD + a.eps);
   }
   float out[NV][V], s = 0.f;
@@ -110,10 +107,10 @@ __global__ __launch_bounds__(TPR * kRows<TPR>) void k_block_norm_fwd(fdc_block_n
     params<V>(sc, a.scale, c, nc);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const float g = (float)gr[k].v[i];
+      const float g = gr[k].at(i);
       const float act = gate ? gate_act(a.act, g, sigmoid(g)) : 1.f;
-      const float post = (float)fr[k].v[i] * rf * wp[i];
-      out[k][i] = fmaf(sc[i] * act, post, (float)xr[k].v[i]);
+      const float post = fr[k].at(i) * rf * wp[i];
+      out[k][i] = fmaf(sc[i] * act, post, xr[k].at(i));
       s = fmaf(out[k][i], out[k][i], s);
     }
     if (o.out != nullptr && nc > 0) store_some<T, V>(static_cast<T *>(o.out) + row * o.out_stride + c, out[k], nc);
@@ -190,11 +187,11 @@ __global__ __launch_bounds__(TPR * kRows<TPR>) void k_block_norm_bwd(fdc_block_n
       params<V>(w, a.w_pre, c, nc);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const float gv = (float)ar[k].v[i];
+        const float gv = ar[k].at(i);
         const float act = has_gate ? gate_act(a.act, gv, sigmoid(gv)) : 1.f;
-        const float out = fmaf(sc[i] * act, (float)fr[k].v[i] * rf * wp[i], (float)xr[k].v[i]);
+        const float out = fmaf(sc[i] * act, fr[k].at(i) * rf * wp[i], xr[k].at(i));
         go[k][i] = out;
-        s = fmaf((float)gn_r[k].v[i] * w[i], out, s);
+        s = fmaf(gn_r[k].at(i) * w[i], out, s);
       }
     }
     const float c1 = has_n ? ro * ro * ro * invD * row_sum<TPR>(s, red, turn) : 0.f;
@@ -209,17 +206,17 @@ __global__ __launch_bounds__(TPR * kRows<TPR>) void k_block_norm_bwd(fdc_block_n
       params<V>(w, a.w_pre, c, nc);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const float out = go[k][i], gnv = (float)gn_r[k].v[i], gv = (float)ar[k].v[i];
+        const float out = go[k][i], gnv = gn_r[k].at(i), gv = ar[k].at(i);
         const float sg = sigmoid(gv), act = has_gate ? gate_act(a.act, gv, sg) : 1.f;
         gpre_w[k][i] = fmaf(gnv, out * ro, gpre_w[k][i]);
-        const float t = (float)go_r[k].v[i] + (has_n ? norm_grad(gnv * w[i], out, ro, c1, a.D, a.eps) : 0.f);
-        const float fh = (float)fr[k].v[i] * rf, post = fh * wp[i], gpost = t * sc[i] * act;
+        const float t = go_r[k].at(i) + (has_n ? norm_grad(gnv * w[i], out, ro, c1, a.D, a.eps) : 0.f);
+        const float fh = fr[k].at(i) * rf, post = fh * wp[i], gpost = t * sc[i] * act;
         go[k][i] = t;
         gscale[k][i] = fmaf(t, act * post, gscale[k][i]);
         gpost_w[k][i] = fmaf(gpost, fh, gpost_w[k][i]);
         gg[i] = t * sc[i] * post * gate_slope(a.act, gv, sg);
         u[k][i] = gpost * wp[i];
-        s = fmaf(u[k][i], (float)fr[k].v[i], s);
+        s = fmaf(u[k][i], fr[k].at(i), s);
       }
       if (nc > 0) {
         if (g.gx) store_some<T, V>(static_cast<T *>(g.gx) + row * g.gx_stride + c, go[k], nc);
@@ -234,7 +231,7 @@ __global__ __launch_bounds__(TPR * kRows<TPR>) void k_block_norm_bwd(fdc_block_n
         const int c = (k * TPR + tid) * V, nc = a.D - c;
 #pragma unroll
         for (int i = 0; i < V; ++i)
-          if (normed) u[k][i] = norm_grad(u[k][i], (float)fr[k].v[i], rf, c2, a.D, a.eps);
+          if (normed) u[k][i] = norm_grad(u[k][i], fr[k].at(i), rf, c2, a.D, a.eps);
         if (nc > 0) store_some<T, V>(gf + c, u[k], nc);
       }
     }

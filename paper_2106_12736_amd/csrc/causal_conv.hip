@@ -22,7 +22,7 @@ __device__ __forceinline__ void row_or_zero(float (&f)[V], const T *base, int64_
   if (live) {
     const Pack<T, V> x = load_some<T, V>(base + (int64_t)t * stride, nch);
 #pragma unroll
-    for (int i = 0; i < V; ++i) f[i] = (float)x.v[i];
+    for (int i = 0; i < V; ++i) f[i] = x.at(i);
   } else {
 #pragma unroll
     for (int i = 0; i < V; ++i) f[i] = 0.f;

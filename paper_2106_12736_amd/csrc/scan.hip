@@ -65,7 +65,7 @@ __device__ __forceinline__ void load4(float (&v)[4], const float *p, int nvalid)
   if (nvalid > 0) {
     const Pack<float, 4> x = load_some<float, 4>(p, nvalid);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) v[r] = x.v[r];
+    for (int r = 0; r < 4; ++r) v[r] = x.at(r);
   }
 }
 __device__ __forceinline__ void store4(float *p, const float (&v)[4], int nvalid) {
@@ -526,8 +526,8 @@ __global__ __launch_bounds__(256) void k_scan_step(fdc_scan_args a, int Dg) {
   const float delta = step_size(raw, a.softplus), u = delta * x;
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
-    h[r] = fmaf(exp2_fast(delta * (A[r] * kLog2e)), h[r], u * (float)Bv.v[r]);
-    s = fmaf((float)Cv.v[r], h[r], s);
+    h[r] = fmaf(exp2_fast(delta * (A[r] * kLog2e)), h[r], u * Bv.at(r));
+    s = fmaf(Cv.at(r), h[r], s);
   }
   store4(a.h_last + at, h, nvalid);
   s = lane_sum<LN>(s);

@@ -20,6 +20,7 @@ constexpr int kScanMaxStates = 64;
 constexpr int kScanBlock = 16;  // tokens between two saved states
 constexpr int kNormMaxWidth = 8192;
 constexpr int kDistillMaxTeacher = 1024;
+constexpr int kDistillStats = 5;  // floats a row that the forward keeps for the backward
 
 hipError_t launch_causal_conv_fwd(const fdc_causal_conv_args &a, hipStream_t s);
 size_t causal_conv_bwd_ws(int dtype, int B, int L, int D, int n);  // bytes
@@ -72,12 +73,31 @@ inline long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 // ---- device ----------------------------------------------------------------
 #ifdef __HIPCC__
 
-// V consecutive elements from any element-aligned address (16-byte global accesses need no
-// alignment beyond the element's on this hardware), as floats.
+// V consecutive elements in 32-bit words as they lie in memory (16-bit elements stay two a register).
 template <class T, int V>
 struct Pack {
-  T v[V];
+  static constexpr int W = V * (int)sizeof(T) / 4;
+  unsigned w[W];
+  __device__ __forceinline__ float at(int i) const {
+    if constexpr (sizeof(T) == 4) {
+      return __uint_as_float(w[i]);
+    } else if constexpr (std::is_same_v<T, __bf16>) {
+      return __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+    } else {
+      const unsigned short h = (unsigned short)(i % 2 ? w[i / 2] >> 16 : w[i / 2]);
+      return (float)__builtin_bit_cast(_Float16, h);
+    }
+  }
 };
+template <class T>
+__device__ __forceinline__ unsigned element_bits(T v) {
+  if constexpr (sizeof(T) == 4)
+    return __float_as_uint(v);
+  else
+    return __builtin_bit_cast(unsigned short, v);
+}
+// From and to any element-aligned address (16-byte global accesses need no alignment beyond the
+// element's on this hardware).
 template <class T, int V>
 __device__ __forceinline__ Pack<T, V> load_pack(const T *p) {
   Pack<T, V> x;
@@ -86,18 +106,26 @@ __device__ __forceinline__ Pack<T, V> load_pack(const T *p) {
 }
 template <class T, int V>
 __device__ __forceinline__ void store_pack(T *p, const float (&f)[V]) {
-  Pack<T, V> x;
+  struct {
+    T v[V];
+  } x;
 #pragma unroll
   for (int i = 0; i < V; ++i) x.v[i] = (T)f[i];
   __builtin_memcpy(p, &x, sizeof x);
 }
-// The first n (>= 1) of V elements; the others are 0.
+// The first n (>= 1) of V elements; the others are `fill`.
 template <class T, int V>
-__device__ __forceinline__ Pack<T, V> load_some(const T *p, int n) {
+__device__ __forceinline__ Pack<T, V> load_some(const T *p, int n, float fill = 0.f) {
   if (n >= V) return load_pack<T, V>(p);
+  constexpr int E = 4 / sizeof(T);  // elements a word
   Pack<T, V> x;
 #pragma unroll
-  for (int i = 0; i < V; ++i) x.v[i] = i < n ? p[i] : (T)0.f;
+  for (int j = 0; j < Pack<T, V>::W; ++j) {
+    x.w[j] = 0;
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+      x.w[j] |= element_bits<T>(j * E + i < n ? p[j * E + i] : (T)fill) << (i * 8 * (int)sizeof(T) % 32);
+  }
   return x;
 }
 template <class T, int V>

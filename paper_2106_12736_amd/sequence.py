@@ -298,7 +298,7 @@ def distill_forward(z, idx, teacher, temperature=1.0, labels=None, alpha=1.0, we
     -1: absent) and, with labels [rows] (int32, -1: none), 1 - alpha of the cross-entropy
     (fdc_distill_forward) -> (loss [rows], stats)."""
     a = _distill_args(z, idx, teacher, temperature, labels, alpha, weight)
-    loss, stats = _empty((a.R,), z, torch.float32), _empty((a.R, 4), z, torch.float32)
+    loss, stats = _empty((a.R,), z, torch.float32), _empty((a.R, 5), z, torch.float32)
     ws = _distill_ws(a, z)
     call("fdc_distill_forward", a, _ptr(loss), _ptr(stats), _ptr(ws), ws.numel(), _stream())
     return loss, stats
@@ -309,7 +309,7 @@ def distill_backward(gloss, stats, z, idx, teacher, temperature=1.0, labels=None
     a = _distill_args(z, idx, teacher, temperature, labels, alpha, weight)
     gz = _empty(z.shape, z) if gz is None else gz
     gp, gs = _rows(gz, z, z.shape, "gz")
-    call("fdc_distill_backward", a, _f32(stats, z, (a.R, 4), "stats"), _f32(gloss, z, (a.R,), "gloss"), gp, gs,
+    call("fdc_distill_backward", a, _f32(stats, z, (a.R, 5), "stats"), _f32(gloss, z, (a.R,), "gloss"), gp, gs,
          _stream())
     return gz
 
@@ -317,7 +317,7 @@ def distill_backward(gloss, stats, z, idx, teacher, temperature=1.0, labels=None
 def distill_forward_backward(gloss, z, idx, teacher, temperature=1.0, labels=None, alpha=1.0, weight=None, gz=None):
     """Loss and gradient in one call, for a gradient of the loss that is known beforehand -> (loss, gz)."""
     a = _distill_args(z, idx, teacher, temperature, labels, alpha, weight)
-    loss, stats = _empty((a.R,), z, torch.float32), _empty((a.R, 4), z, torch.float32)
+    loss, stats = _empty((a.R,), z, torch.float32), _empty((a.R, 5), z, torch.float32)
     gz = _empty(z.shape, z) if gz is None else gz
     gp, gs = _rows(gz, z, z.shape, "gz")
     ws = _distill_ws(a, z)
