@@ -417,7 +417,7 @@ fdc_status fdc_adam_step(float *p, const float *g, float *m, float *v, int64_t n
  *            is formed in float32 and each output is rounded once.
  * Tokens.    fdc_tokens is a [B][L][width] tensor: element (b, t, c) is at
  *            p[b * batch_stride + t * token_stride + c] (strides in elements, >= 0,
- *            token_stride below 2^26).  p == NULL: the tensor is absent, where that is
+ *            token_stride below 2^25).  p == NULL: the tensor is absent, where that is
  *            allowed.  Input strides may be 0 (one row for every token); the elements
  *            of an output must not overlap.  No alignment beyond the type's own is
  *            asked for.

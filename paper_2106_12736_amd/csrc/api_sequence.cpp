@@ -11,7 +11,7 @@ using fdc::fail;
 
 namespace {
 
-constexpr int64_t kMaxTokenStride = 1LL << 26;
+constexpr int64_t kMaxTokenStride = 1LL << 25;
 constexpr int64_t kMaxElements = 1LL << 46;  // of a tensor, and of a batch stride: products stay far below 2^63
 
 fdc_status check_dtype(int dtype) {
