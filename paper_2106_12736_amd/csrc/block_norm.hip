@@ -9,8 +9,10 @@
 //   u = gpost w_post;  gf = u rf - f rf^3 mean(u f);  gw_post = sum gpost fh
 //
 // A row is in the registers of the threads that share it, so everything is read and written once;
-// both directions are bound by HBM.  The sums over a row are formed in float32, across the wave
-// by lane moves and across waves through LDS.
+// both directions are bound by HBM.  Workgroups take row after row and keep the parameters in
+// registers (read again for every row they would be more than the row itself), and the next row's
+// loads are on their way while a row is worked on.  The sums over a row are formed in float32, across
+// the wave by lane moves and across waves through LDS.
 #include <algorithm>
 
 #include "sequence.h"
@@ -69,68 +71,87 @@ struct NormOut {
   float *stats;
 };
 
+// The part of a row that a thread holds of `Count` tensors.
+template <class T, int V, int NV, int Count>
+struct RowParts {
+  Pack<T, V> r[Count][NV];
+  template <int TPR>
+  __device__ __forceinline__ void load(const T *const (&p)[Count], const int64_t (&stride)[Count], int64_t row, int tid,
+                                       int D) {
+#pragma unroll
+    for (int j = 0; j < Count; ++j)
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        const int c = (k * TPR + tid) * V;
+        r[j][k] = row_part<T, V>(p[j] ? p[j] + row * stride[j] : nullptr, c, D - c);
+      }
+  }
+};
+
 template <class T, int TPR, int NV>
 __global__ __launch_bounds__(TPR * kRows<TPR>) void k_block_norm_fwd(fdc_block_norm_args a, NormOut o) {
   constexpr int V = kNormV<T>, RPB = kRows<TPR>;
   __shared__ float red[2 * (TPR / 64)];
   int turn = 0;
   const int tid = threadIdx.x % TPR;
-  const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * RPB + threadIdx.x / TPR;
-  if (row >= a.R) return;  // whole waves, and no barrier follows where a workgroup has several rows
-  const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
-  const T *f = a.f ? static_cast<const T *>(a.f) + row * a.f_stride : nullptr;
-  const T *gate = a.gate ? static_cast<const T *>(a.gate) + row * a.gate_stride : nullptr;
-  Pack<T, V> xr[NV], fr[NV], gr[NV];
-#pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    const int c = (k * TPR + tid) * V, nc = a.D - c;
-    xr[k] = row_part<T, V>(x, c, nc);
-    fr[k] = row_part<T, V>(f, c, nc);
-    gr[k] = row_part<T, V>(gate, c, nc);
-  }
+  const int64_t first = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR, step = (int64_t)gridDim.x * RPB;
+  const T *const src[3] = {static_cast<const T *>(a.x), static_cast<const T *>(a.f), static_cast<const T *>(a.gate)};
+  const int64_t stride[3] = {a.x_stride, a.f_stride, a.gate_stride};
   const float invD = 1.f / (float)a.D;
-  float rf = 1.f, ro = 1.f;
-  if (f != nullptr && a.w_post != nullptr) {
-    float s = 0.f;
-#pragma unroll
-    for (int k = 0; k < NV; ++k)
-#pragma unroll
-      for (int i = 0; i < V; ++i) s = fmaf(fr[k].at(i), fr[k].at(i), s);
-    rf = 1.f / sqrtf(row_sum<TPR>(s, red, turn) * invD + a.eps);
-  }
-  float out[NV][V], s = 0.f;
+  const bool has_gate = a.gate != nullptr, normed = a.f != nullptr && a.w_post != nullptr;
+  float wp[NV][V], sc[NV][V], w[NV][V];
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
-    const int c = (k * TPR + tid) * V, nc = a.D - c;
-    float wp[V], sc[V];
-    params<V>(wp, a.w_post, c, nc);
-    params<V>(sc, a.scale, c, nc);
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const float g = gr[k].at(i);
-      const float act = gate ? gate_act(a.act, g, sigmoid(g)) : 1.f;
-      const float post = fr[k].at(i) * rf * wp[i];
-      out[k][i] = fmaf(sc[i] * act, post, xr[k].at(i));
-      s = fmaf(out[k][i], out[k][i], s);
-    }
-    if (o.out != nullptr && nc > 0) store_some<T, V>(static_cast<T *>(o.out) + row * o.out_stride + c, out[k], nc);
+    const int c = (k * TPR + tid) * V;
+    params<V>(wp[k], a.w_post, c, a.D - c);
+    params<V>(sc[k], a.scale, c, a.D - c);
+    params<V>(w[k], a.w_pre, c, a.D - c);
   }
-  if (a.w_pre != nullptr) {
-    ro = 1.f / sqrtf(row_sum<TPR>(s, red, turn) * invD + a.eps);
-    T *n = static_cast<T *>(o.n) + row * o.n_stride;
+  constexpr bool Ahead = NV == 1;  // two vectors a thread leave no registers for the next row
+  RowParts<T, V, NV, 3> in, next;
+  if (Ahead && first < a.R) in.template load<TPR>(src, stride, first, tid, a.D);
+  for (int64_t row = first; row < a.R; row += step) {
+    if (!Ahead)
+      in.template load<TPR>(src, stride, row, tid, a.D);
+    else if (row + step < a.R)
+      next.template load<TPR>(src, stride, row + step, tid, a.D);
+    float rf = 1.f, ro = 1.f, s = 0.f;
+    if (normed) {
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int i = 0; i < V; ++i) s = fmaf(in.r[1][k].at(i), in.r[1][k].at(i), s);
+      rf = 1.f / sqrtf(row_sum<TPR>(s, red, turn) * invD + a.eps);
+    }
+    float out[NV][V];
+    s = 0.f;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const int c = (k * TPR + tid) * V, nc = a.D - c;
-      float w[V];
-      params<V>(w, a.w_pre, c, nc);
 #pragma unroll
-      for (int i = 0; i < V; ++i) w[i] *= out[k][i] * ro;
-      if (nc > 0) store_some<T, V>(n + c, w, nc);
+      for (int i = 0; i < V; ++i) {
+        const float g = in.r[2][k].at(i);
+        const float act = has_gate ? gate_act(a.act, g, sigmoid(g)) : 1.f;
+        out[k][i] = fmaf(sc[k][i] * act, in.r[1][k].at(i) * rf * wp[k][i], in.r[0][k].at(i));
+        s = fmaf(out[k][i], out[k][i], s);
+      }
+      if (o.out != nullptr && nc > 0) store_some<T, V>(static_cast<T *>(o.out) + row * o.out_stride + c, out[k], nc);
     }
-  }
-  if (o.stats != nullptr && tid == 0) {
-    o.stats[2 * row] = rf;
-    o.stats[2 * row + 1] = ro;
+    if (o.n != nullptr) {
+      ro = 1.f / sqrtf(row_sum<TPR>(s, red, turn) * invD + a.eps);
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        const int c = (k * TPR + tid) * V, nc = a.D - c;
+#pragma unroll
+        for (int i = 0; i < V; ++i) out[k][i] *= ro * w[k][i];
+        if (nc > 0) store_some<T, V>(static_cast<T *>(o.n) + row * o.n_stride + c, out[k], nc);
+      }
+    }
+    if (o.stats != nullptr && tid == 0) {
+      o.stats[2 * row] = rf;
+      o.stats[2 * row + 1] = ro;
+    }
+    if (Ahead) in = next;
   }
 }
 
@@ -152,46 +173,50 @@ __global__ __launch_bounds__(TPR * kRows<TPR>) void k_block_norm_bwd(fdc_block_n
   int turn = 0;
   const int tid = threadIdx.x % TPR;
   const int64_t first = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR, step = (int64_t)gridDim.x * RPB;
-  const bool has_f = a.f != nullptr, has_gate = a.gate != nullptr, normed = a.w_post != nullptr;
+  const bool has_gate = a.gate != nullptr, normed = a.w_post != nullptr;
   const bool has_n = g.gn != nullptr && a.w_pre != nullptr;
+  const T *const src[5] = {static_cast<const T *>(a.x), static_cast<const T *>(a.f), static_cast<const T *>(a.gate),
+                           static_cast<const T *>(g.gout), has_n ? static_cast<const T *>(g.gn) : nullptr};
+  const int64_t stride[5] = {a.x_stride, a.f_stride, a.gate_stride, g.gout_stride, g.gn_stride};
   const float invD = 1.f / (float)a.D;
-  float gscale[NV][V], gpost_w[NV][V], gpre_w[NV][V];
+  constexpr bool Ahead = NV == 1;  // two vectors a thread leave no registers for the next row or the parameters
+  float gscale[NV][V], gpost_w[NV][V], gpre_w[NV][V], wp[V], sc[V], w[V];
+  auto load_params = [&](int k) {
+    const int c = (k * TPR + tid) * V;
+    params<V>(wp, a.w_post, c, a.D - c);
+    params<V>(sc, a.scale, c, a.D - c);
+    params<V>(w, a.w_pre, c, a.D - c);
+  };
+  if (Ahead) load_params(0);
 #pragma unroll
   for (int k = 0; k < NV; ++k)
 #pragma unroll
     for (int i = 0; i < V; ++i) gscale[k][i] = gpost_w[k][i] = gpre_w[k][i] = 0.f;
+  RowParts<T, V, NV, 5> in, next;
+  float2 st = make_float2(1.f, 1.f), next_st = st;
+  if (Ahead && first < a.R) {
+    in.template load<TPR>(src, stride, first, tid, a.D);
+    st = reinterpret_cast<const float2 *>(stats)[first];
+  }
   for (int64_t row = first; row < a.R; row += step) {
-    Pack<T, V> xr[NV], fr[NV], ar[NV], go_r[NV], gn_r[NV];
-    const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
-    const T *f = has_f ? static_cast<const T *>(a.f) + row * a.f_stride : nullptr;
-    const T *gate = has_gate ? static_cast<const T *>(a.gate) + row * a.gate_stride : nullptr;
-    const T *gout = g.gout ? static_cast<const T *>(g.gout) + row * g.gout_stride : nullptr;
-    const T *gn = has_n ? static_cast<const T *>(g.gn) + row * g.gn_stride : nullptr;
-#pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      const int c = (k * TPR + tid) * V, nc = a.D - c;
-      xr[k] = row_part<T, V>(x, c, nc);
-      fr[k] = row_part<T, V>(f, c, nc);
-      ar[k] = row_part<T, V>(gate, c, nc);
-      go_r[k] = row_part<T, V>(gout, c, nc);
-      gn_r[k] = row_part<T, V>(gn, c, nc);
+    if (!Ahead) {
+      in.template load<TPR>(src, stride, row, tid, a.D);
+      st = reinterpret_cast<const float2 *>(stats)[row];
+    } else if (row + step < a.R) {
+      next.template load<TPR>(src, stride, row + step, tid, a.D);
+      next_st = reinterpret_cast<const float2 *>(stats)[row + step];
     }
-    const float rf = stats[2 * row], ro = stats[2 * row + 1];
-    float s = 0.f, go[NV][V];
+    const float rf = st.x, ro = st.y;
+    float s = 0.f, go[NV][V], act[NV][V];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const int c = (k * TPR + tid) * V, nc = a.D - c;
-      float wp[V], sc[V], w[V];
-      params<V>(wp, a.w_post, c, nc);
-      params<V>(sc, a.scale, c, nc);
-      params<V>(w, a.w_pre, c, nc);
+      if (!Ahead) load_params(k);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const float gv = ar[k].at(i);
-        const float act = has_gate ? gate_act(a.act, gv, sigmoid(gv)) : 1.f;
-        const float out = fmaf(sc[i] * act, fr[k].at(i) * rf * wp[i], xr[k].at(i));
-        go[k][i] = out;
-        s = fmaf(gn_r[k].at(i) * w[i], out, s);
+        const float gv = in.r[2][k].at(i);
+        act[k][i] = has_gate ? gate_act(a.act, gv, sigmoid(gv)) : 1.f;
+        go[k][i] = fmaf(sc[i] * act[k][i], in.r[1][k].at(i) * rf * wp[i], in.r[0][k].at(i));  // out
+        s = fmaf(in.r[4][k].at(i) * w[i], go[k][i], s);
       }
     }
     const float c1 = has_n ? ro * ro * ro * invD * row_sum<TPR>(s, red, turn) : 0.f;
@@ -200,23 +225,23 @@ __global__ __launch_bounds__(TPR * kRows<TPR>) void k_block_norm_bwd(fdc_block_n
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const int c = (k * TPR + tid) * V, nc = a.D - c;
-      float wp[V], sc[V], w[V], gg[V];
-      params<V>(wp, a.w_post, c, nc);
-      params<V>(sc, a.scale, c, nc);
-      params<V>(w, a.w_pre, c, nc);
+      float gg[V];
+      if (!Ahead) load_params(k);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const float out = go[k][i], gnv = gn_r[k].at(i), gv = ar[k].at(i);
-        const float sg = sigmoid(gv), act = has_gate ? gate_act(a.act, gv, sg) : 1.f;
+        const float out = go[k][i], gnv = in.r[4][k].at(i), f = in.r[1][k].at(i);
         gpre_w[k][i] = fmaf(gnv, out * ro, gpre_w[k][i]);
-        const float t = go_r[k].at(i) + (has_n ? norm_grad(gnv * w[i], out, ro, c1, a.D, a.eps) : 0.f);
-        const float fh = fr[k].at(i) * rf, post = fh * wp[i], gpost = t * sc[i] * act;
+        const float t = in.r[3][k].at(i) + (has_n ? norm_grad(gnv * w[i], out, ro, c1, a.D, a.eps) : 0.f);
+        const float fh = f * rf, post = fh * wp[i], gpost = t * sc[i] * act[k][i];
         go[k][i] = t;
-        gscale[k][i] = fmaf(t, act * post, gscale[k][i]);
+        gscale[k][i] = fmaf(t, act[k][i] * post, gscale[k][i]);
         gpost_w[k][i] = fmaf(gpost, fh, gpost_w[k][i]);
-        gg[i] = t * sc[i] * post * gate_slope(a.act, gv, sg);
+        if (has_gate) {
+          const float gv = in.r[2][k].at(i);
+          gg[i] = t * sc[i] * post * gate_slope(a.act, gv, sigmoid(gv));
+        }
         u[k][i] = gpost * wp[i];
-        s = fmaf(u[k][i], fr[k].at(i), s);
+        s = fmaf(u[k][i], f, s);
       }
       if (nc > 0) {
         if (g.gx) store_some<T, V>(static_cast<T *>(g.gx) + row * g.gx_stride + c, go[k], nc);
@@ -225,15 +250,18 @@ __global__ __launch_bounds__(TPR * kRows<TPR>) void k_block_norm_bwd(fdc_block_n
     }
     if (g.gf) {
       const float c2 = normed ? rf * rf * rf * invD * row_sum<TPR>(s, red, turn) : 0.f;
-      T *gf = static_cast<T *>(g.gf) + row * g.gf_stride;
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
         const int c = (k * TPR + tid) * V, nc = a.D - c;
+        if (normed)
 #pragma unroll
-        for (int i = 0; i < V; ++i)
-          if (normed) u[k][i] = norm_grad(u[k][i], fr[k].at(i), rf, c2, a.D, a.eps);
-        if (nc > 0) store_some<T, V>(gf + c, u[k], nc);
+          for (int i = 0; i < V; ++i) u[k][i] = norm_grad(u[k][i], in.r[1][k].at(i), rf, c2, a.D, a.eps);
+        if (nc > 0) store_some<T, V>(static_cast<T *>(g.gf) + row * g.gf_stride + c, u[k], nc);
       }
+    }
+    if (Ahead) {
+      in = next;
+      st = next_st;
     }
   }
   if (part == nullptr) return;
@@ -250,31 +278,22 @@ __global__ __launch_bounds__(TPR * kRows<TPR>) void k_block_norm_bwd(fdc_block_n
 
 namespace {
 
-// f(threads a row, vectors a thread) for rows of `vecs` vectors: as few threads as hold the row.
-template <class F>
-hipError_t by_fwd_row(int vecs, F &&f) {
+// f(threads a row, vectors a thread) for rows of `vecs` vectors: as few threads as hold the row, a vector
+// each up to 1024 of them.  (Forward vectors are 16 bytes; the backward, which has five rows, three
+// parameters and their sums in registers, takes four channels a thread.)
+template <int MostNV, class F>
+hipError_t by_row(int vecs, F &&f) {
   using std::integral_constant;
 #define FDC_ROW(TPR, NV) \
   if (vecs <= TPR * NV) return f(integral_constant<int, TPR>{}, integral_constant<int, NV>{});
-  FDC_ROW(64, 1)
-  FDC_ROW(64, 2)
-  FDC_ROW(64, 4)
-  FDC_ROW(256, 2)
-  FDC_ROW(256, 4)
-  return f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
-}
-// The backward has five rows, three rows of parameters and their sums in registers: four channels a
-// thread up to 4096 channels, eight beyond.
-template <class F>
-hipError_t by_bwd_row(int vecs, F &&f) {
-  using std::integral_constant;
   FDC_ROW(64, 1)
   FDC_ROW(128, 1)
   FDC_ROW(256, 1)
   FDC_ROW(512, 1)
   FDC_ROW(1024, 1)
-  return f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
 #undef FDC_ROW
+  if constexpr (MostNV == 2) return f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+  return hipErrorInvalidValue;
 }
 
 template <class T>
@@ -282,9 +301,18 @@ int fwd_vecs(int D) {
   return (int)ceil_div(D, kNormV<T>);
 }
 int bwd_vecs(int D) { return (int)ceil_div(D, kBwdV); }
-// Workgroups of the backward: enough to fill the chip, few enough that their sums of the parameters'
-// gradients are little next to the rows.
-long long bwd_blocks(int64_t R, int rows_per_block) { return std::min<long long>(ceil_div(R, rows_per_block), 1024); }
+// Workgroups: the forward's as many as run at once (eight waves a SIMD); the backward's half of that, by
+// its registers, and because each leaves its sums of the parameters' gradients.
+constexpr long long kCus = 256;
+long long row_blocks(int64_t R, int rows, int threads, int waves_a_simd) {
+  return std::min<long long>(ceil_div(R, rows), kCus * 256 * waves_a_simd / threads);
+}
+template <int TPR>
+long long bwd_blocks(int64_t R) {
+  const long long most = row_blocks(R, kRows<TPR>, TPR * kRows<TPR>, 4);
+  // four rows each at least, once every compute unit has a workgroup
+  return std::min(most, std::max(kCus, ceil_div(R, 4 * kRows<TPR>)));
+}
 
 }  // namespace
 
@@ -293,20 +321,20 @@ hipError_t launch_block_norm_fwd(const fdc_block_norm_args &a, void *out, int64_
   const NormOut o{out, n, out_stride, n_stride, stats};
   return by_dtype(a.dtype, [&](auto tag) {
     using T = decltype(tag);
-    return by_fwd_row(fwd_vecs<T>(a.D), [&](auto tpr, auto nv) {
+    return by_row<kNormMaxWidth / (1024 * kNormV<T>)>(fwd_vecs<T>(a.D), [&](auto tpr, auto nv) {
       constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value, RPB = kRows<TPR>;
-      const long long blocks = ceil_div(a.R, RPB), x = std::min<long long>(blocks, 1 << 20);
-      return timed_launch("block_norm_fwd", k_block_norm_fwd<T, TPR, NV>, dim3((unsigned)x, (unsigned)ceil_div(blocks, x)),
-                          dim3(TPR * RPB), 0, s, a, o);
+      const long long blocks = row_blocks(a.R, RPB, TPR * RPB, 8);
+      return timed_launch("block_norm_fwd", k_block_norm_fwd<T, TPR, NV>, dim3((unsigned)blocks), dim3(TPR * RPB), 0, s, a,
+                          o);
     });
   });
 }
 
 size_t block_norm_bwd_ws_floats(int64_t R, int D) {
   size_t n = 0;
-  (void)by_bwd_row(bwd_vecs(D), [&](auto tpr, auto) {
+  (void)by_row<kNormMaxWidth / (1024 * kBwdV)>(bwd_vecs(D), [&](auto tpr, auto) {
     constexpr int TPR = decltype(tpr)::value, RPB = kRows<TPR>;
-    n = (size_t)bwd_blocks(R, RPB) * RPB * 3 * D;
+    n = (size_t)bwd_blocks<TPR>(R) * RPB * 3 * D;
     return hipSuccess;
   });
   return n;
@@ -318,9 +346,9 @@ hipError_t launch_block_norm_bwd(const fdc_block_norm_args &a, const float *stat
   long long sharers = 0;
   const hipError_t e = by_dtype(a.dtype, [&](auto tag) {
     using T = decltype(tag);
-    return by_bwd_row(bwd_vecs(a.D), [&](auto tpr, auto nv) {
+    return by_row<kNormMaxWidth / (1024 * kBwdV)>(bwd_vecs(a.D), [&](auto tpr, auto nv) {
       constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value, RPB = kRows<TPR>;
-      const long long blocks = bwd_blocks(a.R, RPB);
+      const long long blocks = bwd_blocks<TPR>(a.R);
       sharers = blocks * RPB;
       return timed_launch("block_norm_bwd", k_block_norm_bwd<T, TPR, NV>, dim3((unsigned)blocks), dim3(TPR * RPB), 0, s,
                           a, g, stats, p);

@@ -18,28 +18,42 @@ struct ConvGrid {
 };
 
 template <class T, int V>
-__device__ __forceinline__ void row_or_zero(float (&f)[V], const T *base, int64_t stride, int t, bool live, int nch) {
-  if (live) {
-    const Pack<T, V> x = load_some<T, V>(base + (int64_t)t * stride, nch);
+__device__ __forceinline__ Pack<T, V> row_or_zero(const T *base, int64_t stride, int t, bool live, int nch) {
+  return live ? load_some<T, V>(base + (int64_t)t * stride, nch) : Pack<T, V>{};
+}
+template <class T, int V>
+__device__ __forceinline__ void unpack(float (&f)[V], const Pack<T, V> &x) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) f[i] = x.at(i);
-  } else {
-#pragma unroll
-    for (int i = 0; i < V; ++i) f[i] = 0.f;
-  }
+  for (int i = 0; i < V; ++i) f[i] = x.at(i);
 }
 
 // Token t of a sequence and, before it, of its state: zero before both and from `len` on.
 template <class T, int V>
-__device__ __forceinline__ void token_row(float (&f)[V], const T *xb, int64_t stride, const T *state, int D, int n,
-                                          int t, int len, int nch) {
-  if (t >= 0)
-    row_or_zero<T, V>(f, xb, stride, t, t < len, nch);
-  else
-    row_or_zero<T, V>(f, state, D, t + n - 1, state != nullptr, nch);
+__device__ __forceinline__ Pack<T, V> token_row(const T *xb, int64_t stride, const T *state, int D, int n, int t,
+                                                int len, int nch) {
+  return t >= 0 ? row_or_zero<T, V>(xb, stride, t, t < len, nch)
+                : row_or_zero<T, V>(state, D, t + n - 1, state != nullptr, nch);
 }
 
-constexpr int kConvUnroll = 4;  // tokens loaded together
+// The taps [V][N] and biases of a thread's channels (those of channels that are not there are 0): rows of w
+// lie one after another, so they are read in pieces of four whatever N is.
+template <int V, int N>
+__device__ __forceinline__ void load_taps(float (&w)[N][V], float (&bias)[V], const float *wp, const float *bp, int c0,
+                                          int nch) {
+  static_assert(V * N % 4 == 0);
+#pragma unroll
+  for (int m = 0; m < V * N / 4; ++m) {
+    const int n = nch * N - 4 * m;
+    const Pack<float, 4> x = n > 0 ? load_some<float, 4>(wp + (int64_t)c0 * N + 4 * m, n) : Pack<float, 4>{};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[(4 * m + e) % N][(4 * m + e) / N] = x.at(e);
+  }
+  const Pack<float, V> x = bp ? load_some<float, V>(bp + c0, nch) : Pack<float, V>{};
+#pragma unroll
+  for (int i = 0; i < V; ++i) bias[i] = x.at(i);
+}
+
+constexpr int kConvUnroll = 4;  // tokens loaded together, while the four before them are worked on
 
 template <class T, int V, int N>
 __global__ __launch_bounds__(256) void k_causal_conv_fwd(fdc_causal_conv_args a, ConvGrid cg) {
@@ -53,30 +67,37 @@ __global__ __launch_bounds__(256) void k_causal_conv_fwd(fdc_causal_conv_args a,
   const int t0 = tile * cg.run, t1 = min(a.L, t0 + cg.run);
 
   float w[N][V], bias[V], x[N - 1 + kConvUnroll][V];
+  load_taps<V, N>(w, bias, a.w, a.bias, c0, nch);
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
-    bias[i] = a.bias && i < nch ? a.bias[c0 + i] : 0.f;
+  for (int k = 0; k < N - 1; ++k)
+    unpack(x[k], token_row<T, V>(xb, a.x.token_stride, st, a.D, N, t0 - (N - 1) + k, len, nch));
+  Pack<T, V> next[kConvUnroll];
+  const int end = min(len, t1);
+  auto fetch = [&](int t) {
 #pragma unroll
-    for (int j = 0; j < N; ++j) w[j][i] = i < nch ? a.w[(int64_t)(c0 + i) * N + j] : 0.f;
-  }
-#pragma unroll
-  for (int k = 0; k < N - 1; ++k) token_row<T, V>(x[k], xb, a.x.token_stride, st, a.D, N, t0 - (N - 1) + k, len, nch);
+    for (int u = 0; u < kConvUnroll; ++u) next[u] = row_or_zero<T, V>(xb, a.x.token_stride, t + u, t + u < end, nch);
+  };
+  fetch(t0);
   if (tile == 0 && a.new_state != nullptr) {
     // rows len - (n - 1) .. len - 1 of the sequence with its state in front; only this thread reads
     // these channels' state (a run is no shorter than n - 1), and all of it is read before
     // new_state, which may be the same memory, is written
-    float keep[N][V];
+    Pack<T, V> keep[N];
 #pragma unroll
     for (int k = 0; k < N - 1; ++k)
-      token_row<T, V>(keep[k], xb, a.x.token_stride, st, a.D, N, len - (N - 1) + k, len, nch);
+      keep[k] = token_row<T, V>(xb, a.x.token_stride, st, a.D, N, len - (N - 1) + k, len, nch);
     T *ns = static_cast<T *>(a.new_state) + ((int64_t)b * (N - 1)) * a.D + c0;
 #pragma unroll
-    for (int k = 0; k < N - 1; ++k) store_some<T, V>(ns + (int64_t)k * a.D, keep[k], nch);
+    for (int k = 0; k < N - 1; ++k) {
+      float f[V];
+      unpack(f, keep[k]);
+      store_some<T, V>(ns + (int64_t)k * a.D, f, nch);
+    }
   }
   for (int t = t0; t < t1; t += kConvUnroll) {
 #pragma unroll
-    for (int u = 0; u < kConvUnroll; ++u)
-      row_or_zero<T, V>(x[N - 1 + u], xb, a.x.token_stride, t + u, t + u < min(len, t1), nch);
+    for (int u = 0; u < kConvUnroll; ++u) unpack(x[N - 1 + u], next[u]);
+    if (t + kConvUnroll < t1) fetch(t + kConvUnroll);
 #pragma unroll
     for (int u = 0; u < kConvUnroll; ++u) {
       float y[V];
@@ -112,31 +133,38 @@ __global__ __launch_bounds__(256) void k_causal_conv_bwd(fdc_causal_conv_args a,
   const int t0 = tile * cg.run, t1 = min(a.L, t0 + cg.run);
 
   float w[N][V], bias[V], x[N - 1 + kConvUnroll][V], gp[N - 1 + kConvUnroll][V], gw[N][V], gb[V];
+  load_taps<V, N>(w, bias, a.w, a.bias, c0, nch);
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    bias[i] = a.bias && i < nch ? a.bias[c0 + i] : 0.f;
     gb[i] = 0.f;
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      w[j][i] = i < nch ? a.w[(int64_t)(c0 + i) * N + j] : 0.f;
-      gw[j][i] = 0.f;
-    }
+    for (int j = 0; j < N; ++j) gw[j][i] = 0.f;
   }
 #pragma unroll
   for (int k = 0; k < N - 1; ++k) {
-    token_row<T, V>(x[k], xb, a.x.token_stride, st, a.D, N, t0 - (N - 1) + k, len, nch);
+    unpack(x[k], token_row<T, V>(xb, a.x.token_stride, st, a.D, N, t0 - (N - 1) + k, len, nch));
 #pragma unroll
     for (int i = 0; i < V; ++i) gp[k][i] = 0.f;
   }
   const int last = gxb ? t1 + N - 1 : t1;  // gp is wanted for t < last
+  const int end = min(len, last);
+  Pack<T, V> next_x[kConvUnroll], next_g[kConvUnroll];
+  auto fetch = [&](int t) {
+#pragma unroll
+    for (int u = 0; u < kConvUnroll; ++u) {
+      next_x[u] = row_or_zero<T, V>(xb, a.x.token_stride, t + u, t + u < end, nch);
+      next_g[u] = row_or_zero<T, V>(gyb, gy.token_stride, t + u, t + u < end, nch);
+    }
+  };
+  fetch(t0);
   for (int t = t0; t < last; t += kConvUnroll) {
     float g[kConvUnroll][V];
 #pragma unroll
     for (int u = 0; u < kConvUnroll; ++u) {
-      const bool live = t + u < min(len, last);
-      row_or_zero<T, V>(x[N - 1 + u], xb, a.x.token_stride, t + u, live, nch);
-      row_or_zero<T, V>(g[u], gyb, gy.token_stride, t + u, live, nch);
+      unpack(x[N - 1 + u], next_x[u]);
+      unpack(g[u], next_g[u]);
     }
+    if (t + kConvUnroll < last) fetch(t + kConvUnroll);
 #pragma unroll
     for (int u = 0; u < kConvUnroll; ++u) {
       const bool mine = t + u < t1;
@@ -203,7 +231,7 @@ template <class T>
 constexpr int kFwdV = sizeof(T) == 2 ? 8 : 4;  // 16 bytes a lane
 constexpr int kBwdV = 4;  // two windows and the sums of gw in registers
 
-ConvGrid bwd_grid(int B, int L, int D) { return conv_grid(B, L, D, kBwdV, 64, 1 << 17); }
+ConvGrid bwd_grid(int B, int L, int D) { return conv_grid(B, L, D, kBwdV, 128, 1 << 17); }
 
 template <class F>
 hipError_t by_taps(int n, F &&f) {
@@ -226,7 +254,7 @@ hipError_t launch_causal_conv_fwd(const fdc_causal_conv_args &a, hipStream_t s) 
     using T = decltype(tag);
     constexpr int V = kFwdV<T>;
     return by_taps(a.n, [&](auto taps) {
-      const ConvGrid cg = conv_grid(a.B, a.L, a.D, V, 32, 1 << 17);
+      const ConvGrid cg = conv_grid(a.B, a.L, a.D, V, 64, 1 << 17);
       const long long blocks = ceil_div((long long)cg.CV * cg.tiles, 256);
       return timed_launch("causal_conv_fwd", k_causal_conv_fwd<T, V, taps.value>, dim3((unsigned)blocks, a.B),
                           dim3(256), 0, s, a, cg);

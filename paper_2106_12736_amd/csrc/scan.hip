@@ -593,35 +593,48 @@ __global__ __launch_bounds__(256) void k_scan_sum_bc(const float *__restrict__ p
   static_cast<T *>(o.p)[b * o.batch_stride + t * o.token_stride + c] = (T)s;
 }
 
-// One token: LN lanes a (sequence, channel); a pass over the states (HBM: 8 bytes a state).
-template <class T, int LN>
+// One token: LN lanes a channel, for BT sequences, which the channel's parameters are read once for.  A
+// pass over the states (HBM: 8 bytes a state): 64 sequences, 4096 channels of 16 states move 34 MB.
+template <class T, int LN, int BT>
 __global__ __launch_bounds__(256) void k_scan_step(fdc_scan_args a, int Dg) {
-  const int i = blockIdx.x * (256 / LN) + threadIdx.x / LN, q = threadIdx.x % LN, b = blockIdx.y;
+  const int i = blockIdx.x * (256 / LN) + threadIdx.x / LN, q = threadIdx.x % LN, b0 = blockIdx.y * BT;
   const bool live = i < a.D;
-  const int d = live ? i : 0, g = d / Dg, nvalid = live ? max(0, min(4, a.N - 4 * q)) : 0;
-  const float x = (float)static_cast<const T *>(a.x.p)[b * a.x.batch_stride + d];
-  const float raw = (float)static_cast<const T *>(a.dt.p)[b * a.dt.batch_stride + d] + (a.dt_bias ? a.dt_bias[d] : 0.f);
-  const float gate = a.gate.p ? (float)static_cast<const T *>(a.gate.p)[b * a.gate.batch_stride + d] : 0.f;
-  const int64_t at = ((int64_t)b * a.D + d) * a.N + 4 * q;
-  float A[SN], h[SN], s = 0.f;
-  load_states(A, a.A + (int64_t)d * a.N + 4 * q, nvalid);
-  load_states(h, a.h0 + at, nvalid);
-  Pack<T, 4> Bv{}, Cv{};
-  if (nvalid > 0) {
-    Bv = load_some<T, 4>(static_cast<const T *>(a.Bm.p) + b * a.Bm.batch_stride + g * a.N + 4 * q, nvalid);
-    Cv = load_some<T, 4>(static_cast<const T *>(a.Cm.p) + b * a.Cm.batch_stride + g * a.N + 4 * q, nvalid);
-  }
-  const float delta = step_size(raw, a.softplus, true), u = delta * x;
+  const int d = live ? i : 0, g = d / Dg, nvalid = live ? max(0, min(SN, a.N - SN * q)) : 0;
+  float A2[SN], h[BT][SN], x[BT], raw[BT], gate[BT];
+  Pack<T, SN> Bv[BT], Cv[BT];
 #pragma unroll
-  for (int r = 0; r < SN; ++r) {
-    h[r] = fmaf(exp2_fast(delta * (A[r] * kLog2e)), h[r], u * Bv.at(r));
-    s = fmaf(Cv.at(r), h[r], s);
+  for (int k = 0; k < BT; ++k) {
+    const int b = min(b0 + k, a.B - 1);
+    load_states(h[k], a.h0 + ((int64_t)b * a.D + d) * a.N + SN * q, nvalid);
+    x[k] = (float)static_cast<const T *>(a.x.p)[b * a.x.batch_stride + d];
+    raw[k] = (float)static_cast<const T *>(a.dt.p)[b * a.dt.batch_stride + d];
+    gate[k] = a.gate.p ? (float)static_cast<const T *>(a.gate.p)[b * a.gate.batch_stride + d] : 0.f;
+    Bv[k] = Cv[k] = Pack<T, SN>{};
+    if (nvalid > 0) {
+      Bv[k] = load_some<T, SN>(static_cast<const T *>(a.Bm.p) + b * a.Bm.batch_stride + g * a.N + SN * q, nvalid);
+      Cv[k] = load_some<T, SN>(static_cast<const T *>(a.Cm.p) + b * a.Cm.batch_stride + g * a.N + SN * q, nvalid);
+    }
   }
-  store_states(a.h_last + at, h, nvalid);
-  s = lane_sum<LN>(s);
-  if (a.skip) s = fmaf(a.skip[d], x, s);
-  if (a.gate.p) s *= gate * sigmoid(gate);
-  if (live && q == 0) static_cast<T *>(a.y.p)[b * a.y.batch_stride + d] = (T)s;
+  load_states(A2, a.A + (int64_t)d * a.N + SN * q, nvalid);
+  const float bias = a.dt_bias ? a.dt_bias[d] : 0.f, skip = a.skip ? a.skip[d] : 0.f;
+#pragma unroll
+  for (int r = 0; r < SN; ++r) A2[r] *= kLog2e;
+#pragma unroll
+  for (int k = 0; k < BT; ++k) {
+    const int b = b0 + k;
+    if (b >= a.B) return;
+    const float delta = step_size(raw[k] + bias, a.softplus, true), u = delta * x[k];
+    float s = 0.f;
+#pragma unroll
+    for (int r = 0; r < SN; ++r) {
+      h[k][r] = fmaf(exp2_fast(delta * A2[r]), h[k][r], u * Bv[k].at(r));
+      s = fmaf(Cv[k].at(r), h[k][r], s);
+    }
+    store_states(a.h_last + ((int64_t)b * a.D + d) * a.N + SN * q, h[k], nvalid);
+    s = fmaf(skip, x[k], lane_sum<LN>(s));
+    if (a.gate.p) s *= gate[k] * sigmoid(gate[k]);
+    if (live && q == 0) static_cast<T *>(a.y.p)[b * a.y.batch_stride + d] = (T)s;
+  }
 }
 
 namespace {
@@ -740,8 +753,12 @@ hipError_t launch_scan_step(const fdc_scan_args &a, hipStream_t s) {
     using T = decltype(tag);
     return by_lanes(a.N, [&](auto lanes) {
       constexpr int LN = decltype(lanes)::value;
-      return timed_launch("scan_step", k_scan_step<T, LN>, dim3((unsigned)ceil_div(a.D, 256 / LN), (unsigned)a.B),
-                          dim3(256), 0, s, a, a.D / a.G);
+      const unsigned x = (unsigned)ceil_div(a.D, 256 / LN);
+      // four sequences a thread where that leaves every SIMD two waves
+      if ((long long)x * a.B >= 2 * kSimds)
+        return timed_launch("scan_step", k_scan_step<T, LN, 4>, dim3(x, (unsigned)ceil_div(a.B, 4)), dim3(256), 0, s, a,
+                            a.D / a.G);
+      return timed_launch("scan_step", k_scan_step<T, LN, 1>, dim3(x, (unsigned)a.B), dim3(256), 0, s, a, a.D / a.G);
     });
   });
 }

@@ -19,7 +19,7 @@ import torch
 
 from . import _lib
 from ._lib import ConvArgs, DistillArgs, NormArgs, NormGrads, ScanArgs, Tokens, call
-from .layers import _check, _ptr, _stream, _workspace
+from .layers import _ptr, _stream, _workspace
 
 _DTYPES = {torch.float32: _lib.DTYPE_F32, torch.bfloat16: _lib.DTYPE_BF16, torch.float16: _lib.DTYPE_F16}
 _ACTS = {"none": 0, "sigmoid": 1, "silu": 2}
@@ -29,76 +29,83 @@ ScanGradients = namedtuple("ScanGradients", "x dt A B C skip gate dt_bias")
 NormGradients = namedtuple("NormGradients", "x f gate scale w_post w_pre")
 
 
-def _dtype(t, name):
+# Calls on single tokens are bound by this file's own work, so a tensor that passes its check costs one
+# comparison chain, and what is wrong with another is found out afterwards.
+def _kind(t, name):
+    """The fdc_dtype of an activation on the current device."""
     d = _DTYPES.get(t.dtype)
     if d is None:
         raise ValueError(f"{name} must be float32, bfloat16 or float16 (got {t.dtype})")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a GPU tensor")
-    if t.device.index != torch.cuda.current_device():
+    if t.get_device() != torch.cuda.current_device():
         raise ValueError(f"{name} is on {t.device}, not on the current device")
     return d
 
 
-def _like(t, ref, shape, name):
-    """t is an activation of ref's type and device, of this shape, its last dimension dense."""
-    if t.dtype != ref.dtype or t.device != ref.device:
-        raise ValueError(f"{name} must be {ref.dtype} on {ref.device} (got {t.dtype} on {t.device})")
+def _wrong(t, dtype, device, shape, name):
+    if t.dtype != dtype or t.device != device:
+        raise ValueError(f"{name} must be {dtype} on {device} (got {t.dtype} on {t.device})")
     if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if t.stride(-1) != 1 and t.shape[-1] > 1:
+
+
+def _strides(t, ref, shape, name):
+    """The strides of an activation of ref's type and device, of this shape, its last dimension dense."""
+    if t is not ref and not (t.dtype == ref.dtype and t.get_device() == ref.get_device() and t.shape == shape):
+        _wrong(t, ref.dtype, ref.device, shape, name)
+    s = t.stride()
+    if s[-1] != 1 and shape[-1] > 1:
         raise ValueError(f"{name}'s last dimension must be dense")
+    return s
 
 
 def _tokens(t, ref, shape, name):
     if t is None:
         return _ABSENT
-    _like(t, ref, shape, name)
-    s = t.stride()
+    s = _strides(t, ref, shape, name)
     return Tokens(t.data_ptr(), s[0], s[1] if len(s) > 2 else 0)
 
 
 def _tokens_groups(t, ref, shape, name):
     """B or C of a scan, [..., G, N] with the groups of a token side by side."""
-    _like(t, ref, shape, name)
-    s = t.stride()
-    if shape[-2] > 1 and s[-2] != shape[-1]:
+    s = _strides(t, ref, shape, name)
+    if s[-2] != shape[-1] and shape[-2] > 1:
         raise ValueError(f"{name}'s groups must be dense")
     return Tokens(t.data_ptr(), s[0], s[1] if len(s) > 3 else 0)
-
-
-def _f32(t, ref, shape, name):
-    """The pointer of an optional float32 parameter, state or loss."""
-    if t is None:
-        return None
-    _check(t, torch.float32, shape, name)
-    if t.device != ref.device:
-        raise ValueError(f"{name} must be on {ref.device}")
-    return t.data_ptr()
-
-
-def _i32(t, ref, shape, name):
-    if t is None:
-        return None
-    _check(t, torch.int32, shape, name)
-    if t.device != ref.device:
-        raise ValueError(f"{name} must be on {ref.device}")
-    return t.data_ptr()
 
 
 def _rows(t, ref, shape, name):
     """Pointer and row stride of an optional [R, D] activation."""
     if t is None:
         return None, 0
-    _like(t, ref, shape, name)
-    return t.data_ptr(), t.stride(0)
+    return t.data_ptr(), _strides(t, ref, shape, name)[0]
+
+
+def _dense(t, dtype, ref, shape, name):
+    """The pointer of an optional dense parameter, state, loss or list of integers."""
+    if t is None:
+        return None
+    if t.dtype == dtype and t.get_device() == ref.get_device() and t.shape == shape and t.is_contiguous():
+        return t.data_ptr()
+    _wrong(t, dtype, ref.device, shape, name)
+    raise ValueError(f"{name} must be contiguous")
+
+
+def _f32(t, ref, shape, name):
+    return _dense(t, torch.float32, ref, shape, name)
+
+
+def _i32(t, ref, shape, name):
+    return _dense(t, torch.int32, ref, shape, name)
 
 
 def _empty(shape, ref, dtype=None):
     return torch.empty(shape, dtype=dtype or ref.dtype, device=ref.device)
 
 
-def _f32_like(t):
+def _like(t):
+    """An output of t's shape (and of its layout, where that is dense)."""
     return None if t is None else torch.empty_like(t)
 
 
@@ -108,25 +115,24 @@ def _f32_like(t):
 def _conv_args(x, w, bias, silu, state, lengths, y, new_state):
     if x.dim() not in (2, 3):
         raise ValueError(f"x must be [B, L, D] or [B, D] (got {tuple(x.shape)})")
-    dt = _dtype(x, "x")
-    B, D = x.shape[0], x.shape[-1]
+    dt = _kind(x, "x")
+    shape = x.shape
+    B, D = shape[0], shape[-1]
     if w.dim() != 2:
         raise ValueError(f"w must be [D, taps] (got {tuple(w.shape)})")
     n = w.shape[1]
-    if state is not None:
-        _check(state, x.dtype, (B, n - 1, D), "state")
-    if new_state is not None:
-        _check(new_state, x.dtype, (B, n - 1, D), "new_state")
-    return ConvArgs(dt, B, x.shape[1] if x.dim() == 3 else 1, D, n, int(silu), _tokens(x, x, x.shape, "x"),
-                    _ABSENT if y is None else _tokens(y, x, x.shape, "y"), _f32(w, x, (D, n), "w"),
-                    _f32(bias, x, (D,), "bias"), _ptr(state), _ptr(new_state), _i32(lengths, x, (B,), "lengths"))
+    kept = (B, n - 1, D)
+    return ConvArgs(dt, B, shape[1] if len(shape) == 3 else 1, D, n, silu, _tokens(x, x, shape, "x"),
+                    _tokens(y, x, shape, "y"), _f32(w, x, (D, n), "w"), _f32(bias, x, (D,), "bias"),
+                    _dense(state, x.dtype, x, kept, "state"), _dense(new_state, x.dtype, x, kept, "new_state"),
+                    _i32(lengths, x, (B,), "lengths"))
 
 
 def causal_conv_forward(x, w, bias=None, silu=False, state=None, lengths=None, last=False, y=None):
     """x [B, L, D], w [D, taps], bias [D] -> (y, new_state): y[t] = bias + sum_j w[j] x[t - taps + 1 + j],
     with SiLU if asked (fdc_causal_conv_forward).  state [B, taps - 1, D]: the tokens before x;
     new_state: the last ones, if `last` is asked for, else None."""
-    y = _empty(x.shape, x) if y is None else y
+    y = torch.empty_like(x) if y is None else y
     new_state = _empty((x.shape[0], w.shape[1] - 1, x.shape[-1]), x) if last else None
     a = _conv_args(x, w, bias, silu, state, lengths, y, new_state)
     call("fdc_causal_conv_forward", a, _stream())
@@ -138,7 +144,7 @@ def causal_conv_step(x, w, state, bias=None, silu=False, new_state=None, y=None)
     new_state is given."""
     if x.dim() != 2:
         raise ValueError(f"x must be [B, D] (got {tuple(x.shape)})")
-    y = _empty(x.shape, x) if y is None else y
+    y = torch.empty_like(x) if y is None else y
     new_state = state if new_state is None else new_state
     call("fdc_causal_conv_forward", _conv_args(x, w, bias, silu, state, None, y, new_state), _stream())
     return y, new_state
@@ -147,9 +153,9 @@ def causal_conv_step(x, w, state, bias=None, silu=False, new_state=None, y=None)
 def causal_conv_backward(gy, x, w, bias=None, silu=False, state=None, lengths=None, need_gx=True, need_gw=True):
     """-> (gx, gw, gbias) from gy (fdc_causal_conv_backward); gbias is None without a bias."""
     a = _conv_args(x, w, bias, silu, state, lengths, None, None)
-    gx = _empty(x.shape, x) if need_gx else None
+    gx = torch.empty_like(x) if need_gx else None
     gw = torch.empty_like(w) if need_gw else None
-    gbias = _f32_like(bias) if need_gw else None
+    gbias = _like(bias) if need_gw else None
     n = ctypes.c_size_t()
     call("fdc_causal_conv_workspace_size", a.dtype, a.B, a.L, a.D, a.n, ctypes.byref(n))
     ws = _workspace(n.value if need_gw else 0, x.device)
@@ -162,19 +168,19 @@ def causal_conv_backward(gy, x, w, bias=None, silu=False, state=None, lengths=No
 # selective scan
 # ----------------------------------------------------------------------------
 def _scan_args(x, dt, A, B, C, skip, gate, dt_bias, softplus, h0, h_last, lengths, y):
-    kind = _dtype(x, "x")
-    nb, D = x.shape[0], x.shape[-1]
+    kind = _kind(x, "x")
+    shape = x.shape
+    nb, D = shape[0], shape[-1]
     if A.dim() != 2 or B.dim() != x.dim() + 1:
         raise ValueError(f"A must be [D, N] and B {'[B, L, G, N]' if x.dim() == 3 else '[B, G, N]'} "
                          f"(got {tuple(A.shape)}, {tuple(B.shape)})")
     N, G = A.shape[1], B.shape[-2]
-    shared = x.shape[:-1] + (G, N)
-    return ScanArgs(kind, nb, x.shape[1] if x.dim() == 3 else 1, D, N, G, int(softplus),
-                    _tokens(x, x, x.shape, "x"), _tokens(dt, x, x.shape, "dt"), _tokens(gate, x, x.shape, "gate"),
-                    _tokens_groups(B, x, shared, "B"), _tokens_groups(C, x, shared, "C"),
-                    _tokens(y, x, x.shape, "y"), _f32(A, x, (D, N), "A"), _f32(skip, x, (D,), "skip"),
-                    _f32(dt_bias, x, (D,), "dt_bias"), _f32(h0, x, (nb, D, N), "h0"),
-                    _f32(h_last, x, (nb, D, N), "h_last"), _i32(lengths, x, (nb,), "lengths"))
+    shared, state = (nb, G, N) if len(shape) == 2 else (nb, shape[1], G, N), (nb, D, N)
+    return ScanArgs(kind, nb, shape[1] if len(shape) == 3 else 1, D, N, G, softplus, _tokens(x, x, shape, "x"),
+                    _tokens(dt, x, shape, "dt"), _tokens(gate, x, shape, "gate"), _tokens_groups(B, x, shared, "B"),
+                    _tokens_groups(C, x, shared, "C"), _tokens(y, x, shape, "y"), _f32(A, x, (D, N), "A"),
+                    _f32(skip, x, (D,), "skip"), _f32(dt_bias, x, (D,), "dt_bias"), _f32(h0, x, state, "h0"),
+                    _f32(h_last, x, state, "h_last"), _i32(lengths, x, (nb,), "lengths"))
 
 
 def scan_forward(x, dt, A, B, C, skip=None, gate=None, dt_bias=None, softplus=True, h0=None, lengths=None,
@@ -184,7 +190,7 @@ def scan_forward(x, dt, A, B, C, skip=None, gate=None, dt_bias=None, softplus=Tr
     is asked for, and what scan_backward needs if `save` is; else None."""
     if x.dim() != 3:
         raise ValueError(f"x must be [B, L, D] (got {tuple(x.shape)})")
-    y = _empty(x.shape, x) if y is None else y
+    y = torch.empty_like(x) if y is None else y
     h_last = _empty((x.shape[0], x.shape[2], A.shape[1]), x, torch.float32) if last else None
     a = _scan_args(x, dt, A, B, C, skip, gate, dt_bias, softplus, h0, h_last, lengths, y)
     n, saved = ctypes.c_size_t(), None
@@ -205,9 +211,8 @@ def scan_backward(gy, saved, x, dt, A, B, C, skip=None, gate=None, dt_bias=None,
     _f32(saved, x, (m.value // 4,), "saved")
     call("fdc_scan_workspace_size", a.B, a.L, a.D, a.N, a.G, None, ctypes.byref(n))
     ws = _workspace(n.value, x.device)
-    g = ScanGradients(_empty(x.shape, x), _empty(x.shape, x), torch.empty_like(A), _empty(B.shape, x),
-                      _empty(B.shape, x), _f32_like(skip), None if gate is None else _empty(x.shape, x),
-                      _f32_like(dt_bias))
+    g = ScanGradients(*(_like(t) for t in (x, x, A)), _empty(B.shape, x), _empty(B.shape, x),
+                      *(_like(t) for t in (skip, None if gate is None else x, dt_bias)))
     s = _lib.ScanGrads(_tokens(gy, x, x.shape, "gy"), _tokens(g.x, x, x.shape, "gx"), _tokens(g.dt, x, x.shape, "gdt"),
                        _tokens(g.gate, x, x.shape, "ggate"), _tokens_groups(g.B, x, B.shape, "gB"),
                        _tokens_groups(g.C, x, B.shape, "gC"), _ptr(g.A), _ptr(g.skip), _ptr(g.dt_bias))
@@ -220,7 +225,7 @@ def scan_step(x, dt, A, B, C, h, skip=None, gate=None, dt_bias=None, softplus=Tr
     (y, h_new); the state is updated in place unless h_new is given."""
     if x.dim() != 2:
         raise ValueError(f"x must be [B, D] (got {tuple(x.shape)})")
-    y = _empty(x.shape, x) if y is None else y
+    y = torch.empty_like(x) if y is None else y
     h_new = h if h_new is None else h_new
     call("fdc_scan_step", _scan_args(x, dt, A, B, C, skip, gate, dt_bias, softplus, h, h_new, None, y), _stream())
     return y, h_new
@@ -230,13 +235,14 @@ def scan_step(x, dt, A, B, C, h, skip=None, gate=None, dt_bias=None, softplus=Tr
 # block norm
 # ----------------------------------------------------------------------------
 def _norm_args(x, f, gate, scale, w_post, w_pre, act, eps):
-    dt = _dtype(x, "x")
+    dt = _kind(x, "x")
     if x.dim() != 2:
         raise ValueError(f"x must be [tokens, D] (got {tuple(x.shape)})")
     if act not in _ACTS:
         raise ValueError(f"act must be one of {sorted(_ACTS)} (got {act!r})")
-    R, D = x.shape
-    (xp, xs), (fp, fs), (gp, gs) = (_rows(t, x, x.shape, n) for t, n in ((x, "x"), (f, "f"), (gate, "gate")))
+    shape = x.shape
+    R, D = shape
+    (xp, xs), (fp, fs), (gp, gs) = _rows(x, x, shape, "x"), _rows(f, x, shape, "f"), _rows(gate, x, shape, "gate")
     return NormArgs(dt, D, _ACTS[act], R, eps, xp, fp, gp, xs, fs, gs, _f32(scale, x, (D,), "scale"),
                     _f32(w_post, x, (D,), "w_post"), _f32(w_pre, x, (D,), "w_pre"))
 
@@ -245,11 +251,11 @@ def block_norm_forward(x, f=None, gate=None, scale=None, w_post=None, w_pre=None
     """x, f, gate [tokens, D] -> (out, n, stats) (fdc_block_norm_forward): out = x + scale act(gate) rms(f; w_post)
     and n = rms(out; w_pre).  Without f, out is x itself; n is None without w_pre."""
     a = _norm_args(x, f, gate, scale, w_post, w_pre, act, eps)
-    out = x if f is None else _empty(x.shape, x)
-    n = None if w_pre is None else _empty(x.shape, x)
+    out = x if f is None else torch.empty_like(x)
+    n = None if w_pre is None else torch.empty_like(x)
     stats = _empty((a.R, 2), x, torch.float32)
-    call("fdc_block_norm_forward", a, None if f is None else out.data_ptr(), a.D, _ptr(n), a.D, _ptr(stats),
-         _stream())
+    call("fdc_block_norm_forward", a, None if f is None else out.data_ptr(), out.stride(0), _ptr(n),
+         0 if n is None else n.stride(0), stats.data_ptr(), _stream())
     return out, n, stats
 
 
@@ -260,14 +266,14 @@ def block_norm_backward(gout, gn, stats, x, f=None, gate=None, scale=None, w_pos
     a = _norm_args(x, f, gate, scale, w_post, w_pre, act, eps)
     _f32(stats, x, (a.R, 2), "stats")
     (gop, gos), (gnp, gns) = _rows(gout, x, x.shape, "gout"), _rows(gn, x, x.shape, "gn")
-    g = NormGradients(_empty(x.shape, x), None if f is None else _empty(x.shape, x),
-                      None if gate is None else _empty(x.shape, x), _f32_like(scale), _f32_like(w_post),
-                      _f32_like(w_pre))
+    rows = torch.empty_like(x)
+    g = NormGradients(rows, *(None if t is None else torch.empty_like(rows) for t in (f, gate)),
+                      *(_like(t) for t in (scale, w_post, w_pre)))
     n = ctypes.c_size_t()
     call("fdc_block_norm_workspace_size", a.R, a.D, ctypes.byref(n))
     ws = _workspace(n.value, x.device)
-    s = NormGrads(gop, gnp, _ptr(g.x), _ptr(g.f), _ptr(g.gate), gos, gns, a.D, a.D, a.D, _ptr(g.scale),
-                  _ptr(g.w_post), _ptr(g.w_pre))
+    s = NormGrads(gop, gnp, _ptr(g.x), _ptr(g.f), _ptr(g.gate), gos, gns, *(rows.stride(0),) * 3,
+                  _ptr(g.scale), _ptr(g.w_post), _ptr(g.w_pre))
     call("fdc_block_norm_backward", a, _ptr(stats), s, _ptr(ws), ws.numel(), _stream())
     return g
 
@@ -276,15 +282,13 @@ def block_norm_backward(gout, gn, stats, x, f=None, gate=None, scale=None, w_pos
 # distillation
 # ----------------------------------------------------------------------------
 def _distill_args(z, idx, teacher, temperature, labels, alpha, weight):
-    dt = _dtype(z, "z")
+    dt = _kind(z, "z")
     if z.dim() != 2 or idx.dim() != 2:
         raise ValueError(f"z must be [rows, vocabulary] and idx [rows, K] (got {tuple(z.shape)}, {tuple(idx.shape)})")
     R, K = z.shape[0], idx.shape[1]
-    _like(z, z, z.shape, "z")
-    _check(teacher, z.dtype, (R, K), "teacher")
-    return DistillArgs(dt, z.shape[1], K, R, temperature, alpha, z.data_ptr(), z.stride(0),
-                       _i32(idx, z, (R, K), "idx"), teacher.data_ptr(), _i32(labels, z, (R,), "labels"),
-                       _f32(weight, z, (R,), "weight"))
+    return DistillArgs(dt, z.shape[1], K, R, temperature, alpha, *_rows(z, z, z.shape, "z"),
+                       _i32(idx, z, (R, K), "idx"), _dense(teacher, z.dtype, z, (R, K), "teacher"),
+                       _i32(labels, z, (R,), "labels"), _f32(weight, z, (R,), "weight"))
 
 
 def _distill_ws(a, ref):
@@ -307,7 +311,7 @@ def distill_forward(z, idx, teacher, temperature=1.0, labels=None, alpha=1.0, we
 def distill_backward(gloss, stats, z, idx, teacher, temperature=1.0, labels=None, alpha=1.0, weight=None, gz=None):
     """Gradient of z from that of the loss [rows] and distill_forward's stats (gz may be z itself)."""
     a = _distill_args(z, idx, teacher, temperature, labels, alpha, weight)
-    gz = _empty(z.shape, z) if gz is None else gz
+    gz = torch.empty_like(z) if gz is None else gz
     gp, gs = _rows(gz, z, z.shape, "gz")
     call("fdc_distill_backward", a, _f32(stats, z, (a.R, 5), "stats"), _f32(gloss, z, (a.R,), "gloss"), gp, gs,
          _stream())
@@ -318,7 +322,7 @@ def distill_forward_backward(gloss, z, idx, teacher, temperature=1.0, labels=Non
     """Loss and gradient in one call, for a gradient of the loss that is known beforehand -> (loss, gz)."""
     a = _distill_args(z, idx, teacher, temperature, labels, alpha, weight)
     loss, stats = _empty((a.R,), z, torch.float32), _empty((a.R, 5), z, torch.float32)
-    gz = _empty(z.shape, z) if gz is None else gz
+    gz = torch.empty_like(z) if gz is None else gz
     gp, gs = _rows(gz, z, z.shape, "gz")
     ws = _distill_ws(a, z)
     call("fdc_distill_forward_backward", a, _f32(gloss, z, (a.R,), "gloss"), _ptr(loss), _ptr(stats), gp, gs, _ptr(ws),
