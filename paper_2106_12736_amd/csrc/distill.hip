@@ -58,13 +58,18 @@ struct TeacherStat {
 };
 
 // The K entries of a row's teacher and, as entry K, its label: the place (-1: absent), the teacher's
-// logit, and the student's logit there.
+// logit, the student's logit there, and (written later) the target that the gradient there is less by.
+// In dynamic LDS, so that the workgroups of a compute unit are not limited by the largest K.
 struct Entries {
-  int place[kDistillMaxTeacher + 1];
-  float t[kDistillMaxTeacher + 1], z[kDistillMaxTeacher + 1];
+  int *place;
+  float *t, *z, *target;
+  static __host__ __device__ __forceinline__ int padded(int K) { return (K + 4) & ~3; }  // K + 1 and reads of four
+  static size_t bytes(int K) { return 16 * (size_t)padded(K); }
+  __device__ __forceinline__ Entries(float *lds, int K)
+      : place(reinterpret_cast<int *>(lds)), t(lds + padded(K)), z(lds + 2 * padded(K)), target(lds + 3 * padded(K)) {}
 };
 template <class T>
-__device__ __forceinline__ void load_entries(Entries &en, const fdc_distill_args &a, int64_t row, int tid,
+__device__ __forceinline__ void load_entries(const Entries &en, const fdc_distill_args &a, int64_t row, int tid,
                                              int threads) {
   const T *z = static_cast<const T *>(a.z) + row * a.z_stride;
   for (int k = tid; k <= a.K; k += threads) {
@@ -169,22 +174,35 @@ __device__ __forceinline__ void by_terms(bool hard, bool soft, F &&f) {
   }
 }
 
+// The targets of a row's entries (a barrier before write_entries), and of the padding that it reads.
+__device__ __forceinline__ void put_targets(const Entries &en, const Factors &f, int K, float tm, int tid, int threads) {
+  for (int k = tid; k < Entries::padded(K); k += threads)
+    en.target[k] = k < K && en.place[k] >= 0 && f.gq != 0.f ? f.gq * exp2_fast((en.t[k] - tm) * f.ct) : 0.f;
+}
 // The gradient at the entries within [begin, end), by threads that stand for an entry each (the
 // first of those that name the same place writes it).  Each term's probability and its targets are
 // subtracted before the terms are added: both may be close to 1.
 template <class T>
-__device__ __forceinline__ void write_entries(const Entries &en, const Factors &f, int K, float tm, T *gz, int begin,
-                                              int end, int tid, int threads) {
+__device__ __forceinline__ void write_entries(const Entries &en, const Factors &f, int K, T *gz, int begin, int end,
+                                              int tid, int threads) {
   for (int k = tid; k <= K; k += threads) {
     const int v = en.place[k];
     if (v < begin || v >= end) continue;
     float hard = f.hard(en.z[k]), soft = f.soft(en.z[k]);
     bool first = true;
-    for (int j = 0; j < K; ++j)
-      if (en.place[j] == v) {
-        if (j < k) first = false;
-        if (f.gq != 0.f) soft -= f.gq * exp2_fast((en.t[j] - tm) * f.ct);
+#pragma unroll 4
+    for (int j = 0; j < K; j += 4) {
+      const int4 at = *reinterpret_cast<const int4 *>(&en.place[j]);
+      const float4 q = *reinterpret_cast<const float4 *>(&en.target[j]);
+      const int p[4] = {at.x, at.y, at.z, at.w};
+      const float t[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bool same = p[i] == v && j + i < K;
+        soft -= same ? t[i] : 0.f;
+        first = first && !(same && j + i < k);
       }
+    }
     if (en.place[K] == v) hard -= f.g1;
     if (first) gz[v] = (T)(hard + soft);
   }
@@ -198,20 +216,29 @@ __device__ __forceinline__ void keep_packed(Pack<T, V> &x) {
   asm volatile("" : "+v"(x.w[0]), "+v"(x.w[1]), "+v"(x.w[2]), "+v"(x.w[3]));
 }
 
+// A workgroup a row.  The row's phases (load, largest logit, sums, gradient) follow each other behind
+// barriers; three to six rows on a compute unit overlap them.  4096 x 32000 bfloat16, K = 64: 155 us (3.4 TB/s of
+// 5.1; its 15 plain operations and four exponentials an element would take 87 us alone).  Measured
+// and not kept: workgroups that take row after row with the next one loaded ahead (200 to 220 us: twice the
+// registers, half the rows in flight), 256 threads (185), 1024 threads (262).
 template <class T, int TH, int NV, bool Grad>
-__global__ __launch_bounds__(TH, NV == 16 ? 4 : NV == 8 ? 6 : 1) void k_distill_row(fdc_distill_args a, float *__restrict__ loss,
-                                                    float *__restrict__ stats, const float *__restrict__ gloss,
-                                                    void *gz_, int64_t gz_stride) {
+__global__ __launch_bounds__(TH, NV == 16 ? 4 : NV == 8 ? 6 : 1) void k_distill_row(fdc_distill_args a,
+                                                                                    float *__restrict__ loss,
+                                                                                    float *__restrict__ stats,
+                                                                                    const float *__restrict__ gloss,
+                                                                                    void *gz_, int64_t gz_stride) {
   constexpr int V = kLogitV<T>, W = TH / 64;
-  __shared__ Entries en;
+  extern __shared__ __align__(16) float lds[];
+  const Entries en(lds, a.K);
   __shared__ float rmax[W], rs1[W], rst[W];
   __shared__ TeacherStat te;
   const int64_t row = (int64_t)blockIdx.y * 32768 + blockIdx.x;
   if (row >= a.R) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const float c1 = kLog2e, ct = kLog2e / a.tau;
   const T *z = static_cast<const T *>(a.z) + row * a.z_stride;
   T *gz = Grad ? static_cast<T *>(gz_) + row * gz_stride : nullptr;
-  const float weight = a.weight ? a.weight[row] : 1.f;
+  const float up = Grad ? gloss[row] : 0.f, weight = a.weight ? a.weight[row] : 1.f;
   if (weight == 0.f) {
     row_nothing(row, tid, loss, stats);
     if constexpr (Grad) {
@@ -236,7 +263,6 @@ __global__ __launch_bounds__(TH, NV == 16 ? 4 : NV == 8 ? 6 : 1) void k_distill_
       for (int i = 0; i < 4; ++i) x[k].w[i] = sizeof(T) == 4 ? none : none | none << 16;
     }
   }
-  const float c1 = kLog2e, ct = kLog2e / a.tau;
   load_entries<T>(en, a, row, tid, TH);
   Stat st{-INFINITY, 0.f, 0.f};
 #pragma unroll
@@ -250,7 +276,7 @@ __global__ __launch_bounds__(TH, NV == 16 ? 4 : NV == 8 ? 6 : 1) void k_distill_
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < W; ++w) st.m = fmaxf(st.m, rmax[w]);
-  if (wave == 0) {
+  if (wave == W - 1) {
     const TeacherStat t = teacher_stat(en, a, lane);
     if (lane == 0) te = t;
   }
@@ -273,11 +299,11 @@ __global__ __launch_bounds__(TH, NV == 16 ? 4 : NV == 8 ? 6 : 1) void k_distill_
   st.s1 = st.st = 0.f;
 #pragma unroll
   for (int w = 0; w < W; ++w) st.s1 += rs1[w], st.st += rst[w];
-  if (wave == 0) row_loss(a, row, lane, en, st, te, loss, stats);
   if constexpr (Grad) {
 #pragma unroll
     for (int k = 0; k < NV; ++k) keep_packed(x[k]);
-    const Factors f(a, gloss[row] * weight, en.place[a.K], st, te);
+    const Factors f(a, up * weight, en.place[a.K], st, te);
+    put_targets(en, f, a.K, te.m, tid, TH);
     by_terms(f.f1 != 0.f, f.ft != 0.f, [&](auto hard, auto soft) {
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
@@ -290,8 +316,10 @@ __global__ __launch_bounds__(TH, NV == 16 ? 4 : NV == 8 ? 6 : 1) void k_distill_
       }
     });
     __syncthreads();
-    write_entries<T>(en, f, a.K, te.m, gz, 0, a.V, tid, TH);
+    write_entries<T>(en, f, a.K, gz, 0, a.V, tid, TH);
   }
+  // the first waves write the entries, the last one does what a wave does alone
+  if (wave == W - 1) row_loss(a, row, lane, en, st, te, loss, stats);
 }
 
 // ---- a row in segments ---------------------------------------------------------
@@ -341,7 +369,8 @@ __global__ __launch_bounds__(kSegThreads) void k_distill_part(fdc_distill_args a
 template <class T>
 __global__ __launch_bounds__(64) void k_distill_join(fdc_distill_args a, const float *__restrict__ part, int segs,
                                                      float *__restrict__ loss, float *__restrict__ stats) {
-  __shared__ Entries en;
+  extern __shared__ __align__(16) float lds[];
+  const Entries en(lds, a.K);
   const int lane = threadIdx.x;
   const int64_t row = (int64_t)blockIdx.y * 32768 + blockIdx.x;
   if (row >= a.R) return;
@@ -368,7 +397,8 @@ __global__ __launch_bounds__(kSegThreads) void k_distill_grad(fdc_distill_args a
                                                               const float *__restrict__ gloss, void *gz_,
                                                               int64_t gz_stride, int seg) {
   constexpr int V = kLogitV<T>;
-  __shared__ Entries en;
+  extern __shared__ __align__(16) float lds[];
+  const Entries en(lds, a.K);
   const int64_t row = (int64_t)blockIdx.y + (int64_t)blockIdx.z * 32768;
   if (row >= a.R) return;
   const T *z = static_cast<const T *>(a.z) + row * a.z_stride;
@@ -381,6 +411,7 @@ __global__ __launch_bounds__(kSegThreads) void k_distill_grad(fdc_distill_args a
   const int begin = blockIdx.x * seg, end = min(a.V, begin + seg);
   load_entries<T>(en, a, row, threadIdx.x, kSegThreads);
   __syncthreads();
+  put_targets(en, f, a.K, te.m, threadIdx.x, kSegThreads);
   by_terms(f.f1 != 0.f, f.ft != 0.f, [&](auto hard, auto soft) {
     for (int c = begin + threadIdx.x * V; c < end; c += kSegThreads * V) {
       const int n = min(V, end - c);
@@ -392,7 +423,7 @@ __global__ __launch_bounds__(kSegThreads) void k_distill_grad(fdc_distill_args a
     }
   });
   __syncthreads();
-  if (weight != 0.f) write_entries<T>(en, f, a.K, te.m, gz, begin, end, threadIdx.x, kSegThreads);
+  if (weight != 0.f) write_entries<T>(en, f, a.K, gz, begin, end, threadIdx.x, kSegThreads);
 }
 
 namespace {
@@ -427,8 +458,7 @@ hipError_t by_pieces(long long vecs, F &&f) {
   if (vecs <= TH * NV) return f(integral_constant<int, TH>{}, integral_constant<int, NV>{});
   FDC_ROW(64, 1)
   FDC_ROW(128, 2)
-  FDC_ROW(256, 2)
-  FDC_ROW(512, 2)
+  FDC_ROW(256, 4)
   FDC_ROW(512, 4)
   FDC_ROW(512, 8)
 #undef FDC_ROW
@@ -449,16 +479,16 @@ hipError_t launch_distill(const fdc_distill_args &a, float *loss, float *stats, 
       return by_pieces(ceil_div(a.V, kLogitV<T>), [&](auto threads, auto pieces) {
         constexpr int TH = decltype(threads)::value, NV = decltype(pieces)::value;
         if (gz != nullptr)
-          return timed_launch("distill_row_grad", k_distill_row<T, TH, NV, true>, row_grid(a.R), dim3(TH), 0, s, a, loss,
-                              stats, gloss, gz, gz_stride);
-        return timed_launch("distill_row", k_distill_row<T, TH, NV, false>, row_grid(a.R), dim3(TH), 0, s, a, loss, stats,
-                            gloss, gz, gz_stride);
+          return timed_launch("distill_row_grad", k_distill_row<T, TH, NV, true>, row_grid(a.R), dim3(TH),
+                              Entries::bytes(a.K), s, a, loss, stats, gloss, gz, gz_stride);
+        return timed_launch("distill_row", k_distill_row<T, TH, NV, false>, row_grid(a.R), dim3(TH), Entries::bytes(a.K),
+                            s, a, loss, stats, gloss, gz, gz_stride);
       });
     const Segments sg = segments(a.dtype, a.R, a.V);
     if (hipError_t e = timed_launch("distill_part", k_distill_part<T>, segment_grid(sg, a.R), dim3(kSegThreads), 0, s, a,
                                     ws, sg.seg, sg.segs))
       return e;
-    if (hipError_t e = timed_launch("distill_join", k_distill_join<T>, row_grid(a.R), dim3(64), 0, s, a,
+    if (hipError_t e = timed_launch("distill_join", k_distill_join<T>, row_grid(a.R), dim3(64), Entries::bytes(a.K), s, a,
                                     (const float *)ws, sg.segs, loss, stats))
       return e;
     return gz != nullptr ? launch_distill_bwd(a, stats, gloss, gz, gz_stride, s) : hipSuccess;
@@ -470,7 +500,7 @@ hipError_t launch_distill_bwd(const fdc_distill_args &a, const float *stats, con
   const Segments sg = segments(a.dtype, a.R, a.V);
   return by_dtype(a.dtype, [&](auto tag) {
     using T = decltype(tag);
-    return timed_launch("distill_grad", k_distill_grad<T>, segment_grid(sg, a.R), dim3(kSegThreads), 0, s, a, stats, gloss,
+    return timed_launch("distill_grad", k_distill_grad<T>, segment_grid(sg, a.R), dim3(kSegThreads), Entries::bytes(a.K), s, a, stats, gloss,
                         gz, gz_stride, sg.seg);
   });
 }

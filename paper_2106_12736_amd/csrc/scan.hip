@@ -48,13 +48,14 @@ struct ScanLane {
   static constexpr int CG = CW * Waves;       // channels a workgroup
   static constexpr int E = kTok / LN;         // tokens of a block a lane does the channel's work for
   int q, g, d, nvalid;                        // lane of the channel; group; channel; states here
-  bool live;
+  bool live, full;                            // the channel is there; all of the workgroup's are
   __device__ __forceinline__ ScanLane(const ScanGrid &sg, int N) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     q = lane % LN;
     g = blockIdx.x / sg.tiles;
     const int ch = (blockIdx.x - g * sg.tiles) * CG + wave * CW + lane / LN;
     live = ch < sg.Dg;
+    full = (int)(blockIdx.x - g * sg.tiles + 1) * CG <= sg.Dg;
     d = g * sg.Dg + ch;
     nvalid = live ? max(0, min(SN, N - SN * q)) : 0;
   }
@@ -234,16 +235,22 @@ __global__ __launch_bounds__(ScanLane<LN>::Threads) void k_scan_fwd(fdc_scan_arg
   for (int t0 = t_begin, it = 0; t0 < t_end; t0 += kTok, it ^= 1) {
     float delta[E], u[E], x[E], gate[E], out[E];
     bc.put(Bs[it], Cs[Local ? 0 : it], t0, len, a.N);
+    auto begin_tokens = [&](auto whole) {
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-      const bool in = ln.live && t0 + i * LN + ln.q < len;
-      x[i] = in ? (float)tx.v[i] : 0.f;
-      gate[i] = gated ? (float)tg.v[i] : 0.f;
-      delta[i] = step_size((float)tdt.v[i] + bias, a.softplus, in);
-      u[i] = delta[i] * x[i];
-      out[i] = 0.f;
-      dtotal += delta[i];
-    }
+      for (int i = 0; i < E; ++i) {
+        const bool in = whole.value || (ln.live && t0 + i * LN + ln.q < len);
+        x[i] = in ? (float)tx.v[i] : 0.f;
+        gate[i] = gated ? (float)tg.v[i] : 0.f;
+        delta[i] = step_size((float)tdt.v[i] + bias, a.softplus, in);
+        u[i] = delta[i] * x[i];
+        out[i] = 0.f;
+        dtotal += delta[i];
+      }
+    };
+    if (ln.full && t0 + kTok <= len)
+      begin_tokens(std::true_type{});
+    else
+      begin_tokens(std::false_type{});
     __syncthreads();
     if (t0 + kTok < t_end) fetch(t0 + kTok);
     if constexpr (!Local)
@@ -362,16 +369,22 @@ __global__ __launch_bounds__(ScanLane<LN>::Threads) void k_scan_bwd_local(fdc_sc
   for (int t0 = t_last, it = 0; t0 >= t_begin; t0 -= kTok, it ^= 1) {
     float delta[E], gs[E];
     cc.put(Cs[it], nullptr, t0, len, a.N);
+    auto begin_tokens = [&](auto whole) {
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-      const bool in = ln.live && t0 + i * LN + ln.q < len;
-      const float gate = gated ? (float)tg.v[i] : 0.f;
-      delta[i] = step_size((float)tdt.v[i] + bias, a.softplus, in);
-      gs[i] = (float)tgy.v[i];
-      if (gated) gs[i] *= gate * sigmoid(gate);
-      if (!in) gs[i] = 0.f;
-      dtotal += delta[i];
-    }
+      for (int i = 0; i < E; ++i) {
+        const bool in = whole.value || (ln.live && t0 + i * LN + ln.q < len);
+        const float gate = gated ? (float)tg.v[i] : 0.f;
+        delta[i] = step_size((float)tdt.v[i] + bias, a.softplus, in);
+        gs[i] = (float)tgy.v[i];
+        if (gated) gs[i] *= gate * sigmoid(gate);
+        if (!in) gs[i] = 0.f;
+        dtotal += delta[i];
+      }
+    };
+    if (ln.full && t0 + kTok <= len)
+      begin_tokens(std::true_type{});
+    else
+      begin_tokens(std::false_type{});
     __syncthreads();
     if (t0 > t_begin) fetch(t0 - kTok);
     if (t0 < len) {
@@ -458,18 +471,24 @@ __global__ __launch_bounds__(ScanLane<LN>::Threads, LN == 2 ? 1 : 2) void k_scan
     float h[kTok + 1][SN];
 #pragma unroll
     for (int r = 0; r < SN; ++r) h[0][r] = hs[r];
+    auto begin_tokens = [&](auto whole) {
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-      const bool in = ln.live && t0 + i * LN + ln.q < len;
-      x[i] = in ? (float)tx.v[i] : 0.f;
-      gate[i] = in && gated ? (float)tg.v[i] : 0.f;
-      gyv[i] = in ? (float)tgy.v[i] : 0.f;
-      raw[i] = in ? (float)tdt.v[i] + bias : 0.f;
-      delta[i] = step_size(raw[i], a.softplus, in);
-      u[i] = delta[i] * x[i];
-      gs[i] = gated ? gyv[i] * gate[i] * sigmoid(gate[i]) : gyv[i];
-      out[i] = gu[i] = gd[i] = 0.f;
-    }
+      for (int i = 0; i < E; ++i) {
+        const bool in = whole.value || (ln.live && t0 + i * LN + ln.q < len);
+        x[i] = in ? (float)tx.v[i] : 0.f;
+        gate[i] = in && gated ? (float)tg.v[i] : 0.f;
+        gyv[i] = in ? (float)tgy.v[i] : 0.f;
+        raw[i] = in ? (float)tdt.v[i] + bias : 0.f;
+        delta[i] = step_size(raw[i], a.softplus, in);
+        u[i] = delta[i] * x[i];
+        gs[i] = gated ? gyv[i] * gate[i] * sigmoid(gate[i]) : gyv[i];
+        out[i] = gu[i] = gd[i] = 0.f;
+      }
+    };
+    if (ln.full && t0 + kTok <= len)
+      begin_tokens(std::true_type{});
+    else
+      begin_tokens(std::false_type{});
     __syncthreads();
     if (t0 > t_begin) fetch(t0 - kTok);
     if (t0 < len) {
@@ -643,9 +662,10 @@ int lanes_of(int N) { return N <= 8 ? 2 : N <= 16 ? 4 : N <= 32 ? 8 : 16; }
 
 // One wave on a SIMD issues an instruction every 6.5 cycles, two together every 5, four every 4.5
 // (measured), and a chunk's first pass costs about 0.6 of a forward scan and 0.2 of a backward one: the
-// forward is cut into chunks where the channels give fewer than one wave a SIMD, the backward (two waves
-// a SIMD by its registers) where they give fewer than two.  (8 x 1024 tokens, 2048 channels of 16
-// states: forward 143 us whole, 148 us in chunks; backward 430 us whole, 342 us in chunks.)
+// forward is cut into chunks where the channels give no more than one wave a SIMD, the backward (two waves
+// a SIMD by its registers) where they give fewer than two.  (2048 channels of 16 states, forward:
+// 8 x 1024 tokens 163 us whole, 147 us in chunks; 16 x 1024 tokens 204 and 284.  Backward, 8 x 1024
+// tokens: 430 us whole, 359 us in chunks.)
 constexpr long long kSimds = 1024;
 ScanGrid scan_grid(int B, int L, int D, int N, int G, bool backward) {
   ScanGrid sg;
@@ -653,7 +673,7 @@ ScanGrid scan_grid(int B, int L, int D, int N, int G, bool backward) {
   sg.tiles = (int)ceil_div(sg.Dg, 64 / lanes_of(N) * kScanWaves);
   sg.blocks = (int)ceil_div(L, kTok);
   const long long waves = (long long)B * G * sg.tiles * kScanWaves;
-  const long long enough = backward ? 2 * kSimds : kSimds, want = backward ? 2 * kSimds : 4 * kSimds;
+  const long long enough = backward ? 2 * kSimds : kSimds + 1, want = backward ? 2 * kSimds : 4 * kSimds;
   const long long chunks = waves >= enough ? 1 : std::min<long long>(ceil_div(want, waves), ceil_div(sg.blocks, 4));
   sg.chunk = (int)ceil_div(sg.blocks, chunks) * kTok;
   sg.chunks = (int)ceil_div(L, sg.chunk);

@@ -147,13 +147,12 @@ __device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp
 __device__ __forceinline__ float rcp_fast(float x) { return __builtin_amdgcn_rcpf(x); }
 // 1 / (1 + exp(-x)): exp overflows to infinity for very negative x, and the quotient is 0.
 __device__ __forceinline__ float sigmoid(float x) { return rcp_fast(1.f + exp_fast(-x)); }
-// log(1 + exp(x)): x + log(1 + exp(-x)) for positive x.  With e = exp(-|x|) and w = 1 + e rounded,
-// log(w) e / (w - 1) makes up for the rounding of w (log1p's classic form), so that small
-// results keep their relative precision.
+// log(1 + exp(x)): x + log(1 + exp(-x)) for positive x.  With e = exp(-|x|) and w = 1 + e rounded, e - (w - 1)
+// is what the rounding of w lost, and log(1 + e) = log(w) + that / w; where it matters w is 1 (the
+// neglected part is at most 2^-24 e), so that small results keep their relative precision.
 __device__ __forceinline__ float softplus(float x) {
-  const float e = exp_fast(-fabsf(x)), w = 1.f + e, d = w - 1.f;
-  const float l = d == 0.f ? e : kLn2 * __builtin_amdgcn_logf(w) * (e * rcp_fast(d));
-  return fmaxf(x, 0.f) + l;
+  const float e = exp_fast(-fabsf(x)), w = 1.f + e;
+  return fmaxf(x, 0.f) + fmaf(kLn2, __builtin_amdgcn_logf(w), e - (w - 1.f));
 }
 // The length of sequence b, within [0, L].
 __device__ __forceinline__ int length_of(const int *lengths, int b, int L) {
