@@ -555,7 +555,8 @@ fdc_status fdc_distill_forward(const fdc_distill_args *a, float *loss, float *st
  * may be z itself. */
 fdc_status fdc_distill_backward(const fdc_distill_args *a, const float *stats, const float *gloss, void *gz,
                                 int64_t gz_stride, hipStream_t stream);
-/* Both in one call, for a gloss that is known beforehand (the mean over a batch): z is read once. */
+/* Both in one call, for a gloss that is known beforehand (the mean over a batch): rows that fit a
+ * workgroup's registers (many of them, up to 64 Ki 16-bit logits) are read once. */
 fdc_status fdc_distill_forward_backward(const fdc_distill_args *a, const float *gloss, float *loss, float *stats,
                                         void *gz, int64_t gz_stride, void *ws, size_t ws_bytes, hipStream_t stream);
 
