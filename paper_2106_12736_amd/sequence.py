@@ -14,12 +14,13 @@ allocates its outputs and workspace there.  include/fdc.h defines each operation
 
 import ctypes
 from collections import namedtuple
+from functools import lru_cache
 
 import torch
 
 from . import _lib
 from ._lib import ConvArgs, DistillArgs, NormArgs, NormGrads, ScanArgs, Tokens, call
-from .layers import _ptr, _stream, _workspace
+from .layers import _ptr, _stream
 
 _DTYPES = {torch.float32: _lib.DTYPE_F32, torch.bfloat16: _lib.DTYPE_BF16, torch.float16: _lib.DTYPE_F16}
 _ACTS = {"none": 0, "sigmoid": 1, "silu": 2}
@@ -101,7 +102,23 @@ def _i32(t, ref, shape, name):
 
 
 def _empty(shape, ref, dtype=None):
-    return torch.empty(shape, dtype=dtype or ref.dtype, device=ref.device)
+    return ref.new_empty(shape, dtype=dtype)
+
+
+@lru_cache(maxsize=4096)
+def _bytes(name, *sizes, which=0, of=1):
+    """What a workspace query (a function of sizes alone) says: its output `which` of `of`."""
+    n = [ctypes.c_size_t() for _ in range(of)]
+    call(name, *sizes, *(ctypes.byref(v) for v in n))
+    return n[which].value
+
+
+def _scratch(nbytes, ref):
+    """Pointer and size of a workspace, and the tensor that keeps it (until the call has been enqueued)."""
+    if nbytes == 0:
+        return None, 0, None
+    t = ref.new_empty(nbytes, dtype=torch.uint8)
+    return t.data_ptr(), nbytes, t
 
 
 def _like(t):
@@ -156,11 +173,10 @@ def causal_conv_backward(gy, x, w, bias=None, silu=False, state=None, lengths=No
     gx = torch.empty_like(x) if need_gx else None
     gw = torch.empty_like(w) if need_gw else None
     gbias = _like(bias) if need_gw else None
-    n = ctypes.c_size_t()
-    call("fdc_causal_conv_workspace_size", a.dtype, a.B, a.L, a.D, a.n, ctypes.byref(n))
-    ws = _workspace(n.value if need_gw else 0, x.device)
+    need = _bytes("fdc_causal_conv_workspace_size", a.dtype, a.B, a.L, a.D, a.n) if need_gw else 0
+    ws, size, keep = _scratch(need, x)
     call("fdc_causal_conv_backward", a, _tokens(gy, x, x.shape, "gy"), _tokens(gx, x, x.shape, "gx"), _ptr(gw),
-         _ptr(gbias), _ptr(ws), ws.numel(), _stream())
+         _ptr(gbias), ws, size, _stream())
     return gx, gw, gbias
 
 
@@ -193,30 +209,23 @@ def scan_forward(x, dt, A, B, C, skip=None, gate=None, dt_bias=None, softplus=Tr
     y = torch.empty_like(x) if y is None else y
     h_last = _empty((x.shape[0], x.shape[2], A.shape[1]), x, torch.float32) if last else None
     a = _scan_args(x, dt, A, B, C, skip, gate, dt_bias, softplus, h0, h_last, lengths, y)
-    n, saved = ctypes.c_size_t(), None
-    if save:
-        call("fdc_scan_saved_size", a.B, a.L, a.D, a.N, ctypes.byref(n))
-        saved = _empty((n.value // 4,), x, torch.float32)
-    call("fdc_scan_workspace_size", a.B, a.L, a.D, a.N, a.G, ctypes.byref(n), None)
-    ws = _workspace(n.value, x.device)
-    call("fdc_scan_forward", a, _ptr(saved), _ptr(ws), ws.numel(), _stream())
+    saved = _empty((_bytes("fdc_scan_saved_size", a.B, a.L, a.D, a.N) // 4,), x, torch.float32) if save else None
+    ws, size, keep = _scratch(_bytes("fdc_scan_workspace_size", a.B, a.L, a.D, a.N, a.G, which=0, of=2), x)
+    call("fdc_scan_forward", a, _ptr(saved), ws, size, _stream())
     return y, h_last, saved
 
 
 def scan_backward(gy, saved, x, dt, A, B, C, skip=None, gate=None, dt_bias=None, softplus=True, lengths=None):
     """Gradients of scan_forward's inputs (None for those that are not given) from gy and what it saved."""
     a = _scan_args(x, dt, A, B, C, skip, gate, dt_bias, softplus, None, None, lengths, None)
-    n, m = ctypes.c_size_t(), ctypes.c_size_t()
-    call("fdc_scan_saved_size", a.B, a.L, a.D, a.N, ctypes.byref(m))
-    _f32(saved, x, (m.value // 4,), "saved")
-    call("fdc_scan_workspace_size", a.B, a.L, a.D, a.N, a.G, None, ctypes.byref(n))
-    ws = _workspace(n.value, x.device)
+    _f32(saved, x, (_bytes("fdc_scan_saved_size", a.B, a.L, a.D, a.N) // 4,), "saved")
+    ws, size, keep = _scratch(_bytes("fdc_scan_workspace_size", a.B, a.L, a.D, a.N, a.G, which=1, of=2), x)
     g = ScanGradients(*(_like(t) for t in (x, x, A)), _empty(B.shape, x), _empty(B.shape, x),
                       *(_like(t) for t in (skip, None if gate is None else x, dt_bias)))
     s = _lib.ScanGrads(_tokens(gy, x, x.shape, "gy"), _tokens(g.x, x, x.shape, "gx"), _tokens(g.dt, x, x.shape, "gdt"),
                        _tokens(g.gate, x, x.shape, "ggate"), _tokens_groups(g.B, x, B.shape, "gB"),
                        _tokens_groups(g.C, x, B.shape, "gC"), _ptr(g.A), _ptr(g.skip), _ptr(g.dt_bias))
-    call("fdc_scan_backward", a, _ptr(saved), s, _ptr(ws), ws.numel(), _stream())
+    call("fdc_scan_backward", a, _ptr(saved), s, ws, size, _stream())
     return g
 
 
@@ -269,12 +278,10 @@ def block_norm_backward(gout, gn, stats, x, f=None, gate=None, scale=None, w_pos
     rows = torch.empty_like(x)
     g = NormGradients(rows, *(None if t is None else torch.empty_like(rows) for t in (f, gate)),
                       *(_like(t) for t in (scale, w_post, w_pre)))
-    n = ctypes.c_size_t()
-    call("fdc_block_norm_workspace_size", a.R, a.D, ctypes.byref(n))
-    ws = _workspace(n.value, x.device)
+    ws, size, keep = _scratch(_bytes("fdc_block_norm_workspace_size", a.R, a.D), x)
     s = NormGrads(gop, gnp, _ptr(g.x), _ptr(g.f), _ptr(g.gate), gos, gns, *(rows.stride(0),) * 3,
                   _ptr(g.scale), _ptr(g.w_post), _ptr(g.w_pre))
-    call("fdc_block_norm_backward", a, _ptr(stats), s, _ptr(ws), ws.numel(), _stream())
+    call("fdc_block_norm_backward", a, _ptr(stats), s, ws, size, _stream())
     return g
 
 
@@ -292,9 +299,7 @@ def _distill_args(z, idx, teacher, temperature, labels, alpha, weight):
 
 
 def _distill_ws(a, ref):
-    n = ctypes.c_size_t()
-    call("fdc_distill_workspace_size", a.dtype, a.R, a.V, ctypes.byref(n))
-    return _workspace(n.value, ref.device)
+    return _scratch(_bytes("fdc_distill_workspace_size", a.dtype, a.R, a.V), ref)
 
 
 def distill_forward(z, idx, teacher, temperature=1.0, labels=None, alpha=1.0, weight=None):
@@ -303,8 +308,8 @@ def distill_forward(z, idx, teacher, temperature=1.0, labels=None, alpha=1.0, we
     (fdc_distill_forward) -> (loss [rows], stats)."""
     a = _distill_args(z, idx, teacher, temperature, labels, alpha, weight)
     loss, stats = _empty((a.R,), z, torch.float32), _empty((a.R, 5), z, torch.float32)
-    ws = _distill_ws(a, z)
-    call("fdc_distill_forward", a, _ptr(loss), _ptr(stats), _ptr(ws), ws.numel(), _stream())
+    ws, size, keep = _distill_ws(a, z)
+    call("fdc_distill_forward", a, _ptr(loss), _ptr(stats), ws, size, _stream())
     return loss, stats
 
 
@@ -324,7 +329,7 @@ def distill_forward_backward(gloss, z, idx, teacher, temperature=1.0, labels=Non
     loss, stats = _empty((a.R,), z, torch.float32), _empty((a.R, 5), z, torch.float32)
     gz = torch.empty_like(z) if gz is None else gz
     gp, gs = _rows(gz, z, z.shape, "gz")
-    ws = _distill_ws(a, z)
-    call("fdc_distill_forward_backward", a, _f32(gloss, z, (a.R,), "gloss"), _ptr(loss), _ptr(stats), gp, gs, _ptr(ws),
-         ws.numel(), _stream())
+    ws, size, keep = _distill_ws(a, z)
+    call("fdc_distill_forward_backward", a, _f32(gloss, z, (a.R,), "gloss"), _ptr(loss), _ptr(stats), gp, gs, ws,
+         size, _stream())
     return loss, gz
