@@ -420,7 +420,8 @@ fdc_status fdc_adam_step(float *p, const float *g, float *m, float *v, int64_t n
  *            token_stride below 2^25).  p == NULL: the tensor is absent, where that is
  *            allowed.  Input strides may be 0 (one row for every token); the elements
  *            of an output must not overlap.  No alignment beyond the type's own is
- *            asked for.
+ *            asked for.  Outputs are other memory than inputs unless a call says
+ *            that they may be the same.
  * Lengths.   lengths [B] int32 (device memory; NULL: every sequence has L tokens):
  *            sequence b has the tokens t < lengths[b] (a value outside [0, L] is taken
  *            as 0 or L).  What inputs hold at the other tokens is never used, NaN

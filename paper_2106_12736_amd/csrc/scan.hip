@@ -666,6 +666,8 @@ int lanes_of(int N) { return N <= 8 ? 2 : N <= 16 ? 4 : N <= 32 ? 8 : 16; }
 // a SIMD by its registers) where they give fewer than two.  (2048 channels of 16 states, forward:
 // 8 x 1024 tokens 163 us whole, 147 us in chunks; 16 x 1024 tokens 204 and 284.  Backward, 8 x 1024
 // tokens: 430 us whole, 359 us in chunks.)
+// A chunk may be as short as a block; but a block alone takes a wave 3 us forward and 7 us backward and
+// the two launches that chunks add 9 us, so that sequences of fewer than 6 and 4 blocks are not cut.
 constexpr long long kSimds = 1024;
 ScanGrid scan_grid(int B, int L, int D, int N, int G, bool backward) {
   ScanGrid sg;
@@ -674,7 +676,8 @@ ScanGrid scan_grid(int B, int L, int D, int N, int G, bool backward) {
   sg.blocks = (int)ceil_div(L, kTok);
   const long long waves = (long long)B * G * sg.tiles * kScanWaves;
   const long long enough = backward ? 2 * kSimds : kSimds + 1, want = backward ? 2 * kSimds : 4 * kSimds;
-  const long long chunks = waves >= enough ? 1 : std::min<long long>(ceil_div(want, waves), ceil_div(sg.blocks, 4));
+  const int least = backward ? 4 : 6;
+  const long long chunks = waves >= enough || sg.blocks < least ? 1 : std::min<long long>(ceil_div(want, waves), sg.blocks);
   sg.chunk = (int)ceil_div(sg.blocks, chunks) * kTok;
   sg.chunks = (int)ceil_div(L, sg.chunk);
   return sg;
