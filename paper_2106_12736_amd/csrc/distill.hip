@@ -210,10 +210,11 @@ __device__ __forceinline__ void write_entries(const Entries &en, const Factors &
 
 // ---- a row a workgroup -------------------------------------------------------
 // Keeps the compiler from holding the floats of one pass over a row's pieces for the next: 16-bit
-// logits would take twice their registers, and fewer rows would be in flight on a compute unit.
+// logits would take twice their registers, and fewer rows would be in flight on a compute unit
+// (for float32 it only costs: 2048 x 32000 206 us with it, 166 us without).
 template <class T, int V>
 __device__ __forceinline__ void keep_packed(Pack<T, V> &x) {
-  asm volatile("" : "+v"(x.w[0]), "+v"(x.w[1]), "+v"(x.w[2]), "+v"(x.w[3]));
+  if constexpr (sizeof(T) == 2) asm volatile("" : "+v"(x.w[0]), "+v"(x.w[1]), "+v"(x.w[2]), "+v"(x.w[3]));
 }
 
 // A workgroup a row.  The row's phases (load, largest logit, sums, gradient) follow each other behind
@@ -222,7 +223,7 @@ __device__ __forceinline__ void keep_packed(Pack<T, V> &x) {
 // and not kept: workgroups that take row after row with the next one loaded ahead (200 to 220 us: twice the
 // registers, half the rows in flight), 256 threads (185), 1024 threads (262).
 template <class T, int TH, int NV, bool Grad>
-__global__ __launch_bounds__(TH, NV == 16 ? 4 : NV == 8 ? 6 : 1) void k_distill_row(fdc_distill_args a,
+__global__ __launch_bounds__(TH, NV == 16 ? (sizeof(T) == 4 ? 3 : 4) : NV == 8 ? 6 : 1) void k_distill_row(fdc_distill_args a,
                                                                                     float *__restrict__ loss,
                                                                                     float *__restrict__ stats,
                                                                                     const float *__restrict__ gloss,
@@ -289,7 +290,7 @@ __global__ __launch_bounds__(TH, NV == 16 ? 4 : NV == 8 ? 6 : 1) void k_distill_
         if constexpr (hard.value) st.s1 += exp2_fast(d * c1);
         if constexpr (soft.value) st.st += exp2_fast(d * ct);
       }
-      __builtin_amdgcn_sched_barrier(0);  // a piece at a time: its floats die with it
+      if constexpr (sizeof(T) == 2) __builtin_amdgcn_sched_barrier(0);  // a piece at a time: its floats die with it
     }
   });
   st.s1 = wave_sum(st.s1);
@@ -446,9 +447,13 @@ dim3 segment_grid(const Segments &sg, int64_t R) {
 }
 dim3 row_grid(int64_t R) { return dim3((unsigned)std::min<int64_t>(R, 32768), (unsigned)ceil_div(R, 32768)); }
 
-// Rows that fit a workgroup's registers (16 pieces of 16 bytes in 512 threads), and enough of them
-// for the chip's 256 compute units.
-bool whole_rows(int dtype, int64_t R, int V) { return R >= 256 && V <= 512 * 16 * (16 / (int)dtype_size(dtype)); }
+// Rows that fit a workgroup's registers (16 pieces of 16 bytes in 512 threads), and enough of them for
+// the chip's 256 compute units: one for each, or three where a row takes a third of a unit's
+// registers (300 rows of 20000 f16: 39 us a row a workgroup, 24 us in segments).
+bool whole_rows(int dtype, int64_t R, int V) {
+  const long long pieces = ceil_div(V, 16 / (int)dtype_size(dtype));
+  return pieces <= 512 * 16 && R >= (pieces <= 512 * 4 ? 256 : 3 * 256);
+}
 
 // f(threads, pieces a thread) for rows of `vecs` 16-byte pieces (at most 512 * 16).
 template <class F>

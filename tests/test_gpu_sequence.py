@@ -452,6 +452,13 @@ def test_distill_shapes(R, V):
     distill_case(R, V, 12, "bf16" if R < 1000 else "f32", seed=R)
 
 
+@pytest.mark.parametrize("R,V,dtype", [(260, 60, "f32"), (260, 2000, "f16"), (260, 7001, "bf16"), (260, 16384, "bf16"),
+                                       (770, 20001, "bf16"), (770, 20001, "f16"), (770, 12000, "f32"), (770, 20001, "f32")])
+def test_distill_rows_in_registers(R, V, dtype):
+    # a workgroup a row, in each of its widths
+    distill_case(R, V, 20, dtype, seed=R)
+
+
 def test_distill_masked_and_odd_values():
     lowest = {"f32": torch.finfo(torch.float32).min, "bf16": torch.finfo(torch.bfloat16).min, "f16": -65504.0}
 
