@@ -6,7 +6,8 @@
 // A thread owns V adjacent channels of a run of tokens and walks along it with the last n - 1
 // rows in registers, so each input crosses HBM once but for the n - 1 rows in front of a run.
 // Both directions are bound by HBM: no channel shares anything with another, and a token
-// takes n multiply-adds a channel.
+// takes n multiply-adds a channel.  8 x 2048 tokens, 4096 channels, 4 taps, bf16: forward 64 us (4.2 TB/s),
+// backward 97 to 110 us (3.7 to 4.1 TB/s); a large copy runs at 5.1.
 #include "sequence.h"
 
 namespace fdc {
@@ -217,7 +218,9 @@ __global__ __launch_bounds__(256) void k_causal_conv_bwd(fdc_causal_conv_args a,
 namespace {
 
 // Runs as long as leave at least `want` threads (so that the rows in front of a run are few), in powers of
-// two from 8 (no shorter than the n - 1 <= 7 tokens of a state) to `most`.
+// two from 8 (no shorter than the n - 1 <= 7 tokens of a state) to `most`.  (The case above: runs of 8 163
+// us forward and 198 backward, of 64 63 and 116, of 128 82 and 94, of 256 147 and 138; a sequence of
+// 4096 tokens of 2048 channels: runs of 16 15 and 19, of 64 23 and 37.)
 ConvGrid conv_grid(int B, int L, int D, int V, int most, long long want) {
   ConvGrid cg;
   cg.CV = (int)ceil_div(D, V);

@@ -11,7 +11,8 @@
 // The decay differs for every channel, state and token, so there is no matrix product in it: each
 // (token, channel, state) takes an exponential (four issue slots of a full-rate operation) and
 // four multiplications and additions forward, about thirteen backward.  The vector units bound both;
-// HBM would take a fifth of the time.
+// HBM would take a ninth of the time (8 x 1024 tokens, 2048 channels of 16 states, bf16: 142 us
+// forward, 355 us backward; one sequence of 16384 tokens: 259 us forward).
 //
 // LN adjacent lanes share a channel and hold SN = 4 states each, so a wave owns 64 / LN channels and
 // walks along the tokens in blocks of 16.  What a token needs once per channel (softplus, gate,
