@@ -4,9 +4,11 @@
 //   fh = f rf, rf = 1 / sqrt(mean(f^2) + eps);  post = fh w_post;  out = x + scale act(gate) post
 //   n = out ro w_pre, ro = 1 / sqrt(mean(out^2) + eps)
 // Backward, from gout and gn:
-//   v = gn w_pre;  go = gout + v ro - out ro^3 mean(v out) = gx;  gw_pre = sum gn out ro
+//   oh = out ro;  v = gn w_pre;  go = gout + (v - oh mean(v oh)) ro = gx;  gw_pre = sum gn oh
 //   gscale = sum go act post;  ggate = go scale post act'(gate);  gpost = go scale act
-//   u = gpost w_post;  gf = u rf - f rf^3 mean(u f);  gw_post = sum gpost fh
+//   u = gpost w_post;  gf = (u - fh mean(u fh)) rf;  gw_post = sum gpost fh
+// The means are of normed rows, of size 1: rf^3 and ro^3 would leave float32's range for rows of 1e13 and
+// for rows of zeros under a small eps.
 //
 // A row is in the registers of the threads that share it, so everything is read and written once;
 // both directions are bound by HBM.  Workgroups take row after row and keep the parameters in
@@ -156,10 +158,10 @@ __global__ __launch_bounds__(TPR * kRows<TPR>) void k_block_norm_fwd(fdc_block_n
   }
 }
 
-// What a norm's backward leaves of the gradient u of (v r w) by w: u r - v c, c = r^3 mean(u v).  Of a
-// single channel that is u r (1 - v^2 r^2) = u eps r^3, which the difference would lose.
-__device__ __forceinline__ float norm_grad(float u, float v, float r, float c, int D, float eps) {
-  return D == 1 ? u * (eps * r * r * r) : u * r - v * c;
+// What a norm's backward leaves of the gradient u of (v r w) by w: (u - vh c) r with vh = v r, c = mean(u vh).
+// Of a single channel that is u r (1 - vh^2) = u r (eps r^2), which the difference would lose.
+__device__ __forceinline__ float norm_grad(float u, float vh, float r, float c, int D, float eps) {
+  return D == 1 ? u * (eps * r * r * r) : fmaf(-vh, c, u) * r;
 }
 
 // Rows first, first + step, ...: the sums of the parameters' gradients stay in registers and go to
@@ -217,10 +219,10 @@ __global__ __launch_bounds__(TPR * kRows<TPR>) void k_block_norm_bwd(fdc_block_n
         const float gv = in.r[2][k].at(i);
         act[k][i] = has_gate ? gate_act(a.act, gv, sigmoid(gv)) : 1.f;
         go[k][i] = fmaf(sc[i] * act[k][i], in.r[1][k].at(i) * rf * wp[i], in.r[0][k].at(i));  // out
-        s = fmaf(in.r[4][k].at(i) * w[i], go[k][i], s);
+        s = fmaf(in.r[4][k].at(i) * w[i], go[k][i] * ro, s);
       }
     }
-    const float c1 = has_n ? ro * ro * ro * invD * row_sum<TPR>(s, red, turn) : 0.f;
+    const float c1 = has_n ? invD * row_sum<TPR>(s, red, turn) : 0.f;
     float u[NV][V];
     s = 0.f;
 #pragma unroll
@@ -230,10 +232,10 @@ __global__ __launch_bounds__(TPR * kRows<TPR>) void k_block_norm_bwd(fdc_block_n
       if (!Ahead) load_params(k);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const float out = go[k][i], gnv = in.r[4][k].at(i), f = in.r[1][k].at(i);
-        gpre_w[k][i] = fmaf(gnv, out * ro, gpre_w[k][i]);
-        const float t = in.r[3][k].at(i) + (has_n ? norm_grad(gnv * w[i], out, ro, c1, a.D, a.eps) : 0.f);
-        const float fh = f * rf, post = fh * wp[i], gpost = t * sc[i] * act[k][i];
+        const float oh = go[k][i] * ro, gnv = in.r[4][k].at(i);
+        gpre_w[k][i] = fmaf(gnv, oh, gpre_w[k][i]);
+        const float t = in.r[3][k].at(i) + (has_n ? norm_grad(gnv * w[i], oh, ro, c1, a.D, a.eps) : 0.f);
+        const float fh = in.r[1][k].at(i) * rf, post = fh * wp[i], gpost = t * sc[i] * act[k][i];
         go[k][i] = t;
         gscale[k][i] = fmaf(t, act[k][i] * post, gscale[k][i]);
         gpost_w[k][i] = fmaf(gpost, fh, gpost_w[k][i]);
@@ -242,7 +244,7 @@ __global__ __launch_bounds__(TPR * kRows<TPR>) void k_block_norm_bwd(fdc_block_n
           gg[i] = t * sc[i] * post * gate_slope(a.act, gv, sigmoid(gv));
         }
         u[k][i] = gpost * wp[i];
-        s = fmaf(u[k][i], f, s);
+        s = fmaf(u[k][i], fh, s);
       }
       if (nc > 0) {
         if (g.gx) store_some<T, V>(static_cast<T *>(g.gx) + row * g.gx_stride + c, go[k], nc);
@@ -250,13 +252,13 @@ __global__ __launch_bounds__(TPR * kRows<TPR>) void k_block_norm_bwd(fdc_block_n
       }
     }
     if (g.gf) {
-      const float c2 = normed ? rf * rf * rf * invD * row_sum<TPR>(s, red, turn) : 0.f;
+      const float c2 = normed ? invD * row_sum<TPR>(s, red, turn) : 0.f;
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
         const int c = (k * TPR + tid) * V, nc = a.D - c;
         if (normed)
 #pragma unroll
-          for (int i = 0; i < V; ++i) u[k][i] = norm_grad(u[k][i], in.r[1][k].at(i), rf, c2, a.D, a.eps);
+          for (int i = 0; i < V; ++i) u[k][i] = norm_grad(u[k][i], in.r[1][k].at(i) * rf, rf, c2, a.D, a.eps);
         if (nc > 0) store_some<T, V>(static_cast<T *>(g.gf) + row * g.gf_stride + c, u[k], nc);
       }
     }
