@@ -421,7 +421,9 @@ fdc_status fdc_adam_step(float *p, const float *g, float *m, float *v, int64_t n
  *            allowed.  Input strides may be 0 (one row for every token); the elements
  *            of an output must not overlap.  No alignment beyond the type's own is
  *            asked for.  Outputs are other memory than inputs unless a call says
- *            that they may be the same.
+ *            that they may be the same (same address and strides); an activation
+ *            output that shares memory with an activation input of the same strides
+ *            otherwise is refused.
  * Lengths.   lengths [B] int32 (device memory; NULL: every sequence has L tokens):
  *            sequence b has the tokens t < lengths[b] (a value outside [0, L] is taken
  *            as 0 or L).  What inputs hold at the other tokens is never used, NaN
@@ -442,7 +444,8 @@ typedef struct {
  * x[b][t] for t < 0 is state[b][t + n - 1] (state [B][n-1][D] dense, of the activations'
  * type; NULL: zeros).  w [D][n], bias [D] (NULL: none).  new_state [B][n-1][D] (NULL: not
  * wanted): the last n - 1 tokens of each sequence, those of `state` among them where it is
- * shorter; it may be `state` itself.  A single token is a call with L = 1. */
+ * shorter; it may be `state` itself.  A single token is a call with L = 1; y may be x itself
+ * there, and only there. */
 typedef struct {
   int dtype, B, L, D, n, silu;
   fdc_tokens x, y;
@@ -465,7 +468,7 @@ fdc_status fdc_causal_conv_backward(const fdc_causal_conv_args *a, fdc_tokens gy
  *   h[t][n] = exp(delta A[d][n]) h[t-1][n] + delta x[t] Bm[t][g][n]
  *   y[t] = (sum_n Cm[t][g][n] h[t][n] + skip[d] x[t]) silu(gate[t])
  * x, dt, gate, y: [B][L][D]; Bm, Cm: [B][L][G N]; A [D][N]; skip, dt_bias [D] (NULL: 0);
- * gate absent: no factor.  h0 [B][D][N] (NULL: zeros) is the state before the first token,
+ * gate absent: no factor.  y may be x, dt or gate itself (a backward needs them).  h0 [B][D][N] (NULL: zeros) is the state before the first token,
  * h_last [B][D][N] (NULL: not wanted; not h0) the one after the last.
  * saved (NULL: no backward follows): fdc_scan_saved_size bytes, 16-byte aligned, for the
  * backward: the states at every 16th token. */

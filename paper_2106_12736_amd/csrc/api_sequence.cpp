@@ -1,6 +1,8 @@
 // C ABI of the sequence operators: argument validation and workspaces.  Every entry point
 // validates on the host first and returns before enqueuing anything when an argument is wrong.
 #include <cmath>
+#include <cstdlib>
+#include <utility>
 
 #include "fdc.h"
 #include "sequence.h"
@@ -38,6 +40,52 @@ fdc_status check_tokens(const fdc_tokens &t, const char *name, int B, int L, int
       return fail(FDC_EINVAL, "%s is an output whose elements overlap (strides %lld, %lld)", name,
                   (long long)t.batch_stride, (long long)t.token_stride);
   }
+  return FDC_OK;
+}
+
+// Whether the rows of an output (whose elements are apart) and of an input of the same strides share memory:
+// some db * outer + dt * inner + dc, rows' distances and an element's within them, is the distance of the two.  With
+// other strides only the same address is seen.  `same`: it is the input itself that is written.
+struct Sharing {
+  bool any, same;
+};
+Sharing sharing(const fdc_tokens &out, int64_t out_width, const fdc_tokens &in, int64_t in_width, int64_t B, int64_t L,
+                size_t size) {
+  if (out.p == nullptr || in.p == nullptr) return {false, false};
+  if ((B > 1 && out.batch_stride != in.batch_stride) || (L > 1 && out.token_stride != in.token_stride))
+    return {out.p == in.p, false};
+  if (out.p == in.p) return {true, out_width == in_width};
+  struct Axis {
+    int64_t count, stride;
+  } outer{B, out.batch_stride * (int64_t)size}, inner{L, out.token_stride * (int64_t)size};
+  if (outer.count == 1 || (inner.count > 1 && inner.stride > outer.stride)) std::swap(outer, inner);
+  // the (at most two) steps along an axis that leave less than its stride of a distance, either way
+  auto any_step = [](const Axis &x, int64_t distance, auto &&rest_shares) {
+    if (x.count == 1) return rest_shares(distance);
+    const int64_t step = distance / x.stride, next = distance < 0 ? step - 1 : step + 1;
+    return (std::abs(step) < x.count && rest_shares(distance - step * x.stride)) ||
+           (std::abs(next) < x.count && rest_shares(distance - next * x.stride));
+  };
+  const int64_t distance = (int64_t)(reinterpret_cast<uintptr_t>(out.p) - reinterpret_cast<uintptr_t>(in.p));
+  const bool any = any_step(outer, distance, [&](int64_t d) {
+    return any_step(inner, d, [&](int64_t c) { return c < in_width * (int64_t)size && -c < out_width * (int64_t)size; });
+  });
+  return {any, false};
+}
+
+// `itself`: the output may be the whole of that input.
+fdc_status check_apart(const fdc_tokens &out, const char *out_name, int64_t out_width, const fdc_tokens &in,
+                       const char *in_name, int64_t in_width, int64_t B, int64_t L, int dtype, bool itself) {
+  const Sharing sh = sharing(out, out_width, in, in_width, B, L, fdc::dtype_size(dtype));
+  if (sh.any && !(itself && sh.same)) return fail(FDC_EINVAL, "%s shares memory with %s", out_name, in_name);
+  return FDC_OK;
+}
+
+// The same of dense arrays.
+fdc_status check_apart(const void *out, const void *in, size_t bytes, const char *what) {
+  const uintptr_t o = reinterpret_cast<uintptr_t>(out), i = reinterpret_cast<uintptr_t>(in);
+  if (out != nullptr && in != nullptr && o != i && o < i + bytes && i < o + bytes)
+    return fail(FDC_EINVAL, "%s share memory in part", what);
   return FDC_OK;
 }
 
@@ -92,9 +140,19 @@ fdc_status check_scan(const fdc_scan_args *a, bool needs_y) {
   FDC_TRY(check_tokens(a->gate, "gate", a->B, a->L, a->D, false, true));
   FDC_TRY(check_tokens(a->Bm, "Bm", a->B, a->L, (int64_t)a->G * a->N, false));
   FDC_TRY(check_tokens(a->Cm, "Cm", a->B, a->L, (int64_t)a->G * a->N, false));
-  if (needs_y) FDC_TRY(check_tokens(a->y, "y", a->B, a->L, a->D, true));
   if (!a->A) return fail(FDC_EINVAL, "A is NULL");
-  return FDC_OK;
+  return needs_y ? check_tokens(a->y, "y", a->B, a->L, a->D, true) : FDC_OK;
+}
+
+// y may be x, dt or gate itself: the lanes that write a block of a channel's tokens have read it before.
+fdc_status check_scan_apart(const fdc_scan_args *a) {
+  const int64_t GN = (int64_t)a->G * a->N;
+  FDC_TRY(check_apart(a->y, "y", a->D, a->x, "x", a->D, a->B, a->L, a->dtype, true));
+  FDC_TRY(check_apart(a->y, "y", a->D, a->dt, "dt", a->D, a->B, a->L, a->dtype, true));
+  FDC_TRY(check_apart(a->y, "y", a->D, a->gate, "gate", a->D, a->B, a->L, a->dtype, true));
+  FDC_TRY(check_apart(a->y, "y", a->D, a->Bm, "Bm", GN, a->B, a->L, a->dtype, false));
+  FDC_TRY(check_apart(a->y, "y", a->D, a->Cm, "Cm", GN, a->B, a->L, a->dtype, false));
+  return check_apart(a->h_last, a->h0, (size_t)a->B * a->D * a->N * sizeof(float), "h_last and h0");
 }
 
 // ---- block norm ----------------------------------------------------------------
@@ -160,6 +218,10 @@ fdc_status check_ws(const void *ws, size_t got, size_t need, const char *what) {
 fdc_status fdc_causal_conv_forward(const fdc_causal_conv_args *a, hipStream_t s) {
   FDC_TRY(check_conv(a));
   FDC_TRY(check_tokens(a->y, "y", a->B, a->L, a->D, true));
+  // a run of tokens begins with rows in front of it, which another run's thread may have written by then
+  FDC_TRY(check_apart(a->y, "y", a->D, a->x, "x", a->D, a->B, a->L, a->dtype, a->L == 1));
+  FDC_TRY(check_apart(a->new_state, a->state, (size_t)a->B * (a->n - 1) * a->D * fdc::dtype_size(a->dtype),
+                      "new_state and state"));
   return check_hip(fdc::launch_causal_conv_fwd(*a, s), "causal convolution");
 }
 
@@ -178,6 +240,8 @@ fdc_status fdc_causal_conv_backward(const fdc_causal_conv_args *a, fdc_tokens gy
   if (!gx.p && !gw && !gbias) return FDC_OK;
   const size_t need = gw || gbias ? fdc::causal_conv_bwd_ws(a->dtype, a->B, a->L, a->D, a->n) : 0;
   FDC_TRY(check_ws(ws, ws_bytes, need, "causal convolution"));
+  FDC_TRY(check_apart(gx, "gx", a->D, gy, "gy", a->D, a->B, a->L, a->dtype, a->L == 1));
+  FDC_TRY(check_apart(gx, "gx", a->D, a->x, "x", a->D, a->B, a->L, a->dtype, a->L == 1));
   return check_hip(fdc::launch_causal_conv_bwd(*a, gy, gx, gw, gbias, static_cast<float *>(ws), s),
                    "causal convolution backward");
 }
@@ -204,6 +268,7 @@ fdc_status fdc_scan_forward(const fdc_scan_args *a, float *saved, void *ws, size
   if (a->h_last && a->h_last == a->h0) return fail(FDC_EINVAL, "h_last must not be h0");
   if (reinterpret_cast<uintptr_t>(saved) & 15) return fail(FDC_EINVAL, "saved must be 16-byte aligned");
   FDC_TRY(check_ws(ws, ws_bytes, fdc::scan_fwd_ws_floats(a->B, a->L, a->D, a->N, a->G) * sizeof(float), "scan forward"));
+  FDC_TRY(check_scan_apart(a));
   return check_hip(fdc::launch_scan_fwd(*a, saved, static_cast<float *>(ws), s), "scan");
 }
 
@@ -232,6 +297,7 @@ fdc_status fdc_scan_step(const fdc_scan_args *a, hipStream_t s) {
   FDC_TRY(check_scan(a, true));
   if (a->L != 1 || a->lengths) return fail(FDC_EINVAL, "a step takes one token of every sequence (L = 1, no lengths)");
   if (!a->h0 || !a->h_last) return fail(FDC_EINVAL, "a step needs h0 and h_last");
+  FDC_TRY(check_scan_apart(a));
   return check_hip(fdc::launch_scan_step(*a, s), "scan step");
 }
 
@@ -298,7 +364,8 @@ fdc_status fdc_distill_backward(const fdc_distill_args *a, const float *stats, c
   FDC_TRY(check_distill(a));
   if (!stats || !gloss || !gz) return fail(FDC_EINVAL, "stats, gloss or gz is NULL");
   FDC_TRY(check_row_stride(gz_stride, a->R, a->V, "gz", true));
-  if (gz == a->z && gz_stride != a->z_stride) return fail(FDC_EINVAL, "gz in place of z needs z's row stride");
+  FDC_TRY(check_apart({gz, gz_stride, 0}, "gz", a->V, {const_cast<void *>(a->z), a->z_stride, 0}, "z", a->V, a->R, 1,
+                      a->dtype, true));
   return check_hip(fdc::launch_distill_bwd(*a, stats, gloss, gz, gz_stride, s), "distillation backward");
 }
 
@@ -307,7 +374,8 @@ fdc_status fdc_distill_forward_backward(const fdc_distill_args *a, const float *
   FDC_TRY(check_distill(a));
   if (!loss || !stats || !gloss || !gz) return fail(FDC_EINVAL, "loss, stats, gloss or gz is NULL");
   FDC_TRY(check_row_stride(gz_stride, a->R, a->V, "gz", true));
-  if (gz == a->z && gz_stride != a->z_stride) return fail(FDC_EINVAL, "gz in place of z needs z's row stride");
+  FDC_TRY(check_apart({gz, gz_stride, 0}, "gz", a->V, {const_cast<void *>(a->z), a->z_stride, 0}, "z", a->V, a->R, 1,
+                      a->dtype, true));
   FDC_TRY(check_ws(ws, ws_bytes, fdc::distill_ws_floats(a->dtype, a->R, a->V) * sizeof(float), "distillation"));
   return check_hip(fdc::launch_distill(*a, loss, stats, gloss, gz, gz_stride, static_cast<float *>(ws), s),
                    "distillation");

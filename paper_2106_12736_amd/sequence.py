@@ -9,7 +9,8 @@ the loss it is trained with, on tokens of D channels.
 Activations are float32, bfloat16 or float16, of shape [B, L, D] (or [B, D] for one token) with any
 strides whose last dimension is dense; parameters, states and losses are float32 and contiguous.
 Every call runs on the current stream of the current device, which the tensors have to be on, and
-allocates its outputs and workspace there.  include/fdc.h defines each operation.
+allocates its outputs and workspace there; an output that is given is other memory than the inputs
+unless a function says that it may be the same.  include/fdc.h defines each operation.
 """
 
 import ctypes
@@ -158,7 +159,7 @@ def causal_conv_forward(x, w, bias=None, silu=False, state=None, lengths=None, l
 
 def causal_conv_step(x, w, state, bias=None, silu=False, new_state=None, y=None):
     """One token x [B, D] of every sequence -> (y, new_state); the state is updated in place unless
-    new_state is given."""
+    new_state is given, and y may be x itself."""
     if x.dim() != 2:
         raise ValueError(f"x must be [B, D] (got {tuple(x.shape)})")
     y = torch.empty_like(x) if y is None else y
@@ -203,7 +204,7 @@ def scan_forward(x, dt, A, B, C, skip=None, gate=None, dt_bias=None, softplus=Tr
                  last=False, save=False, y=None):
     """Selective scan (fdc_scan_forward) of x, dt, gate [B, L, D] with A [D, N], B, C [B, L, G, N], skip and
     dt_bias [D] from the state h0 [B, D, N] -> (y, h_last, saved): the state after the last token if `last`
-    is asked for, and what scan_backward needs if `save` is; else None."""
+    is asked for, and what scan_backward needs if `save` is; else None.  y may be x, dt or gate itself."""
     if x.dim() != 3:
         raise ValueError(f"x must be [B, L, D] (got {tuple(x.shape)})")
     y = torch.empty_like(x) if y is None else y
@@ -231,7 +232,7 @@ def scan_backward(gy, saved, x, dt, A, B, C, skip=None, gate=None, dt_bias=None,
 
 def scan_step(x, dt, A, B, C, h, skip=None, gate=None, dt_bias=None, softplus=True, h_new=None, y=None):
     """One token of every sequence (fdc_scan_step): x, dt, gate [B, D], B, C [B, G, N], state h [B, D, N] ->
-    (y, h_new); the state is updated in place unless h_new is given."""
+    (y, h_new); the state is updated in place unless h_new is given, and y may be x, dt or gate itself."""
     if x.dim() != 2:
         raise ValueError(f"x must be [B, D] (got {tuple(x.shape)})")
     y = torch.empty_like(x) if y is None else y

@@ -12,7 +12,8 @@ sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
 
 from oracle import sequence as oracle
 from paper_2106_12736_amd import sequence as seq
-from test_gpu_sequence import Make, check, host
+from paper_2106_12736_amd._lib import FdcError
+from test_gpu_sequence import Make, check, host, scan_inputs
 
 pytestmark = pytest.mark.gpu
 
@@ -59,3 +60,43 @@ def test_norm_rows_of_zeros_under_a_small_eps(D):
     for r in range(3 if D > 1 else 1):
         check(g.x[r], want["x"][r], f"gx {r}")
         check(g.f[r], want["f"][r], f"gf {r}")
+
+
+# ----------------------------------------------------------------------------
+# outputs in an input's memory
+# ----------------------------------------------------------------------------
+def test_conv_output_over_its_input():
+    m = Make(1, "bf16")
+    wide, w = m.act(2, 300, 64), m.f32(32, 4)
+    x = wide[..., :32]
+    want = seq.causal_conv_forward(x, w, silu=True)[0]
+    for y in (x, wide[..., 16:48]):
+        with pytest.raises(FdcError, match="y shares memory with x"):
+            seq.causal_conv_forward(x, w, silu=True, y=y)
+    with pytest.raises(FdcError, match="y shares memory with x"):
+        seq.causal_conv_forward(wide[:, :-1, :32], w, y=wide[:, 1:, :32])
+    assert torch.equal(seq.causal_conv_forward(x, w, silu=True, y=wide[..., 32:])[0], want)  # side by side
+    # a single token may be written over
+    x, state = m.act(3, 32), m.act(3, 3, 32)
+    want, after = seq.causal_conv_step(x, w, state, new_state=torch.empty_like(state))
+    y, same = seq.causal_conv_step(x, w, state, y=x)
+    assert y is x and torch.equal(y, want) and torch.equal(same, after)
+
+
+@pytest.mark.parametrize("L", [5, 37, 1000])
+@pytest.mark.parametrize("over", ["x", "dt", "gate"])
+def test_scan_output_over_an_input(L, over):
+    # one pass and, for the many tokens, in chunks
+    print(f"scan over {over} L={L}", flush=True)
+    m = Make(L, "bf16")
+    v = scan_inputs(m, 2, L, 40, 16, 2, True, True, True, True, None, "dense")
+    want, h, _ = seq.scan_forward(**v, last=True)
+    with pytest.raises(FdcError, match="y shares memory with"):
+        seq.scan_forward(**{**v, over: v[over][:, :-1], **{k: t[:, :-1] for k, t in v.items() if t.dim() > 2 and k != over}},
+                         y=v[over][:, 1:])
+    step = {k: t[:, 0].clone() if t.dim() > 2 else t for k, t in v.items()}
+    first, after = seq.scan_step(**step, h=torch.zeros_like(h))
+    same, again = seq.scan_step(**step, h=torch.zeros_like(h), y=step[over])
+    assert torch.equal(first, same) and torch.equal(after, again)
+    y, h2, _ = seq.scan_forward(**v, last=True, y=v[over])
+    assert y is v[over] and torch.equal(y, want) and torch.equal(h, h2)
