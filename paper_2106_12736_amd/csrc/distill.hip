@@ -91,9 +91,9 @@ __device__ __forceinline__ TeacherStat teacher_stat(const Entries &en, const fdc
   }
   te.m = wave_max(te.m);
   te.bad = __any(over);
-  if (te.m != -INFINITY)
-    for (int k = lane; k < a.K; k += 64)
-      if (en.place[k] >= 0) te.s += exp2_fast((en.t[k] - te.m) * ct);
+  // the maximum passes over a NaN, the sum does not
+  for (int k = lane; k < a.K; k += 64)
+    if (en.place[k] >= 0 && en.t[k] != -INFINITY) te.s += exp2_fast((en.t[k] - te.m) * ct);
   te.s = wave_sum(te.s);
   return te;
 }

@@ -100,3 +100,41 @@ def test_scan_output_over_an_input(L, over):
     assert torch.equal(first, same) and torch.equal(after, again)
     y, h2, _ = seq.scan_forward(**v, last=True, y=v[over])
     assert y is v[over] and torch.equal(y, want) and torch.equal(h, h2)
+
+
+# ----------------------------------------------------------------------------
+# distillation
+# ----------------------------------------------------------------------------
+@pytest.mark.parametrize("R,V", [(8, 301), (260, 301), (770, 20001)])  # in segments, rows in registers
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_distill_teacher_of_nan(R, V, dtype):
+    # a NaN among a row's entries is one in its loss and in the gradients of the named places
+    print(f"distill NaN R={R} V={V} {dtype}", flush=True)
+    m = Make(V, dtype)
+    z, teacher, gloss = m.act(R, V, scale=3.0), m.act(R, 6), m.f32(R)
+    idx = torch.stack([torch.randperm(V, generator=m.g)[:6] for _ in range(R)]).int().cuda()
+    labels = torch.randint(0, V, (R,), generator=m.g).int().cuda()
+    kw = {"temperature": 1.5, "labels": labels, "alpha": 0.6}
+    rloss, rgz = oracle.distill(host(z), idx.cpu().numpy(), host(teacher), 1.5, labels.cpu().numpy(), 0.6,
+                                gloss=host(gloss))
+    nan, inf = float("nan"), float("inf")
+    teacher[1] = nan
+    teacher[2, :3], teacher[2, 3:] = nan, -inf
+    teacher[3, 4] = nan
+    for r in (1, 2, 3):
+        rloss[r] = nan
+        rgz[r, idx[r].tolist()] = nan
+    # of an absent entry it is none
+    idx[4, 2], teacher[4, 2] = -1, nan
+    at = [0, 1, 3, 4, 5]
+    one = oracle.distill(host(z[4:5]), idx[4:5, at].cpu().numpy(), host(teacher[4:5, at]), 1.5, labels[4:5].cpu().numpy(),
+                         0.6, gloss=host(gloss[4:5]))
+    rloss[4], rgz[4] = one[0][0], one[1][0]
+    loss, stats = seq.distill_forward(z, idx, teacher, **kw)
+    gz = seq.distill_backward(gloss, stats, z, idx, teacher, **kw)
+    both, gz2 = seq.distill_forward_backward(gloss, z, idx, teacher, **kw)
+    check(loss, rloss, "loss")
+    check(both, rloss, "loss in one call")
+    for r in range(12 if R > 12 else R):
+        check(gz[r], rgz[r], f"gz {r}")
+        check(gz2[r], rgz[r], f"gz in one call {r}")
