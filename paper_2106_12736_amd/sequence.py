@@ -123,8 +123,12 @@ def _scratch(nbytes, ref):
 
 
 def _like(t):
-    """An output of t's shape (and of its layout, where that is dense)."""
-    return None if t is None else torch.empty_like(t)
+    """An output of t's shape, in its layout where that is dense; its last dimension is."""
+    if t is None:
+        return None
+    out = torch.empty_like(t)
+    # rows that overlap (windows one element apart) leave torch no order of the dimensions
+    return out if out.stride(-1) == 1 or t.shape[-1] == 1 else t.new_empty(t.shape)
 
 
 # ----------------------------------------------------------------------------
@@ -150,7 +154,7 @@ def causal_conv_forward(x, w, bias=None, silu=False, state=None, lengths=None, l
     """x [B, L, D], w [D, taps], bias [D] -> (y, new_state): y[t] = bias + sum_j w[j] x[t - taps + 1 + j],
     with SiLU if asked (fdc_causal_conv_forward).  state [B, taps - 1, D]: the tokens before x;
     new_state: the last ones, if `last` is asked for, else None."""
-    y = torch.empty_like(x) if y is None else y
+    y = _like(x) if y is None else y
     new_state = _empty((x.shape[0], w.shape[1] - 1, x.shape[-1]), x) if last else None
     a = _conv_args(x, w, bias, silu, state, lengths, y, new_state)
     call("fdc_causal_conv_forward", a, _stream())
@@ -162,7 +166,7 @@ def causal_conv_step(x, w, state, bias=None, silu=False, new_state=None, y=None)
     new_state is given, and y may be x itself."""
     if x.dim() != 2:
         raise ValueError(f"x must be [B, D] (got {tuple(x.shape)})")
-    y = torch.empty_like(x) if y is None else y
+    y = _like(x) if y is None else y
     new_state = state if new_state is None else new_state
     call("fdc_causal_conv_forward", _conv_args(x, w, bias, silu, state, None, y, new_state), _stream())
     return y, new_state
@@ -171,8 +175,8 @@ def causal_conv_step(x, w, state, bias=None, silu=False, new_state=None, y=None)
 def causal_conv_backward(gy, x, w, bias=None, silu=False, state=None, lengths=None, need_gx=True, need_gw=True):
     """-> (gx, gw, gbias) from gy (fdc_causal_conv_backward); gbias is None without a bias."""
     a = _conv_args(x, w, bias, silu, state, lengths, None, None)
-    gx = torch.empty_like(x) if need_gx else None
-    gw = torch.empty_like(w) if need_gw else None
+    gx = _like(x) if need_gx else None
+    gw = _like(w) if need_gw else None
     gbias = _like(bias) if need_gw else None
     need = _bytes("fdc_causal_conv_workspace_size", a.dtype, a.B, a.L, a.D, a.n) if need_gw else 0
     ws, size, keep = _scratch(need, x)
@@ -207,7 +211,7 @@ def scan_forward(x, dt, A, B, C, skip=None, gate=None, dt_bias=None, softplus=Tr
     is asked for, and what scan_backward needs if `save` is; else None.  y may be x, dt or gate itself."""
     if x.dim() != 3:
         raise ValueError(f"x must be [B, L, D] (got {tuple(x.shape)})")
-    y = torch.empty_like(x) if y is None else y
+    y = _like(x) if y is None else y
     h_last = _empty((x.shape[0], x.shape[2], A.shape[1]), x, torch.float32) if last else None
     a = _scan_args(x, dt, A, B, C, skip, gate, dt_bias, softplus, h0, h_last, lengths, y)
     saved = _empty((_bytes("fdc_scan_saved_size", a.B, a.L, a.D, a.N) // 4,), x, torch.float32) if save else None
@@ -235,7 +239,7 @@ def scan_step(x, dt, A, B, C, h, skip=None, gate=None, dt_bias=None, softplus=Tr
     (y, h_new); the state is updated in place unless h_new is given, and y may be x, dt or gate itself."""
     if x.dim() != 2:
         raise ValueError(f"x must be [B, D] (got {tuple(x.shape)})")
-    y = torch.empty_like(x) if y is None else y
+    y = _like(x) if y is None else y
     h_new = h if h_new is None else h_new
     call("fdc_scan_step", _scan_args(x, dt, A, B, C, skip, gate, dt_bias, softplus, h, h_new, None, y), _stream())
     return y, h_new
@@ -261,8 +265,8 @@ def block_norm_forward(x, f=None, gate=None, scale=None, w_post=None, w_pre=None
     """x, f, gate [tokens, D] -> (out, n, stats) (fdc_block_norm_forward): out = x + scale act(gate) rms(f; w_post)
     and n = rms(out; w_pre).  Without f, out is x itself; n is None without w_pre."""
     a = _norm_args(x, f, gate, scale, w_post, w_pre, act, eps)
-    out = x if f is None else torch.empty_like(x)
-    n = None if w_pre is None else torch.empty_like(x)
+    out = x if f is None else _like(x)
+    n = None if w_pre is None else _like(x)
     stats = _empty((a.R, 2), x, torch.float32)
     call("fdc_block_norm_forward", a, None if f is None else out.data_ptr(), out.stride(0), _ptr(n),
          0 if n is None else n.stride(0), stats.data_ptr(), _stream())
@@ -276,8 +280,8 @@ def block_norm_backward(gout, gn, stats, x, f=None, gate=None, scale=None, w_pos
     a = _norm_args(x, f, gate, scale, w_post, w_pre, act, eps)
     _f32(stats, x, (a.R, 2), "stats")
     (gop, gos), (gnp, gns) = _rows(gout, x, x.shape, "gout"), _rows(gn, x, x.shape, "gn")
-    rows = torch.empty_like(x)
-    g = NormGradients(rows, *(None if t is None else torch.empty_like(rows) for t in (f, gate)),
+    rows = _like(x)
+    g = NormGradients(rows, *(None if t is None else _like(rows) for t in (f, gate)),
                       *(_like(t) for t in (scale, w_post, w_pre)))
     ws, size, keep = _scratch(_bytes("fdc_block_norm_workspace_size", a.R, a.D), x)
     s = NormGrads(gop, gnp, _ptr(g.x), _ptr(g.f), _ptr(g.gate), gos, gns, *(rows.stride(0),) * 3,
@@ -317,7 +321,7 @@ def distill_forward(z, idx, teacher, temperature=1.0, labels=None, alpha=1.0, we
 def distill_backward(gloss, stats, z, idx, teacher, temperature=1.0, labels=None, alpha=1.0, weight=None, gz=None):
     """Gradient of z from that of the loss [rows] and distill_forward's stats (gz may be z itself)."""
     a = _distill_args(z, idx, teacher, temperature, labels, alpha, weight)
-    gz = torch.empty_like(z) if gz is None else gz
+    gz = _like(z) if gz is None else gz
     gp, gs = _rows(gz, z, z.shape, "gz")
     call("fdc_distill_backward", a, _f32(stats, z, (a.R, 5), "stats"), _f32(gloss, z, (a.R,), "gloss"), gp, gs,
          _stream())
@@ -328,7 +332,7 @@ def distill_forward_backward(gloss, z, idx, teacher, temperature=1.0, labels=Non
     """Loss and gradient in one call, for a gradient of the loss that is known beforehand -> (loss, gz)."""
     a = _distill_args(z, idx, teacher, temperature, labels, alpha, weight)
     loss, stats = _empty((a.R,), z, torch.float32), _empty((a.R, 5), z, torch.float32)
-    gz = torch.empty_like(z) if gz is None else gz
+    gz = _like(z) if gz is None else gz
     gp, gs = _rows(gz, z, z.shape, "gz")
     ws, size, keep = _distill_ws(a, z)
     call("fdc_distill_forward_backward", a, _f32(gloss, z, (a.R,), "gloss"), _ptr(loss), _ptr(stats), gp, gs, ws,

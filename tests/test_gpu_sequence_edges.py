@@ -138,3 +138,46 @@ def test_distill_teacher_of_nan(R, V, dtype):
     for r in range(12 if R > 12 else R):
         check(gz[r], rgz[r], f"gz {r}")
         check(gz2[r], rgz[r], f"gz in one call {r}")
+
+
+# ----------------------------------------------------------------------------
+# inputs whose rows overlap
+# ----------------------------------------------------------------------------
+@pytest.mark.parametrize("windows,width", [(9, 40), (40, 9)])
+def test_windows_of_a_signal_as_tokens(windows, width):
+    # one element apart: every stride is 1
+    m = Make(windows)
+    signal = m.f32(3, windows + width - 1)
+    x3, x2 = signal.unfold(1, width, 1), signal[0].unfold(0, width, 1)
+    assert x3.stride()[1:] == x2.stride() == (1, 1)
+
+    def same(f):
+        got, want = f(lambda t: t), f(lambda t: t.contiguous())
+        assert all(torch.equal(a, b) for a, b in zip(got, want) if a is not None)
+
+    w, A, Bm = m.f32(width, 3), -torch.exp(m.f32(width, 4)), m.f32(3, windows, 1, 4)
+    idx, teacher, gloss = torch.arange(3).repeat(windows, 1).int().cuda(), m.f32(windows, 3), m.f32(windows)
+
+    def conv(lay):
+        x = lay(x3)
+        return (*seq.causal_conv_forward(x, w, last=True), *seq.causal_conv_backward(x, x, w),
+                *seq.causal_conv_step(x[:, 0], w, x3.new_zeros(3, 2, width)))
+
+    def scan(lay):
+        x = lay(x3)
+        y, h, saved = seq.scan_forward(x, x, A, Bm, Bm, gate=x, last=True, save=True)
+        return (y, h, *seq.scan_backward(x, saved, x, x, A, Bm, Bm, gate=x))
+
+    def norm(lay):
+        x, p = lay(x2), w[:, 0].contiguous()
+        out, n, stats = seq.block_norm_forward(x, x, x, p, p, p)
+        return (out, n, *seq.block_norm_backward(x, x, stats, x, x, x, p, p, p))
+
+    def distill(lay):
+        z = lay(x2)
+        loss, stats = seq.distill_forward(z, idx, teacher)
+        return (loss, seq.distill_backward(gloss, stats, z, idx, teacher),
+                *seq.distill_forward_backward(gloss, z, idx, teacher))
+
+    for f in (conv, scan, norm, distill):
+        same(f)
