@@ -128,7 +128,7 @@ def _like(t):
         return None
     out = torch.empty_like(t)
     # rows that overlap (windows one element apart) leave torch no order of the dimensions
-    return out if out.stride(-1) == 1 or t.shape[-1] == 1 else t.new_empty(t.shape)
+    return out if out.dim() == 0 or out.stride(-1) == 1 or t.shape[-1] == 1 else t.new_empty(t.shape)
 
 
 # ----------------------------------------------------------------------------
@@ -155,8 +155,9 @@ def causal_conv_forward(x, w, bias=None, silu=False, state=None, lengths=None, l
     with SiLU if asked (fdc_causal_conv_forward).  state [B, taps - 1, D]: the tokens before x;
     new_state: the last ones, if `last` is asked for, else None."""
     y = _like(x) if y is None else y
-    new_state = _empty((x.shape[0], w.shape[1] - 1, x.shape[-1]), x) if last else None
-    a = _conv_args(x, w, bias, silu, state, lengths, y, new_state)
+    a = _conv_args(x, w, bias, silu, state, lengths, y, None)
+    new_state = _empty((a.B, a.n - 1, a.D), x) if last else None
+    a.new_state = _ptr(new_state)
     call("fdc_causal_conv_forward", a, _stream())
     return y, new_state
 
@@ -191,6 +192,8 @@ def causal_conv_backward(gy, x, w, bias=None, silu=False, state=None, lengths=No
 def _scan_args(x, dt, A, B, C, skip, gate, dt_bias, softplus, h0, h_last, lengths, y):
     kind = _kind(x, "x")
     shape = x.shape
+    if len(shape) not in (2, 3):
+        raise ValueError(f"x must be [B, L, D] or [B, D] (got {tuple(shape)})")
     nb, D = shape[0], shape[-1]
     if A.dim() != 2 or B.dim() != x.dim() + 1:
         raise ValueError(f"A must be [D, N] and B {'[B, L, G, N]' if x.dim() == 3 else '[B, G, N]'} "
@@ -212,8 +215,9 @@ def scan_forward(x, dt, A, B, C, skip=None, gate=None, dt_bias=None, softplus=Tr
     if x.dim() != 3:
         raise ValueError(f"x must be [B, L, D] (got {tuple(x.shape)})")
     y = _like(x) if y is None else y
-    h_last = _empty((x.shape[0], x.shape[2], A.shape[1]), x, torch.float32) if last else None
-    a = _scan_args(x, dt, A, B, C, skip, gate, dt_bias, softplus, h0, h_last, lengths, y)
+    a = _scan_args(x, dt, A, B, C, skip, gate, dt_bias, softplus, h0, None, lengths, y)
+    h_last = _empty((a.B, a.D, a.N), x, torch.float32) if last else None
+    a.h_last = _ptr(h_last)
     saved = _empty((_bytes("fdc_scan_saved_size", a.B, a.L, a.D, a.N) // 4,), x, torch.float32) if save else None
     ws, size, keep = _scratch(_bytes("fdc_scan_workspace_size", a.B, a.L, a.D, a.N, a.G, which=0, of=2), x)
     call("fdc_scan_forward", a, _ptr(saved), ws, size, _stream())

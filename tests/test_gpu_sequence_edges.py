@@ -181,3 +181,22 @@ def test_windows_of_a_signal_as_tokens(windows, width):
 
     for f in (conv, scan, norm, distill):
         same(f)
+
+
+def test_refusals_of_other_dimensions():
+    m = Make(1, "bf16")
+    x, w, A, Bm = m.act(2, 6, 8), m.f32(8, 4), m.f32(8, 4), m.act(2, 6, 1, 4)
+    for i, f in enumerate([
+            lambda: seq.causal_conv_forward(x, w[0], last=True),
+            lambda: seq.causal_conv_forward(x, w[0, 0], last=True),
+            lambda: seq.causal_conv_forward(x[0, 0], w, last=True),
+            lambda: seq.causal_conv_forward(x[0, 0, 0], w, last=True),
+            lambda: seq.causal_conv_backward(x[0, 0], x[0, 0], w),
+            lambda: seq.scan_forward(x, x, A[0], Bm, Bm, last=True),
+            lambda: seq.scan_forward(x, x, A, Bm[0, 0, 0], Bm, last=True),
+            lambda: seq.scan_backward(x[0, 0], A, x[0, 0], x[0, 0], A, Bm[0, 0], Bm[0, 0]),
+            lambda: seq.block_norm_forward(x[0, 0, 0]),
+            lambda: seq.distill_forward(x[0, 0], torch.zeros(8, 2, device="cuda").int(), m.act(8, 2))]):
+        with pytest.raises(ValueError):
+            f()
+            print("accepted", i)
