@@ -148,7 +148,7 @@ __global__ __launch_bounds__(256) void k_causal_conv_bwd(fdc_causal_conv_args a,
     for (int i = 0; i < V; ++i) gp[k][i] = 0.f;
   }
   const int last = gxb ? t1 + N - 1 : t1;  // gp is wanted for t < last
-  const int end = min(len, last);
+  const int end = min(len, last), own = min(len, t1);  // tokens loaded; tokens of this run's sums
   Pack<T, V> next_x[kConvUnroll], next_g[kConvUnroll];
   auto fetch = [&](int t) {
 #pragma unroll
@@ -168,7 +168,6 @@ __global__ __launch_bounds__(256) void k_causal_conv_bwd(fdc_causal_conv_args a,
     if (t + kConvUnroll < last) fetch(t + kConvUnroll);
 #pragma unroll
     for (int u = 0; u < kConvUnroll; ++u) {
-      const bool mine = t + u < t1;
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         float v = g[u][i];
@@ -179,12 +178,17 @@ __global__ __launch_bounds__(256) void k_causal_conv_bwd(fdc_causal_conv_args a,
           const float sg = sigmoid(p);
           v *= sg * (1.f + p * (1.f - sg));
         }
-        if (t + u >= len) v = 0.f;
-        gp[N - 1 + u][i] = v;
-        const float vm = mine ? v : 0.f;
-        gb[i] += vm;
+        gp[N - 1 + u][i] = t + u < len ? v : 0.f;
+      }
+      // (a product with 0 would not do: a row of the window may hold what is not finite)
+      if (t + u < own) {
 #pragma unroll
-        for (int j = 0; j < N; ++j) gw[j][i] = fmaf(vm, x[u + j][i], gw[j][i]);
+        for (int i = 0; i < V; ++i) {
+          const float v = gp[N - 1 + u][i];
+          gb[i] += v;
+#pragma unroll
+          for (int j = 0; j < N; ++j) gw[j][i] = fmaf(v, x[u + j][i], gw[j][i]);
+        }
       }
       const int to = t + u - (N - 1);  // gp[to .. t + u] are here
       if (gxb && to >= t0 && to < t1) {

@@ -200,3 +200,28 @@ def test_refusals_of_other_dimensions():
         with pytest.raises(ValueError):
             f()
             print("accepted", i)
+
+
+# ----------------------------------------------------------------------------
+# causal convolution
+# ----------------------------------------------------------------------------
+@pytest.mark.parametrize("n", [2, 4, 8])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_conv_token_that_is_not_finite(n, dtype):
+    # gw sums the products of a sequence's own tokens: a last token that is not finite meets the last tap alone, and
+    # an infinity elsewhere (at the edges of the shortest runs, among others) leaves infinities, no NaN
+    print(f"conv not finite n={n} {dtype}", flush=True)
+    m = Make(n, dtype)
+    places = [5, 7, 8, 9, 15, 16, 20, 39]
+    D, L = 2 * len(places), 40
+    x, gy, w = m.act(1, L, D), m.act(1, L, D), m.f32(D, n)
+    for c, t in enumerate(places):
+        x[0, t, 2 * c] = float("inf")
+        x[0, t, 2 * c + 1] = float("nan")
+    for lengths in (None, [40], [21]):
+        ln = lengths and torch.tensor(lengths, dtype=torch.int32).cuda()
+        gx, gw, _ = seq.causal_conv_backward(gy, x, w, lengths=ln)
+        rx, rw, _ = oracle.causal_conv_backward(host(gy), host(x), host(w), lengths=lengths)
+        check(gx, rx, "gx")
+        for c in range(D):
+            check(gw[c], rw[c], f"gw {c} {lengths}")
