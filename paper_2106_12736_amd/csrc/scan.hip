@@ -583,7 +583,7 @@ __global__ __launch_bounds__(ScanLane<LN>::Threads, LN == 2 ? 1 : 2) void k_scan
     for (int i = threadIdx.x; i < kTok * 2 * NP; i += Lane::Threads) {
       const int s = i / (2 * NP), kind = i / NP % 2, n = i % NP;
       float v = 0.f;
-      if (t0 < len)
+      if (t0 + s < len)
 #pragma unroll
         for (int w = 0; w < Lane::Waves; ++w) v += wsum[w][i];
       if (n < a.N && t0 + s < t_end) pbc[kind * kind_stride + (int64_t)(t0 + s) * GN + n] = v;

@@ -225,3 +225,33 @@ def test_conv_token_that_is_not_finite(n, dtype):
         check(gx, rx, "gx")
         for c in range(D):
             check(gw[c], rw[c], f"gw {c} {lengths}")
+
+
+# ----------------------------------------------------------------------------
+# selective scan
+# ----------------------------------------------------------------------------
+@pytest.mark.parametrize("N", [4, 16, 40])
+def test_scan_state_that_is_not_finite(N):
+    # what comes before it is as it was, and the tokens past the sequence have gradients of 0
+    print(f"scan not finite N={N}", flush=True)
+    m = Make(N)
+    v = scan_inputs(m, 2, 40, 24, N, 1, True, True, True, True, None, "dense")
+    gy = m.act(2, 40, 24)
+    v["x"][0, 20, 3], v["x"][0, 20, 5] = float("inf"), float("nan")
+    gy[0, 21:] = 0
+    lengths = [21, 33]
+    ln = torch.tensor(lengths, dtype=torch.int32).cuda()
+    y, h, saved = seq.scan_forward(**v, lengths=ln, last=True, save=True)
+    g = seq.scan_backward(gy, saved, **v, lengths=ln)
+    hv = {k: host(t) for k, t in v.items()}
+    with np.errstate(invalid="ignore"):
+        ry, rh, _ = oracle.scan(**hv, lengths=lengths)
+        want = oracle.scan_backward(host(gy), **hv, lengths=lengths)
+    check(y[0, :20], ry[0, :20], "y")
+    check(y[1], ry[1], "y of the other sequence")
+    assert not bool(torch.isfinite(y[0, 20, [3, 5]]).any()) and not bool(torch.isfinite(h[0, [3, 5]]).any())
+    for k in ("x", "dt", "B", "C", "gate"):
+        got = getattr(g, k)
+        check(got[0, :20], want[k][0, :20], f"g{k}")
+        check(got[1], want[k][1], f"g{k} of the other sequence")
+        assert not bool(got[0, 21:].any()), f"g{k} past the sequence"
