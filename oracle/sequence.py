@@ -183,9 +183,10 @@ def block_norm_backward(gout, gn, x, f=None, gate=None, scale=None, w_post=None,
 # ----------------------------------------------------------------------------
 # distillation
 # ----------------------------------------------------------------------------
-def _lse(v):
-    m = v.max()
-    return m + np.log(np.exp(v - m).sum())
+def _log_softmax(v):
+    """From the differences to the largest value: m + log(sum) would lose the logarithm next to an m of 1e38."""
+    d = v - v.max()
+    return d - np.log(np.exp(d).sum())
 
 
 def distill(z, idx, teacher, temperature=1.0, labels=None, alpha=1.0, weight=None, gloss=None):
@@ -203,20 +204,20 @@ def distill(z, idx, teacher, temperature=1.0, labels=None, alpha=1.0, weight=Non
             continue
         g = w * (1.0 if gloss is None else gloss[r])
         if label >= 0:
-            lse = _lse(z[r])
-            loss[r] += w * (1 - alpha) * (lse - z[r, label])
-            gz[r] += g * (1 - alpha) * np.exp(z[r] - lse)
+            lp = _log_softmax(z[r])
+            loss[r] -= w * (1 - alpha) * lp[label]
+            gz[r] += g * (1 - alpha) * np.exp(lp)
             gz[r, label] -= g * (1 - alpha)
         at = np.flatnonzero(idx[r] >= 0)
         t = teacher[r, at] / temperature
         if len(at) == 0 or np.all(t == -np.inf):
             continue
-        lse = _lse(z[r] / temperature)
-        lq = t - _lse(t)
+        lp = _log_softmax(z[r] / temperature)
+        lq = _log_softmax(t)
         q = np.exp(lq)
         on = q > 0
-        kl = q[on] * (lq[on] - (z[r, idx[r, at][on]] / temperature - lse))
+        kl = q[on] * (lq[on] - lp[idx[r, at][on]])
         loss[r] += w * alpha * temperature ** 2 * kl.sum()
-        gz[r] += g * alpha * temperature * np.exp(z[r] / temperature - lse)
+        gz[r] += g * alpha * temperature * np.exp(lp)
         np.subtract.at(gz[r], idx[r, at], g * alpha * temperature * q)
     return loss, gz
