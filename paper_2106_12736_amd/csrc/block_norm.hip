@@ -15,7 +15,9 @@
 // registers (read again for every row they would be more than the row itself), and the next row's
 // loads are on their way while a row is worked on.  The sums over a row are formed in float32, across
 // the wave by lane moves and across waves through LDS.  16384 rows of 2048 bf16: forward 69 us (4.9
-// TB/s of a copy's 5.1), backward 131 us (4.1 TB/s).
+// TB/s of a copy's 5.1), backward 128 us (4.2 TB/s); float32 127 us (5.3) and 245 us (4.4).  Past 4096
+// channels the backward's two vectors a thread spill 20 to 25 registers: 16384 rows of 8192 bf16 take
+// 1267 us (1.7 TB/s), 8192 rows in float32 867 us (2.5).
 #include <algorithm>
 
 #include "sequence.h"
@@ -304,8 +306,9 @@ int fwd_vecs(int D) {
   return (int)ceil_div(D, kNormV<T>);
 }
 int bwd_vecs(int D) { return (int)ceil_div(D, kBwdV); }
-// Workgroups: the forward's as many as run at once (eight waves a SIMD); the backward's half of that, by
-// its registers, and because each leaves its sums of the parameters' gradients.
+// Workgroups: the forward's fill eight waves a SIMD (the 16-bit forms have registers for five or six, so up
+// to two rounds of them); the backward's half of that, by its registers (the float32 form of 512 threads has
+// 130 of them, room for one workgroup a compute unit), and because each leaves its sums of the parameters' gradients.
 constexpr long long kCus = 256;
 long long row_blocks(int64_t R, int rows, int threads, int waves_a_simd) {
   return std::min<long long>(ceil_div(R, rows), kCus * 256 * waves_a_simd / threads);

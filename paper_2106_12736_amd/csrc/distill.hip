@@ -211,15 +211,19 @@ __device__ __forceinline__ void write_entries(const Entries &en, const Factors &
 // ---- a row a workgroup -------------------------------------------------------
 // Keeps the compiler from holding the floats of one pass over a row's pieces for the next: 16-bit
 // logits would take twice their registers, and fewer rows would be in flight on a compute unit
-// (for float32 it only costs: 2048 x 32000 206 us with it, 166 us without).
+// (for float32 it only costs: 2048 x 32000 206 us with it, 166 us without).  For float16 rows of 8 pieces
+// it does not hold: the gradient's form spills 164 registers (bfloat16's 5), and 4096 x 32000 takes 497 us
+// where bfloat16 takes 153.
 template <class T, int V>
 __device__ __forceinline__ void keep_packed(Pack<T, V> &x) {
   if constexpr (sizeof(T) == 2) asm volatile("" : "+v"(x.w[0]), "+v"(x.w[1]), "+v"(x.w[2]), "+v"(x.w[3]));
 }
 
 // A workgroup a row.  The row's phases (load, largest logit, sums, gradient) follow each other behind
-// barriers; three to six rows on a compute unit overlap them.  4096 x 32000 bfloat16, K = 64: 155 us (3.4 TB/s of
-// 5.1; its 15 plain operations and four exponentials an element would take 87 us alone).  Measured
+// barriers; the rows on a compute unit overlap them: 512 threads are two waves a SIMD, so that four rows of 4
+// pieces (f16: three), three of 8, and of 16 pieces two in 16 bits and one in float32 (168 registers) fit at once.  4096 x 32000
+// bfloat16, K = 64: 153 us (3.4 TB/s of 5.1; its 15 plain operations and four exponentials an element would take
+// 87 us alone); 2048 x 32000 float32 163 us (3.2).  Measured
 // and not kept: workgroups that take row after row with the next one loaded ahead (200 to 220 us: twice the
 // registers, half the rows in flight), 256 threads (185), 1024 threads (262).
 template <class T, int TH, int NV, bool Grad>
@@ -448,8 +452,11 @@ dim3 segment_grid(const Segments &sg, int64_t R) {
 dim3 row_grid(int64_t R) { return dim3((unsigned)std::min<int64_t>(R, 32768), (unsigned)ceil_div(R, 32768)); }
 
 // Rows that fit a workgroup's registers (16 pieces of 16 bytes in 512 threads), and enough of them for
-// the chip's 256 compute units: one for each, or three where a row takes a third of a unit's
-// registers (300 rows of 20000 f16: 39 us a row a workgroup, 24 us in segments).
+// the chip's 256 compute units: one for each, or three where a row takes a third of a unit's registers or more.
+// Loss and gradient in segments (a row fewer) and a row a workgroup: 256 rows of 8192 bf16 19.5 and 13.0 us, f32
+// 21.9 and 13.4; 768 rows of 20000 bf16 42 and 26, f32 48 and 43; of 60000 bf16 76 and 56.  f16 is as bf16 but for
+// rows of 5 to 8 pieces, whose spills (see keep_packed) make the row a workgroup the slower one: 20000 logits 43
+// and 74 us.  Longer rows are read twice: 1024 of 65536 bf16 75 us, of 65537 107 us.
 bool whole_rows(int dtype, int64_t R, int V) {
   const long long pieces = ceil_div(V, 16 / (int)dtype_size(dtype));
   return pieces <= 512 * 16 && R >= (pieces <= 512 * 4 ? 256 : 3 * 256);

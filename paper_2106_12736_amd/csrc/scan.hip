@@ -11,8 +11,11 @@
 // The decay differs for every channel, state and token, so there is no matrix product in it: each
 // (token, channel, state) takes an exponential (four issue slots of a full-rate operation) and
 // four multiplications and additions forward, about thirteen backward.  The vector units bound both;
-// HBM would take a ninth of the time (8 x 1024 tokens, 2048 channels of 16 states, bf16: 142 us
-// forward, 355 us backward; one sequence of 16384 tokens: 259 us forward).
+// HBM would take a ninth of the time (8 x 1024 tokens, 2048 channels of 16 states, bf16: 143 us
+// forward, 348 us backward; one sequence of 16384 tokens: 259 us forward).  Counted at 8 x 1024 tokens:
+// the vector units are busy for 85 and 88 % of the forward passes' cycles, with 8.3 and 5.5 instructions a
+// state and token, and for 77 and 74 % of the backward ones', with 6.2 and 25; LDS for 29 % of the
+// backward's (the channel sums of gB and gC), without bank conflicts.
 //
 // LN adjacent lanes share a channel and hold SN = 4 states each, so a wave owns 64 / LN channels and
 // walks along the tokens in blocks of 16.  What a token needs once per channel (softplus, gate,
@@ -405,7 +408,10 @@ __global__ __launch_bounds__(ScanLane<LN>::Threads) void k_scan_bwd_local(fdc_sc
 }
 
 // The backward proper.  A block's states are formed again from the saved one in front of it and
-// kept in registers (16 tokens x 4 states and their decays), then the block is walked backwards.
+// kept in registers (16 tokens x 4 states), then the block is walked backwards, with each decay formed
+// once more.  Two waves a SIMD by its registers: with four lanes a channel (9 to 16 states) the bound of
+// 256 spills 6 of them in 16 bits and 19 in float32; with two (up to 8 states) a bound of two waves would
+// spill far more, and one wave a SIMD is left.
 // The sums of gB and gC over the channels: every fourth token the lanes put their four products of
 // four tokens into LDS and add them up over the wave's channels the other way round; the waves'
 // sums are added in wave order, and the workgroups' partial sums
@@ -662,11 +668,14 @@ namespace {
 int lanes_of(int N) { return N <= 8 ? 2 : N <= 16 ? 4 : N <= 32 ? 8 : 16; }
 
 // One wave on a SIMD issues an instruction every 6.5 cycles, two together every 5, four every 4.5
-// (measured), and a chunk's first pass costs about 0.6 of a forward scan and 0.2 of a backward one: the
+// (measured), and a chunk's first pass costs about 0.65 of a forward scan and 0.26 of a backward one: the
 // forward is cut into chunks where the channels give no more than one wave a SIMD, the backward (two waves
 // a SIMD by its registers) where they give fewer than two.  (2048 channels of 16 states, forward:
 // 8 x 1024 tokens 163 us whole, 147 us in chunks; 16 x 1024 tokens 204 and 284.  Backward, 8 x 1024
-// tokens: 430 us whole, 359 us in chunks.)
+// tokens: 430 us whole, 359 us in chunks.)  The rule was measured at 16 states alone; with up to 8 the
+// backward's registers leave it one wave a SIMD whatever the chunks (16 x 1024 tokens: 667 us with 8 states,
+// 535 with 16).  The first pass also walks the chunk that none starts from (the forward's last, the backward's
+// first), whose result is not used.
 // A chunk may be as short as a block; but a block alone takes a wave 3 us forward and 7 us backward and
 // the two launches that chunks add 9 us, so that sequences of fewer than 6 and 4 blocks are not cut.
 constexpr long long kSimds = 1024;
