@@ -98,26 +98,27 @@ __device__ __forceinline__ TeacherStat teacher_stat(const Entries &en, const fdc
   return te;
 }
 
-// By one wave: the loss of a row (of weight other than 0), and its statistics.
+// By one wave: the loss of a row (of weight other than 0), and its statistics.  In units of two binary
+// logarithms, so that a named place at the type's lowest value (masked) stays within float32 like its logit does.
 __device__ __forceinline__ void row_loss(const fdc_distill_args &a, int64_t row, int lane, const Entries &en,
                                          const Stat &st, const TeacherStat &te, float *loss, float *stats) {
-  const float c1 = kLog2e, ct = kLog2e / a.tau;
+  const float c1 = 0.5f * kLog2e, ct = kLog2e / a.tau;
   float kl = 0.f;
   if (!te.bad && te.s != 0.f) {
-    const float log_st = log2_fast(st.st), log_ts = log2_fast(te.s);
+    const float log_st = 0.5f * log2_fast(st.st), log_ts = log2_fast(te.s);
     for (int k = lane; k < a.K; k += 64) {
       if (en.place[k] < 0) continue;
       const float lq = (en.t[k] - te.m) * ct - log_ts, q = exp2_fast(lq);
-      if (!(q == 0.f)) kl += q * (lq - ((en.z[k] - st.m) * ct - log_st));
+      if (!(q == 0.f)) kl += q * (0.5f * lq - ((en.z[k] - st.m) * (0.5f * ct) - log_st));
     }
   }
   kl = wave_sum(kl);
   if (lane != 0) return;
   float l = 0.f;
   if (en.place[a.K] >= 0 && !te.bad && a.alpha < 1.f)
-    l = (1.f - a.alpha) * (log2_fast(st.s1) - (en.z[a.K] - st.m) * c1);
+    l = (1.f - a.alpha) * (0.5f * log2_fast(st.s1) - (en.z[a.K] - st.m) * c1);
   if (a.alpha > 0.f) l += a.alpha * a.tau * a.tau * kl;
-  loss[row] = te.bad ? NAN : (a.weight ? a.weight[row] : 1.f) * kLn2 * l;
+  loss[row] = te.bad ? NAN : (a.weight ? a.weight[row] : 1.f) * (2.f * kLn2) * l;
   float *p = stats + kDistillStats * row;
   p[0] = te.bad ? NAN : st.m;
   p[1] = st.s1, p[2] = st.st, p[3] = te.m, p[4] = te.s;

@@ -255,3 +255,38 @@ def test_scan_state_that_is_not_finite(N):
         check(got[0, :20], want[k][0, :20], f"g{k}")
         check(got[1], want[k][1], f"g{k} of the other sequence")
         assert not bool(got[0, 21:].any()), f"g{k} past the sequence"
+
+
+@pytest.mark.parametrize("R,V", [(12, 301), (260, 301), (770, 20001)])  # in segments, rows in registers
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_distill_named_places_that_are_masked(R, V, dtype):
+    # a label or a teacher's place at the type's lowest value: the loss is large, and finite as the logit is
+    print(f"distill masked names R={R} V={V} {dtype}", flush=True)
+    m = Make(V + 1, dtype)
+    z, teacher, gloss = m.act(R, V, scale=3.0), m.act(R, 6), m.f32(R)
+    idx = torch.stack([torch.randperm(V, generator=m.g)[:6] for _ in range(R)]).int().cuda()
+    labels = torch.full((R,), -1, dtype=torch.int32, device="cuda")
+    low = torch.finfo(z.dtype).min
+    labels[1] = idx[1, 0]
+    z[1, labels[1]] = low
+    idx[1, 0] = -1                                                        # the label alone
+    z[2, idx[2, 3]] = low                                                 # a place of the teacher
+    z[3, idx[3].long()] = low                                             # all of them
+    labels[4], idx[5] = idx[4, 2], -1
+    z[4] = low
+    z[4, (int(labels[4]) + 1) % V] = 2.0                                  # all but one place that is not named
+    idx[4, idx[4] == (labels[4] + 1) % V] = -1
+    kw = {"temperature": 1.25, "labels": labels, "alpha": 0.5}
+    rloss, rgz = oracle.distill(host(z), idx.cpu().numpy(), host(teacher), 1.25, labels.cpu().numpy(), 0.5,
+                                gloss=host(gloss))
+    rows = [0, 1, 2, 3, 5] + ([4] if dtype == "f16" else [])              # (past float32 in the others)
+    assert np.isfinite(rloss[rows].astype(np.float32)).all()
+    loss, stats = seq.distill_forward(z, idx, teacher, **kw)
+    gz = seq.distill_backward(gloss, stats, z, idx, teacher, **kw)
+    both, gz2 = seq.distill_forward_backward(gloss, z, idx, teacher, **kw)
+    for r in rows:
+        check(loss[r:r + 1], rloss[r:r + 1], f"loss {r}")
+        check(both[r:r + 1], rloss[r:r + 1], f"loss in one call {r}")
+    for r in range(6):
+        check(gz[r], rgz[r], f"gz {r}")
+        check(gz2[r], rgz[r], f"gz in one call {r}")
