@@ -488,7 +488,7 @@ __global__ __launch_bounds__(ScanLane<LN>::Threads, LN == 2 ? 1 : 2) void k_scan
         raw[i] = in ? (float)tdt.v[i] + bias : 0.f;
         delta[i] = step_size(raw[i], a.softplus, in);
         u[i] = delta[i] * x[i];
-        gs[i] = gated ? gyv[i] * gate[i] * sigmoid(gate[i]) : gyv[i];
+        gs[i] = gated ? gyv[i] * (gate[i] * sigmoid(gate[i])) : gyv[i];
         out[i] = gu[i] = gd[i] = 0.f;
       }
     };

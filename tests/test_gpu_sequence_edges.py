@@ -290,3 +290,28 @@ def test_distill_named_places_that_are_masked(R, V, dtype):
     for r in range(6):
         check(gz[r], rgz[r], f"gz {r}")
         check(gz2[r], rgz[r], f"gz in one call {r}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("L,N", [(20, 16), (200, 5), (200, 40)])
+def test_scan_tokens_masked_with_the_lowest_value(L, N, dtype):
+    # a gate of the type's lowest value shuts its token off, a dt of it (or of -inf) leaves the state as it is
+    print(f"scan lowest L={L} N={N} {dtype}", flush=True)
+    m = Make(L + N, dtype)
+    v = scan_inputs(m, 2, L, 24, N, 1, True, True, True, True, None, "dense")
+    low = torch.finfo(v["x"].dtype).min
+    v["gate"][0, 3], v["gate"][1, L - 1, ::2] = low, low
+    v["dt"][0, 5], v["dt"][1, 7:12] = low, float("-inf")
+    gy = m.act(2, L, 24, scale=3.0)
+    y, h, saved = seq.scan_forward(**v, last=True, save=True)
+    g = seq.scan_backward(gy, saved, **v)
+    hv = {k: host(t) for k, t in v.items()}
+    with np.errstate(over="ignore"):
+        ry, rh, _ = oracle.scan(**hv)
+        want = oracle.scan_backward(host(gy), **hv)
+    check(y, ry, "y")
+    check(h, rh, "h")
+    for k in v:
+        check(getattr(g, k), want[k], f"g{k}")
+    out, _, _ = seq.block_norm_forward(v["x"][0], v["dt"][1, 12:13].expand(L, 24), v["gate"][0], act="silu")
+    check(out, oracle.block_norm(hv["x"][0], np.repeat(hv["dt"][1, 12:13], L, 0), hv["gate"][0])[0], "out of the norm")
