@@ -468,8 +468,9 @@ fdc_status fdc_causal_conv_backward(const fdc_causal_conv_args *a, fdc_tokens gy
  *   h[t][n] = exp(delta A[d][n]) h[t-1][n] + delta x[t] Bm[t][g][n]
  *   y[t] = (sum_n Cm[t][g][n] h[t][n] + skip[d] x[t]) silu(gate[t])
  * x, dt, gate, y: [B][L][D]; Bm, Cm: [B][L][G N]; A [D][N]; skip, dt_bias [D] (NULL: 0);
- * gate absent: no factor.  y may be x, dt or gate itself (a backward needs them).  h0 [B][D][N] (NULL: zeros) is the state before the first token,
- * h_last [B][D][N] (NULL: not wanted; not h0) the one after the last.
+ * gate absent: no factor.  y may be x, dt or gate itself (which a backward would need).
+ * h0 [B][D][N] (NULL: zeros) is the state before the first token, h_last [B][D][N]
+ * (NULL: not wanted; not h0) the one after the last.
  * saved (NULL: no backward follows): fdc_scan_saved_size bytes, 16-byte aligned, for the
  * backward: the states at every 16th token. */
 typedef struct {

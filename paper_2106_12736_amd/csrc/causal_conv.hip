@@ -6,8 +6,8 @@
 // A thread owns V adjacent channels of a run of tokens and walks along it with the last n - 1
 // rows in registers, so each input crosses HBM once but for the n - 1 rows in front of a run.
 // Both directions are bound by HBM: no channel shares anything with another, and a token
-// takes n multiply-adds a channel.  8 x 2048 tokens, 4096 channels, 4 taps, bf16: forward 65 us (4.1 TB/s),
-// backward 107 us (3.8 TB/s), in float32 4.7 and 4.5 TB/s; a large copy runs at 5.1.
+// takes n multiply-adds a channel.  8 x 2048 tokens, 4096 channels, 4 taps, bf16: forward 65 to 68 us (4.1 TB/s),
+// backward 107 to 114 us (3.8 to 3.5 TB/s), in float32 4.7 and 4.5 TB/s; a large copy runs at 5.1.
 #include "sequence.h"
 
 namespace fdc {

@@ -14,7 +14,7 @@
 // HBM would take a ninth of the time (8 x 1024 tokens, 2048 channels of 16 states, bf16: 143 us
 // forward, 348 us backward; one sequence of 16384 tokens: 259 us forward).  Counted at 8 x 1024 tokens:
 // the vector units are busy for 85 and 88 % of the forward passes' cycles, with 8.3 and 5.5 instructions a
-// state and token, and for 77 and 74 % of the backward ones', with 6.2 and 25; LDS for 29 % of the
+// state and token, and for 78 and 76 % of the backward ones', with 6.2 and 25; LDS for 30 % of the
 // backward's (the channel sums of gB and gC), without bank conflicts.
 //
 // LN adjacent lanes share a channel and hold SN = 4 states each, so a wave owns 64 / LN channels and
@@ -410,7 +410,7 @@ __global__ __launch_bounds__(ScanLane<LN>::Threads) void k_scan_bwd_local(fdc_sc
 // The backward proper.  A block's states are formed again from the saved one in front of it and
 // kept in registers (16 tokens x 4 states), then the block is walked backwards, with each decay formed
 // once more.  Two waves a SIMD by its registers: with four lanes a channel (9 to 16 states) the bound of
-// 256 spills 6 of them in 16 bits and 19 in float32; with two (up to 8 states) a bound of two waves would
+// 256 spills 4 of them in 16 bits and 19 in float32; with two (up to 8 states) a bound of two waves would
 // spill far more, and one wave a SIMD is left.
 // The sums of gB and gC over the channels: every fourth token the lanes put their four products of
 // four tokens into LDS and add them up over the wave's channels the other way round; the waves'

@@ -211,7 +211,8 @@ def scan_forward(x, dt, A, B, C, skip=None, gate=None, dt_bias=None, softplus=Tr
                  last=False, save=False, y=None):
     """Selective scan (fdc_scan_forward) of x, dt, gate [B, L, D] with A [D, N], B, C [B, L, G, N], skip and
     dt_bias [D] from the state h0 [B, D, N] -> (y, h_last, saved): the state after the last token if `last`
-    is asked for, and what scan_backward needs if `save` is; else None.  y may be x, dt or gate itself."""
+    is asked for, and what scan_backward needs if `save` is; else None.  y may be x, dt or gate
+    itself (which scan_backward would need)."""
     if x.dim() != 3:
         raise ValueError(f"x must be [B, L, D] (got {tuple(x.shape)})")
     y = _like(x) if y is None else y
