@@ -565,6 +565,94 @@ fdc_status fdc_distill_backward(const fdc_distill_args *a, const float *stats, c
 fdc_status fdc_distill_forward_backward(const fdc_distill_args *a, const float *gloss, float *loss, float *stats,
                                         void *gz, int64_t gz_stride, void *ws, size_t ws_bytes, hipStream_t stream);
 
+/* A [B][L][heads][D] tensor: element (b, t, h, c) is at p[b * batch_stride + t * token_stride + h * head_stride + c]
+ * (strides in elements, >= 0, token_stride below 2^25, head_stride below 2^30).  What fdc_tokens says of absent tensors, strides
+ * of 0, alignment, and outputs holds here too. */
+typedef struct {
+  void *p;
+  int64_t batch_stride;
+  int64_t token_stride;
+  int64_t head_stride;
+} fdc_heads;
+
+/* Rotary positions of up to 4 axes (for example frame, row and column of a pixel): the first 2 P channels of every head
+ * are P pairs, and each is turned by its angle,
+ *   (u, v) -> (u cos(a) - v sin(a), u sin(a) + v cos(a)),  a = position[axis of the pair] * freqs[pair],
+ * the other D - 2 P channels are copied.  Pairs: the first pairs[0] belong to axis 0, the next pairs[1] to axis 1, ...;
+ * P is their sum, 2 P <= D <= 1024.  Pair i is the channels (i, P + i), or (2 i, 2 i + 1) if interleaved.
+ * x, y [B][L][H][D]; y may be x itself.  positions [B][L][axes] int32, the axes of a token side by side, strides in
+ * elements (>= 0, 0: the same for every sequence).  freqs [P] float32.  The angle is formed and reduced in 64 bits
+ * (positions up to 2^31, |a| up to 2^40).
+ * inverse: turned back by -a, which is the gradient of x from that of y (the backward).  No gradient is formed for freqs. */
+typedef struct {
+  int dtype, B, L, H, D, axes, interleaved, inverse;
+  int pairs[4];
+  fdc_heads x, y;
+  const int32_t *positions;
+  int64_t pos_batch_stride, pos_token_stride;
+  const float *freqs;
+  const int32_t *lengths;
+} fdc_rotary_args;
+fdc_status fdc_rotary(const fdc_rotary_args *a, hipStream_t stream);
+
+/* Attention of Lq tokens to Lk states of another length (an encoder's, for example the pixels of an FDCNN's planes), H
+ * heads of queries, G heads of keys and values that H / G adjacent query heads share:
+ *   s[j] = scale q[b][t][h] . k[b][j][h / (H / G)],   y[b][t][h] = sum_j softmax(s)[j] v[b][j][h / (H / G)]
+ * over the keys j that sequence b has: j < lengths[b] and mask[b * mask_stride + j] != 0 (either NULL: no such limit).
+ * What k and v hold at other keys is never used, NaN included.  A row without keys has y = 0 and lse = -inf.
+ * q, y [B][Lq][H][D]; k, v [B][Lk][G][D]; 1 <= D <= 128; scale > 0.  q_lengths [B] (NULL: Lq): the queries' lengths.
+ * lse [B][H][Lq] float32 (NULL: no backward follows): log sum_j exp(s[j]), -inf past a sequence's queries.
+ * A single token is a call with Lq = 1.  y is other memory than q, k and v.
+ * ws: fdc_cross_attention_workspace_size's fwd_ws bytes. */
+typedef struct {
+  int dtype, B, Lq, Lk, H, G, D;
+  float scale;
+  fdc_heads q, k, v, y;
+  const int32_t *q_lengths, *lengths;
+  const uint8_t *mask;
+  int64_t mask_stride;
+} fdc_cross_attention_args;
+fdc_status fdc_cross_attention_workspace_size(int dtype, int B, int Lq, int Lk, int H, int G, int D, size_t *fwd_ws,
+                                              size_t *bwd_ws);
+fdc_status fdc_cross_attention_forward(const fdc_cross_attention_args *a, float *lse, void *ws, size_t ws_bytes,
+                                       hipStream_t stream);
+/* From gy, the forward's inputs, its y and its lse: gq, gk, gv (type of the activations, all required; gk and gv summed
+ * over the query heads that share them, 0 at keys that a sequence does not have).  Sums run in a fixed order. */
+typedef struct {
+  fdc_heads gy, gq, gk, gv;
+} fdc_cross_attention_grads;
+fdc_status fdc_cross_attention_backward(const fdc_cross_attention_args *a, const float *lse,
+                                        const fdc_cross_attention_grads *g, void *ws, size_t ws_bytes,
+                                        hipStream_t stream);
+
+/* Log probabilities of R rows of V logits z at a temperature tau > 0, with l = log softmax(z / tau):
+ *   logp[r] = l[tokens[r]],   entropy[r] = -sum_v exp(l[v]) l[v],   idx[r][k], top[r][k]: the K largest logits' places
+ * and l there, from high to low, equal logits by rising place (0 <= K <= 128, K <= V; a NaN counts as the largest).
+ * z [R][V] with row stride z_stride.  tokens [R] int32 (NULL: no logp): a row with tokens < 0 has logp 0 (and no gradient
+ * through it); a token >= V gives a NaN logp, and NaN gradients in its row.  A place of -inf adds nothing to the entropy;
+ * a row of -inf alone, or with +inf or NaN, has a NaN logp, entropy and top.  logp, entropy, top float32, idx int32, dense;
+ * idx and top [R][K] go together (both NULL where K = 0).
+ * stats [R][3] float32 (NULL: no backward follows): the largest logit m, the sum of exp((z - m) / tau), the entropy. */
+typedef struct {
+  int dtype, V, K;
+  int64_t R;
+  float tau;
+  const void *z;
+  int64_t z_stride;
+  const int32_t *tokens;
+} fdc_token_logprobs_args;
+fdc_status fdc_token_logprobs_workspace_size(int dtype, int64_t R, int V, int K, size_t *bytes);
+fdc_status fdc_token_logprobs_forward(const fdc_token_logprobs_args *a, float *logp, float *entropy, int32_t *idx,
+                                      float *top, float *stats, void *ws, size_t ws_bytes, hipStream_t stream);
+/* gz (z's type; it may be z itself) from the gradients of logp [R], entropy [R] and top [R][K] (each NULL: zero; gtop with
+ * the forward's idx) and the forward's stats:
+ *   gz[v] = 1/tau ([v = token] glogp + sum_k [v = idx_k] gtop[k] - p[v] (glogp + sum_k gtop[k]) - gentropy p[v] (l[v] + entropy))
+ * A gradient of 0 for all of a row's outputs is a gz row of 0, whatever the row holds.  idx outside [0, V): as a token
+ * there is. */
+fdc_status fdc_token_logprobs_backward(const fdc_token_logprobs_args *a, const float *stats, const float *glogp,
+                                       const float *gentropy, const int32_t *idx, const float *gtop, void *gz,
+                                       int64_t gz_stride, hipStream_t stream);
+
 /* ------------------------------------------------------------------------ */
 /* Kernel timing (measurement support, off by default)                      */
 /* ------------------------------------------------------------------------ */

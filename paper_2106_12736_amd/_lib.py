@@ -33,6 +33,12 @@ class Tokens(ctypes.Structure):
     _fields_ = [("p", _P), ("batch_stride", _I64), ("token_stride", _I64)]
 
 
+class Heads(ctypes.Structure):
+    """fdc_heads: a [B][L][heads][D] tensor by its strides in elements."""
+
+    _fields_ = [("p", _P), ("batch_stride", _I64), ("token_stride", _I64), ("head_stride", _I64)]
+
+
 def _struct(name, doc, *fields):
     return type(name, (ctypes.Structure,), {"__doc__": doc, "_fields_": list(fields)})
 
@@ -56,6 +62,15 @@ NormGrads = _struct("NormGrads", "fdc_block_norm_grads", *_named(_P, "gout gn gx
 DistillArgs = _struct("DistillArgs", "fdc_distill_args", *_named(_I, "dtype V K"), ("R", _I64),
                       *_named(ctypes.c_float, "tau alpha"), ("z", _P), ("z_stride", _I64),
                       *_named(_P, "idx teacher labels weight"))
+RotaryArgs = _struct("RotaryArgs", "fdc_rotary_args", *_named(_I, "dtype B L H D axes interleaved inverse"),
+                     ("pairs", _I * 4), *_named(Heads, "x y"), ("positions", _P),
+                     *_named(_I64, "pos_batch_stride pos_token_stride"), *_named(_P, "freqs lengths"))
+CrossAttentionArgs = _struct("CrossAttentionArgs", "fdc_cross_attention_args", *_named(_I, "dtype B Lq Lk H G D"),
+                             ("scale", ctypes.c_float), *_named(Heads, "q k v y"),
+                             *_named(_P, "q_lengths lengths mask"), ("mask_stride", _I64))
+CrossAttentionGrads = _struct("CrossAttentionGrads", "fdc_cross_attention_grads", *_named(Heads, "gy gq gk gv"))
+TokenLogprobsArgs = _struct("TokenLogprobsArgs", "fdc_token_logprobs_args", *_named(_I, "dtype V K"), ("R", _I64),
+                            ("tau", ctypes.c_float), ("z", _P), ("z_stride", _I64), ("tokens", _P))
 _SZP = ctypes.POINTER(_SZ)
 
 # name -> argtypes (restype is int status unless listed in _RESTYPES)
@@ -134,6 +149,14 @@ _SIGS = {
     "fdc_distill_forward": [ctypes.POINTER(DistillArgs), _P, _P, _P, _SZ, _P],
     "fdc_distill_backward": [ctypes.POINTER(DistillArgs), _P, _P, _P, _I64, _P],
     "fdc_distill_forward_backward": [ctypes.POINTER(DistillArgs), _P, _P, _P, _P, _I64, _P, _SZ, _P],
+    "fdc_rotary": [ctypes.POINTER(RotaryArgs), _P],
+    "fdc_cross_attention_workspace_size": [_I, _I, _I, _I, _I, _I, _I, _SZP, _SZP],
+    "fdc_cross_attention_forward": [ctypes.POINTER(CrossAttentionArgs), _P, _P, _SZ, _P],
+    "fdc_cross_attention_backward": [ctypes.POINTER(CrossAttentionArgs), _P, ctypes.POINTER(CrossAttentionGrads), _P,
+                                     _SZ, _P],
+    "fdc_token_logprobs_workspace_size": [_I, _I64, _I, _I, _SZP],
+    "fdc_token_logprobs_forward": [ctypes.POINTER(TokenLogprobsArgs), _P, _P, _P, _P, _P, _P, _SZ, _P],
+    "fdc_token_logprobs_backward": [ctypes.POINTER(TokenLogprobsArgs), _P, _P, _P, _P, _P, _P, _I64, _P],
 }
 _RESTYPES = {"fdc_status_string": ctypes.c_char_p, "fdc_last_error": ctypes.c_char_p, "fdc_version": _I}
 

@@ -14,6 +14,7 @@ using fdc::fail;
 namespace {
 
 constexpr int64_t kMaxTokenStride = 1LL << 25;
+constexpr int64_t kMaxHeadStride = 1LL << 30;
 constexpr int64_t kMaxElements = 1LL << 46;  // of a tensor, and of a batch stride: products stay far below 2^63
 
 fdc_status check_dtype(int dtype) {
@@ -79,6 +80,84 @@ fdc_status check_apart(const fdc_tokens &out, const char *out_name, int64_t out_
   const Sharing sh = sharing(out, out_width, in, in_width, B, L, fdc::dtype_size(dtype));
   if (sh.any && !(itself && sh.same)) return fail(FDC_EINVAL, "%s shares memory with %s", out_name, in_name);
   return FDC_OK;
+}
+
+// A [B][L][heads][D] tensor: its axes but for the channels, longest stride first.
+struct HeadAxes {
+  int64_t count[3], stride[3];
+  HeadAxes(const fdc_heads &x, int64_t B, int64_t L, int64_t heads)
+      : count{B, L, heads}, stride{x.batch_stride, x.token_stride, x.head_stride} {
+    for (int i = 0; i < 3; ++i)
+      if (count[i] == 1) stride[i] = 0;
+    for (int i = 0; i < 2; ++i)
+      for (int j = 0; j < 2 - i; ++j)
+        if (stride[j] < stride[j + 1]) std::swap(stride[j], stride[j + 1]), std::swap(count[j], count[j + 1]);
+  }
+};
+
+fdc_status check_heads(const fdc_heads &x, const char *name, int B, int L, int heads, int64_t width, bool output) {
+  if (x.p == nullptr) return fail(FDC_EINVAL, "%s is NULL", name);
+  if (x.batch_stride < 0 || x.token_stride < 0 || x.head_stride < 0)
+    return fail(FDC_EINVAL, "%s: strides must not be negative (got %lld, %lld, %lld)", name, (long long)x.batch_stride,
+                (long long)x.token_stride, (long long)x.head_stride);
+  if (x.token_stride >= kMaxTokenStride || x.head_stride >= kMaxHeadStride || x.batch_stride >= kMaxElements)
+    return fail(FDC_EUNSUPPORTED, "%s: strides %lld, %lld, %lld too large", name, (long long)x.batch_stride,
+                (long long)x.token_stride, (long long)x.head_stride);
+  if (output) {
+    const HeadAxes axes(x, B, L, heads);
+    int64_t extent = width;
+    for (int i = 2; i >= 0; --i) {
+      if (axes.count[i] == 1) continue;
+      if (axes.stride[i] < extent)
+        return fail(FDC_EINVAL, "%s is an output whose elements overlap (strides %lld, %lld, %lld)", name,
+                    (long long)x.batch_stride, (long long)x.token_stride, (long long)x.head_stride);
+      extent += (axes.count[i] - 1) * axes.stride[i];
+    }
+  }
+  return FDC_OK;
+}
+
+// Whether an output of these heads (whose elements are apart) and an input of the same strides share memory: as for
+// fdc_tokens, with one more axis, and numbers of tokens and heads of their own.
+struct HeadShape {
+  const fdc_heads &x;
+  const char *name;
+  int64_t L, heads;
+};
+fdc_status check_heads_apart(const HeadShape &out, const HeadShape &in, int64_t B, int64_t D, int dtype, bool itself) {
+  const int64_t size = (int64_t)fdc::dtype_size(dtype);
+  struct Axis {
+    int64_t outs, ins, stride;
+  } axes[3] = {{B, B, 0}, {out.L, in.L, 0}, {out.heads, in.heads, 0}};
+  const int64_t so[3] = {out.x.batch_stride, out.x.token_stride, out.x.head_stride};
+  const int64_t si[3] = {in.x.batch_stride, in.x.token_stride, in.x.head_stride};
+  bool alike = true;
+  for (int i = 0; i < 3; ++i) {
+    const int64_t stride = axes[i].outs > 1 ? so[i] : si[i];
+    if (axes[i].outs > 1 && axes[i].ins > 1 && so[i] != si[i]) alike = false;
+    axes[i].stride = axes[i].outs > 1 || axes[i].ins > 1 ? stride * size : 0;
+  }
+  bool any = out.x.p == in.x.p;
+  const bool same = any && alike && out.L == in.L && out.heads == in.heads;
+  if (same && itself) return FDC_OK;
+  if (alike && !any) {
+    for (int i = 0; i < 2; ++i)
+      for (int j = 0; j < 2 - i; ++j)
+        if (axes[j].stride < axes[j + 1].stride) std::swap(axes[j], axes[j + 1]);
+    // a step along an axis, either way, that leaves less than its stride of a distance
+    auto meets = [&](auto &&self, int i, int64_t distance) -> bool {
+      if (i == 3) return distance < D * size && -distance < D * size;
+      const Axis &x = axes[i];
+      if (x.stride == 0) return self(self, i + 1, distance);
+      const int64_t step = distance / x.stride, next = distance < 0 ? step - 1 : step + 1;
+      for (int64_t k : {step, next})
+        // element k of the input is that much further on than the output's first, or the other way round
+        if (k < x.ins && -k < x.outs && self(self, i + 1, distance - k * x.stride)) return true;
+      return false;
+    };
+    any = meets(meets, 0, (int64_t)(reinterpret_cast<uintptr_t>(out.x.p) - reinterpret_cast<uintptr_t>(in.x.p)));
+  }
+  return any ? fail(FDC_EINVAL, "%s shares memory with %s", out.name, in.name) : FDC_OK;
 }
 
 // The same of dense arrays.
@@ -201,6 +280,90 @@ fdc_status check_distill(const fdc_distill_args *a) {
   if (!(a->tau > 0.f) || !std::isfinite(a->tau)) return fail(FDC_EINVAL, "tau must be positive (got %g)", (double)a->tau);
   if (!(a->alpha >= 0.f && a->alpha <= 1.f)) return fail(FDC_EINVAL, "alpha must be in [0, 1] (got %g)", (double)a->alpha);
   if (!a->z || !a->idx || !a->teacher) return fail(FDC_EINVAL, "NULL tensor");
+  return check_row_stride(a->z_stride, a->R, a->V, "z", false);
+}
+
+// ---- rotary positions --------------------------------------------------------------
+fdc_status check_rotary(const fdc_rotary_args *a) {
+  if (a == nullptr) return fail(FDC_EINVAL, "arguments are NULL");
+  FDC_TRY(check_dtype(a->dtype));
+  FDC_TRY(check_sizes(a->B, a->L, a->D));
+  if (a->H < 1) return fail(FDC_EINVAL, "H must be positive (got %d)", a->H);
+  if (a->H > 65535) return fail(FDC_EUNSUPPORTED, "H = %d exceeds 65535", a->H);
+  if (a->D > fdc::kRotaryMaxWidth) return fail(FDC_EUNSUPPORTED, "D = %d: at most %d", a->D, fdc::kRotaryMaxWidth);
+  if (a->axes < 1 || a->axes > 4) return fail(FDC_EINVAL, "axes must be 1 to 4 (got %d)", a->axes);
+  int64_t P = 0;
+  for (int i = 0; i < a->axes; ++i) {
+    if (a->pairs[i] < 1) return fail(FDC_EINVAL, "axis %d has %d pairs", i, a->pairs[i]);
+    P += a->pairs[i];
+  }
+  if (2 * P > a->D) return fail(FDC_EINVAL, "%lld pairs of channels in heads of D = %d", (long long)P, a->D);
+  if (!a->positions || !a->freqs) return fail(FDC_EINVAL, "positions or freqs are NULL");
+  if (a->pos_batch_stride < 0 || a->pos_token_stride < 0)
+    return fail(FDC_EINVAL, "positions: strides must not be negative (got %lld, %lld)", (long long)a->pos_batch_stride,
+                (long long)a->pos_token_stride);
+  if (a->pos_batch_stride >= kMaxElements || a->pos_token_stride >= kMaxTokenStride)
+    return fail(FDC_EUNSUPPORTED, "positions: strides %lld, %lld too large", (long long)a->pos_batch_stride,
+                (long long)a->pos_token_stride);
+  // a thread at least 4 pairs or 8 other channels of a token
+  if ((int64_t)a->B * a->L * (fdc::ceil_div(P, 4) + fdc::ceil_div(a->D - 2 * P, 8)) >= (1LL << 32) - (1LL << 20))
+    return fail(FDC_EUNSUPPORTED, "B = %d times L = %d exceeds the launch limit", a->B, a->L);
+  FDC_TRY(check_heads(a->x, "x", a->B, a->L, a->H, a->D, false));
+  FDC_TRY(check_heads(a->y, "y", a->B, a->L, a->H, a->D, true));
+  return check_heads_apart({a->y, "y", a->L, a->H}, {a->x, "x", a->L, a->H}, a->B, a->D, a->dtype, true);
+}
+
+// ---- cross attention ---------------------------------------------------------------
+fdc_status check_attention_sizes(int dtype, int B, int Lq, int Lk, int H, int G, int D) {
+  FDC_TRY(check_dtype(dtype));
+  FDC_TRY(check_sizes(B, Lq, D));
+  FDC_TRY(check_sizes(B, Lk, D));
+  if (H < 1 || G < 1) return fail(FDC_EINVAL, "H and G must be positive (got %d, %d)", H, G);
+  if (H % G != 0) return fail(FDC_EINVAL, "H = %d is not a multiple of G = %d", H, G);
+  if (H > 65535) return fail(FDC_EUNSUPPORTED, "H = %d exceeds 65535", H);
+  if (D > fdc::kAttentionMaxWidth) return fail(FDC_EUNSUPPORTED, "D = %d: at most %d", D, fdc::kAttentionMaxWidth);
+  if ((int64_t)(H / G) * Lq > (1 << 30) || !fdc::cross_attention_fits(dtype, B, Lq, Lk, H, G, D))
+    return fail(FDC_EUNSUPPORTED, "B = %d, Lq = %d, Lk = %d, H = %d exceed the launch limit", B, Lq, Lk, H);
+  return FDC_OK;
+}
+
+fdc_status check_attention(const fdc_cross_attention_args *a, bool y_is_output) {
+  if (a == nullptr) return fail(FDC_EINVAL, "arguments are NULL");
+  FDC_TRY(check_attention_sizes(a->dtype, a->B, a->Lq, a->Lk, a->H, a->G, a->D));
+  if (!(a->scale > 0.f) || !std::isfinite(a->scale))
+    return fail(FDC_EINVAL, "scale must be positive (got %g)", (double)a->scale);
+  FDC_TRY(check_heads(a->q, "q", a->B, a->Lq, a->H, a->D, false));
+  FDC_TRY(check_heads(a->k, "k", a->B, a->Lk, a->G, a->D, false));
+  FDC_TRY(check_heads(a->v, "v", a->B, a->Lk, a->G, a->D, false));
+  FDC_TRY(check_heads(a->y, "y", a->B, a->Lq, a->H, a->D, y_is_output));
+  if (a->mask && a->mask_stride < 0)
+    return fail(FDC_EINVAL, "mask: stride must not be negative (got %lld)", (long long)a->mask_stride);
+  if (a->mask && a->mask_stride >= kMaxElements)
+    return fail(FDC_EUNSUPPORTED, "mask: stride %lld too large", (long long)a->mask_stride);
+  return FDC_OK;
+}
+
+// `out` against every activation that a call reads.
+fdc_status check_attention_apart(const fdc_cross_attention_args *a, const HeadShape &out) {
+  FDC_TRY(check_heads_apart(out, {a->q, "q", a->Lq, a->H}, a->B, a->D, a->dtype, false));
+  FDC_TRY(check_heads_apart(out, {a->k, "k", a->Lk, a->G}, a->B, a->D, a->dtype, false));
+  return check_heads_apart(out, {a->v, "v", a->Lk, a->G}, a->B, a->D, a->dtype, false);
+}
+
+// ---- token log probabilities -------------------------------------------------------
+fdc_status check_logprobs_sizes(int dtype, int64_t R, int V, int K) {
+  FDC_TRY(check_distill_sizes(dtype, R, V));
+  if (K < 0 || K > V) return fail(FDC_EINVAL, "K must be 0 to V = %d (got %d)", V, K);
+  if (K > fdc::kLogprobMaxTop) return fail(FDC_EUNSUPPORTED, "K = %d: at most %d", K, fdc::kLogprobMaxTop);
+  if (R * fdc::ceil_div(V, 4096) >= (1LL << 31)) return fail(FDC_EUNSUPPORTED, "R V exceeds the launch limit");
+  return FDC_OK;
+}
+
+fdc_status check_logprobs(const fdc_token_logprobs_args *a) {
+  if (a == nullptr) return fail(FDC_EINVAL, "arguments are NULL");
+  FDC_TRY(check_logprobs_sizes(a->dtype, a->R, a->V, a->K));
+  if (!(a->tau > 0.f) || !std::isfinite(a->tau)) return fail(FDC_EINVAL, "tau must be positive (got %g)", (double)a->tau);
+  if (!a->z) return fail(FDC_EINVAL, "z is NULL");
   return check_row_stride(a->z_stride, a->R, a->V, "z", false);
 }
 
@@ -379,4 +542,88 @@ fdc_status fdc_distill_forward_backward(const fdc_distill_args *a, const float *
   FDC_TRY(check_ws(ws, ws_bytes, fdc::distill_ws_floats(a->dtype, a->R, a->V) * sizeof(float), "distillation"));
   return check_hip(fdc::launch_distill(*a, loss, stats, gloss, gz, gz_stride, static_cast<float *>(ws), s),
                    "distillation");
+}
+
+// ---------------------------------------------------------------------------
+// rotary positions
+// ---------------------------------------------------------------------------
+fdc_status fdc_rotary(const fdc_rotary_args *a, hipStream_t s) {
+  FDC_TRY(check_rotary(a));
+  return check_hip(fdc::launch_rotary(*a, s), "rotary positions");
+}
+
+// ---------------------------------------------------------------------------
+// cross attention
+// ---------------------------------------------------------------------------
+fdc_status fdc_cross_attention_workspace_size(int dtype, int B, int Lq, int Lk, int H, int G, int D, size_t *fwd_ws,
+                                              size_t *bwd_ws) {
+  FDC_TRY(check_attention_sizes(dtype, B, Lq, Lk, H, G, D));
+  if (fwd_ws) *fwd_ws = fdc::cross_attention_fwd_ws(dtype, B, Lq, Lk, H, G, D);
+  if (bwd_ws) *bwd_ws = fdc::cross_attention_bwd_ws(dtype, B, Lq, Lk, H, G, D);
+  return FDC_OK;
+}
+
+fdc_status fdc_cross_attention_forward(const fdc_cross_attention_args *a, float *lse, void *ws, size_t ws_bytes,
+                                       hipStream_t s) {
+  FDC_TRY(check_attention(a, true));
+  FDC_TRY(check_attention_apart(a, {a->y, "y", a->Lq, a->H}));
+  FDC_TRY(check_ws(ws, ws_bytes, fdc::cross_attention_fwd_ws(a->dtype, a->B, a->Lq, a->Lk, a->H, a->G, a->D),
+                   "cross attention forward"));
+  return check_hip(fdc::launch_cross_attention_fwd(*a, lse, static_cast<float *>(ws), s), "cross attention");
+}
+
+fdc_status fdc_cross_attention_backward(const fdc_cross_attention_args *a, const float *lse,
+                                        const fdc_cross_attention_grads *g, void *ws, size_t ws_bytes, hipStream_t s) {
+  FDC_TRY(check_attention(a, false));
+  if (!lse || !g) return fail(FDC_EINVAL, "lse or gradients are NULL");
+  FDC_TRY(check_heads(g->gy, "gy", a->B, a->Lq, a->H, a->D, false));
+  FDC_TRY(check_heads(g->gq, "gq", a->B, a->Lq, a->H, a->D, true));
+  FDC_TRY(check_heads(g->gk, "gk", a->B, a->Lk, a->G, a->D, true));
+  FDC_TRY(check_heads(g->gv, "gv", a->B, a->Lk, a->G, a->D, true));
+  const HeadShape outs[3] = {{g->gq, "gq", a->Lq, a->H}, {g->gk, "gk", a->Lk, a->G}, {g->gv, "gv", a->Lk, a->G}};
+  for (int i = 0; i < 3; ++i) {
+    FDC_TRY(check_attention_apart(a, outs[i]));
+    FDC_TRY(check_heads_apart(outs[i], {a->y, "y", a->Lq, a->H}, a->B, a->D, a->dtype, false));
+    FDC_TRY(check_heads_apart(outs[i], {g->gy, "gy", a->Lq, a->H}, a->B, a->D, a->dtype, false));
+    for (int j = 0; j < i; ++j) FDC_TRY(check_heads_apart(outs[i], outs[j], a->B, a->D, a->dtype, false));
+  }
+  FDC_TRY(check_ws(ws, ws_bytes, fdc::cross_attention_bwd_ws(a->dtype, a->B, a->Lq, a->Lk, a->H, a->G, a->D),
+                   "cross attention backward"));
+  return check_hip(fdc::launch_cross_attention_bwd(*a, lse, *g, static_cast<float *>(ws), s), "cross attention backward");
+}
+
+// ---------------------------------------------------------------------------
+// token log probabilities
+// ---------------------------------------------------------------------------
+fdc_status fdc_token_logprobs_workspace_size(int dtype, int64_t R, int V, int K, size_t *bytes) {
+  FDC_TRY(check_logprobs_sizes(dtype, R, V, K));
+  if (!bytes) return fail(FDC_EINVAL, "bytes is NULL");
+  *bytes = fdc::token_logprobs_ws(dtype, R, V, K);
+  return FDC_OK;
+}
+
+fdc_status fdc_token_logprobs_forward(const fdc_token_logprobs_args *a, float *logp, float *entropy, int32_t *idx,
+                                      float *top, float *stats, void *ws, size_t ws_bytes, hipStream_t s) {
+  FDC_TRY(check_logprobs(a));
+  if ((logp != nullptr) != (a->tokens != nullptr)) return fail(FDC_EINVAL, "logp goes with tokens");
+  if ((a->K > 0) != (idx != nullptr) || (a->K > 0) != (top != nullptr))
+    return fail(FDC_EINVAL, "idx and top go with K > 0");
+  if (!logp && !entropy && !idx && !stats) return fail(FDC_EINVAL, "nothing is wanted");
+  FDC_TRY(check_ws(ws, ws_bytes, fdc::token_logprobs_ws(a->dtype, a->R, a->V, a->K), "token log probabilities"));
+  return check_hip(fdc::launch_token_logprobs(*a, logp, entropy, idx, top, stats, ws, s), "token log probabilities");
+}
+
+fdc_status fdc_token_logprobs_backward(const fdc_token_logprobs_args *a, const float *stats, const float *glogp,
+                                       const float *gentropy, const int32_t *idx, const float *gtop, void *gz,
+                                       int64_t gz_stride, hipStream_t s) {
+  FDC_TRY(check_logprobs(a));
+  if (!stats || !gz) return fail(FDC_EINVAL, "stats or gz is NULL");
+  if (!glogp && !gentropy && !gtop) return fail(FDC_EINVAL, "no gradient is given");
+  if (glogp && !a->tokens) return fail(FDC_EINVAL, "glogp without tokens");
+  if (gtop && (!idx || a->K == 0)) return fail(FDC_EINVAL, "gtop without idx or K");
+  FDC_TRY(check_row_stride(gz_stride, a->R, a->V, "gz", true));
+  FDC_TRY(check_apart({gz, gz_stride, 0}, "gz", a->V, {const_cast<void *>(a->z), a->z_stride, 0}, "z", a->V, a->R, 1,
+                      a->dtype, true));
+  return check_hip(fdc::launch_token_logprobs_bwd(*a, stats, glogp, gentropy, idx, gtop, gz, gz_stride, s),
+                   "token log probabilities backward");
 }

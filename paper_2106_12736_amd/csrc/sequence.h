@@ -1,5 +1,5 @@
 // Internal interface of the sequence operators (causal_conv.hip, scan.hip, block_norm.hip,
-// distill.hip, seq_reduce.hip) and the device helpers they share.
+// distill.hip, rotary.hip, cross_attention.hip, token_logprobs.hip, seq_reduce.hip) and the device helpers they share.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -21,6 +21,10 @@ constexpr int kScanBlock = 16;  // tokens between two saved states
 constexpr int kNormMaxWidth = 8192;
 constexpr int kDistillMaxTeacher = 1024;
 constexpr int kDistillStats = 5;  // floats a row that the forward keeps for the backward
+constexpr int kRotaryMaxWidth = 1024;
+constexpr int kAttentionMaxWidth = 128;
+constexpr int kLogprobMaxTop = 128;
+constexpr int kLogprobStats = 3;
 
 hipError_t launch_causal_conv_fwd(const fdc_causal_conv_args &a, hipStream_t s);
 size_t causal_conv_bwd_ws(int dtype, int B, int L, int D, int n);  // bytes
@@ -47,6 +51,22 @@ hipError_t launch_distill(const fdc_distill_args &a, float *loss, float *stats, 
                           int64_t gz_stride, float *ws, hipStream_t s);
 hipError_t launch_distill_bwd(const fdc_distill_args &a, const float *stats, const float *gloss, void *gz,
                               int64_t gz_stride, hipStream_t s);
+
+hipError_t launch_rotary(const fdc_rotary_args &a, hipStream_t s);
+
+bool cross_attention_fits(int dtype, int B, int Lq, int Lk, int H, int G, int D);
+size_t cross_attention_fwd_ws(int dtype, int B, int Lq, int Lk, int H, int G, int D);  // bytes
+size_t cross_attention_bwd_ws(int dtype, int B, int Lq, int Lk, int H, int G, int D);
+hipError_t launch_cross_attention_fwd(const fdc_cross_attention_args &a, float *lse, float *ws, hipStream_t s);
+hipError_t launch_cross_attention_bwd(const fdc_cross_attention_args &a, const float *lse,
+                                      const fdc_cross_attention_grads &g, float *ws, hipStream_t s);
+
+size_t token_logprobs_ws(int dtype, int64_t R, int V, int K);  // bytes
+hipError_t launch_token_logprobs(const fdc_token_logprobs_args &a, float *logp, float *entropy, int32_t *idx, float *top,
+                                 float *stats, void *ws, hipStream_t s);
+hipError_t launch_token_logprobs_bwd(const fdc_token_logprobs_args &a, const float *stats, const float *glogp,
+                                     const float *gentropy, const int32_t *idx, const float *gtop, void *gz,
+                                     int64_t gz_stride, hipStream_t s);
 
 // Sums over the rows of part [rows][cols] in row order, in segments of columns: column c of
 // segment i goes to out[i][(c % inner[i]) * mult[i] + c / inner[i]] (out NULL: dropped).

@@ -1,0 +1,544 @@
+// Log probabilities of given tokens, entropy and top alternatives of rows of logits, and their gradient.
+//
+//   with d = (z - m) / tau, m the row's largest logit, s = sum exp(d), u = sum exp(d) d:
+//   l[v] = d[v] - log s,   entropy = log s - u / s  (two terms that are not negative: nothing cancels)
+//   gz[v] = 1/tau ([v = token] glogp + sum_k [v = idx_k] gtop_k - p[v] (glogp + sum gtop) - gentropy p[v] (l[v] + entropy))
+//
+// The forward is a pass over z (HBM-bound): a workgroup holds a row, or a segment of one, in its registers as the 16-byte
+// pieces it loaded.  The K best of them: every thread's largest logit is known from the maximum, and the K-th
+// largest of these is a lower bound of the row's K-th (K threads have one that large), below which all but a few more than
+// K logits lie; those above go to LDS, where each finds its place by counting the ones before it.  Rows where
+// too many lie above (many equal logits) raise the bound by bisection until few enough do; equal logits are told
+// apart by their places.
+//
+// Many rows: a workgroup each; few rows or rows that do not fit: segments, joined by a workgroup a row.
+#include <algorithm>
+
+#include "sequence.h"
+
+namespace fdc {
+
+namespace {
+
+constexpr int kMost = 512;  // candidates in LDS
+constexpr float kLowest = -3.402823466e38f;
+
+template <class T>
+constexpr int kLogitV = 16 / (int)sizeof(T);
+
+// Keys of the same order as the logits, -0 as 0, NaN above all.
+__device__ __forceinline__ uint32_t key_of(float x) {
+  if (x != x) return 0xffffffffu;
+  const uint32_t b = __float_as_uint(x + 0.f);
+  return b ^ (b >> 31 ? 0xffffffffu : 0x80000000u);
+}
+__device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k ^ (k >> 31 ? 0x80000000u : 0xffffffffu)); }
+constexpr uint32_t kInfKey = 0xff800000u;
+// A logit and its place: larger logits first, then lower places.  0 stands for none.
+__device__ __forceinline__ uint64_t pair_of(uint32_t key, int place) { return (uint64_t)key << 32 | ~(uint32_t)place; }
+__device__ __forceinline__ int place_of(uint64_t pair) { return (int)~(uint32_t)pair; }
+
+struct Sums {
+  float m, s, u;
+};
+// u is in units of z: sum exp(d) (z - m).
+__device__ __forceinline__ void add(Sums &a, const Sums &b, float c) {
+  if (b.s == 0.f) return;  // nothing but -inf: (m - M) 0 would be NaN
+  if (a.s == 0.f) {
+    a = b;
+    return;
+  }
+  const float m = fmaxf(a.m, b.m);
+  const float fa = a.m == m ? 1.f : exp2_fast((a.m - m) * c), fb = b.m == m ? 1.f : exp2_fast((b.m - m) * c);
+  a.u = fa * (a.u + (a.m == m ? 0.f : a.s * (a.m - m))) + fb * (b.u + (b.m == m ? 0.f : b.s * (b.m - m)));
+  a.s = a.s * fa + b.s * fb;
+  a.m = m;
+}
+
+template <int TH>
+struct TopScratch {
+  uint32_t maxima[TH];
+  uint64_t found[kMost];
+  int count;
+  uint32_t bound;
+  int red[2][TH / 64];
+};
+
+// By one wave: a key that at least K of the maxima are not below, few of them if there is one (0: all).
+template <int TH>
+__device__ __forceinline__ uint32_t bound_of(const uint32_t *maxima, int K, int lane) {
+  constexpr int N = TH / 64;
+  if (K > TH) return 0;
+  uint32_t mine[N], bound = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) mine[i] = maxima[i * 64 + lane];
+  for (int bit = 31; bit >= 0; --bit) {
+    const uint32_t tried = bound | 1u << bit;
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) n += __popcll(__ballot(mine[i] >= tried));
+    if (n < K) continue;
+    bound = tried;
+    if (n <= K + K / 8) break;
+  }
+  return bound;
+}
+
+// The sum of n over the workgroup; `turn` counts the calls (two sets of partial sums in turn: one barrier each).
+template <int TH>
+__device__ __forceinline__ int count_all(TopScratch<TH> &t, int n, int turn) {
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) n += __shfl_xor(n, off, 64);
+  if ((threadIdx.x & 63) == 0) t.red[turn & 1][threadIdx.x >> 6] = n;
+  __syncthreads();
+  int sum = 0;
+#pragma unroll
+  for (int i = 0; i < TH / 64; ++i) sum += t.red[turn & 1][i];
+  return sum;
+}
+
+// Fills t.found with the candidates (at most kMost, the K best among them) and returns how many they are; t.bound and
+// t.count (0) have been written before a barrier.  each(f) calls f(logit, place) for the thread's logits, `largest` is the
+// largest of them, `best` that of the row, odd: the row has NaN.
+template <int TH, class Each>
+__device__ __forceinline__ int find_top(TopScratch<TH> &t, int K, float largest, float best, bool odd, Each &&each) {
+  uint32_t bound = t.bound;
+  if (odd || key_of(largest) >= bound)
+    each([&](float x, int place) {
+      const uint32_t key = key_of(x);
+      if (key >= bound) {
+        const int at = atomicAdd(&t.count, 1);
+        if (at < kMost) t.found[at] = pair_of(key, place);
+      }
+    });
+  __syncthreads();
+  int n = t.count;
+  if (n <= kMost) return n;
+  // bisection: K or more logits are not below lo, fewer than K not below hi
+  uint64_t lo = bound, hi = odd ? 1ull << 32 : (uint64_t)key_of(best) + 1;
+  int turn = 0;
+  while (hi - lo > 1 && n > kMost) {
+    const uint32_t mid = (uint32_t)((lo + hi) / 2);
+    const float f = of_key(mid);
+    int c = 0;
+    if (mid > kInfKey)
+      each([&](float x, int) { c += x != x; });
+    else
+      each([&](float x, int) { c += !(x < f); });
+    c = count_all(t, c, turn++);
+    if (c >= K)
+      lo = mid, n = c;
+    else
+      hi = mid;
+  }
+  // too many equal ones: the places up to `last` are enough
+  uint32_t last = 0xffffffffu;
+  if (n > kMost) {
+    const uint32_t key = (uint32_t)lo;
+    uint32_t none = 0;  // the places below `none` are too few
+    last = 1u << 24;
+    while (last > none && n > kMost) {
+      const uint32_t mid = (none + last) / 2;
+      int c = 0;
+      each([&](float x, int place) {
+        const uint32_t k = key_of(x);
+        c += k > key || (k == key && (uint32_t)place <= mid);
+      });
+      c = count_all(t, c, turn++);
+      if (c >= K)
+        last = mid, n = c;
+      else
+        none = mid + 1;
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) t.count = 0;
+  __syncthreads();
+  each([&](float x, int place) {
+    const uint32_t key = key_of(x);
+    if (key > lo || (key == lo && (uint32_t)place <= last)) {
+      const int at = atomicAdd(&t.count, 1);
+      if (at < kMost) t.found[at] = pair_of(key, place);
+    }
+  });
+  __syncthreads();
+  return min(t.count, kMost);
+}
+
+// put(rank, pair) for the K best of the n candidates, each from one thread.
+template <int TH, class Put>
+__device__ __forceinline__ void rank_top(const TopScratch<TH> &t, int n, int K, Put &&put) {
+  for (int i = threadIdx.x; i < n; i += TH) {
+    const uint64_t mine = t.found[i];
+    int rank = 0;
+    for (int j = 0; j < n; ++j) rank += t.found[j] > mine;
+    if (rank < K) put(rank, mine);
+  }
+}
+
+struct Result {
+  float m, s, log_s, per;  // per: 1 / tau
+  __device__ __forceinline__ Result(const Sums &x, float tau) {
+    m = x.m, s = x.s, log_s = __builtin_amdgcn_logf(x.s) * kLn2, per = 1.f / tau;
+  }
+  __device__ __forceinline__ float logp(float z) const { return (z - m) * per - log_s; }
+};
+
+// By one thread: what a row's sums say, but for its alternatives.
+template <class T>
+__device__ __forceinline__ void row_result(const fdc_token_logprobs_args &a, int64_t row, const Sums &x, float *logp,
+                                           float *entropy, float *stats) {
+  const Result r(x, a.tau);
+  const float h = r.log_s - x.u / x.s * r.per;
+  if (logp != nullptr) {
+    const int v = a.tokens[row];
+    logp[row] = v < 0 ? 0.f : v >= a.V ? NAN : r.logp((float)static_cast<const T *>(a.z)[row * a.z_stride + v]);
+  }
+  if (entropy != nullptr) entropy[row] = h;
+  if (stats != nullptr) {
+    float *p = stats + kLogprobStats * row;
+    p[0] = x.m, p[1] = x.s, p[2] = h;
+  }
+}
+
+// What a call writes.
+struct Out {
+  float *logp, *entropy;
+  int32_t *idx;
+  float *top, *stats;
+  float4 *part;     // [R][segments]: m, s, u of a segment
+  uint64_t *pairs;  // [R][segments][K]
+};
+
+// A workgroup a segment (of `seg` logits, `segs` a row).
+template <class T, int TH, int NV, bool Top>
+__global__ __launch_bounds__(TH) void k_logprobs(fdc_token_logprobs_args a, Out out, int seg, int segs) {
+  constexpr int V = kLogitV<T>, W = TH / 64;
+  __shared__ float rmax[W], rs[W], ru[W];
+  __shared__ std::conditional_t<Top, TopScratch<TH>, int> scratch;
+  const int64_t id = (int64_t)blockIdx.y * 32768 + blockIdx.x;
+  const int64_t row = id / segs;
+  if (row >= a.R) return;
+  const int part = (int)(id - row * segs), begin = part * seg, count = min(a.V - begin, seg);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const float c = kLog2e / a.tau;
+  const T *z = static_cast<const T *>(a.z) + row * a.z_stride + begin;
+  Pack<T, V> x[NV];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int at = (k * TH + tid) * V, n = count - at;
+    if (n > 0) {
+      x[k] = load_some<T, V>(z + at, n, -INFINITY);
+    } else {
+      const unsigned none = element_bits<T>((T)-INFINITY);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[k].w[i] = sizeof(T) == 4 ? none : none | none << 16;
+    }
+  }
+  float mine = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+#pragma unroll
+    for (int i = 0; i < V; ++i) mine = fmaxf(mine, x[k].at(i));
+  const float wave_best = wave_max(mine);
+  if (lane == 0) rmax[wave] = wave_best;
+  if constexpr (Top) {
+    scratch.maxima[tid] = key_of(mine);
+    if (tid == 0) scratch.count = 0;
+  }
+  __syncthreads();
+  Sums t{-INFINITY, 0.f, 0.f};
+#pragma unroll
+  for (int w = 0; w < W; ++w) t.m = fmaxf(t.m, rmax[w]);
+  if constexpr (Top) {
+    if (wave == W - 1) {
+      const uint32_t b = bound_of<TH>(scratch.maxima, a.K, lane);
+      if (lane == 0) scratch.bound = b;
+    }
+  }
+  // of -inf alone (or with NaN): each term is 0 (or NaN)
+  const float base = t.m == -INFINITY ? 0.f : t.m;
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const float d = x[k].at(i) - base, e = exp2_fast(d * c);
+      t.s += e;
+      t.u = fmaf(e, fmaxf(d, kLowest), t.u);  // a place of -inf: 0 times a number
+    }
+  t.s = wave_sum(t.s);
+  t.u = wave_sum(t.u);
+  if (lane == 0) rs[wave] = t.s, ru[wave] = t.u;
+  __syncthreads();
+  t.s = t.u = 0.f;
+#pragma unroll
+  for (int w = 0; w < W; ++w) t.s += rs[w], t.u += ru[w];
+  if (tid == 0) {
+    if (segs == 1)
+      row_result<T>(a, row, t, out.logp, out.entropy, out.stats);
+    else
+      out.part[id] = {t.m, t.s, t.u, 0.f};
+  }
+  if constexpr (Top) {
+    const int n = find_top<TH>(scratch, a.K, mine, t.m, t.s != t.s, [&](auto &&f) {
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        const int at = (k * TH + tid) * V;
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+          if (at + i < count) f(x[k].at(i), begin + at + i);
+      }
+    });
+    if (segs == 1) {
+      const Result r(t, a.tau);
+      rank_top<TH>(scratch, n, a.K, [&](int rank, uint64_t pair) {
+        out.idx[row * a.K + rank] = place_of(pair);
+        out.top[row * a.K + rank] = r.logp(of_key((uint32_t)(pair >> 32)));
+      });
+    } else {
+      uint64_t *to = out.pairs + id * a.K;
+      rank_top<TH>(scratch, n, a.K, [&](int rank, uint64_t pair) { to[rank] = pair; });
+      for (int k = n + tid; k < a.K; k += TH) to[k] = 0;  // a segment of less than K
+    }
+  }
+}
+
+// A workgroup a row: its segments' sums in order, and the best of their K best.
+template <class T>
+__global__ __launch_bounds__(256) void k_logprobs_join(fdc_token_logprobs_args a, Out out, int segs) {
+  __shared__ TopScratch<256> t;
+  __shared__ Sums all;
+  const int64_t row = (int64_t)blockIdx.y * 32768 + blockIdx.x;
+  if (row >= a.R) return;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const float c = kLog2e / a.tau;
+  const uint64_t *pairs = out.pairs + row * segs * a.K;
+  const int total = segs * a.K;
+  uint64_t mine = 0;
+  for (int i = tid; i < total; i += 256) mine = max(mine, pairs[i]);
+  t.maxima[tid] = (uint32_t)(mine >> 32);
+  if (tid == 0) t.count = 0;
+  __syncthreads();
+  if (tid >= 192) {
+    const uint32_t b = a.K > 0 ? bound_of<256>(t.maxima, a.K, lane) : 0;
+    if (lane == 0) t.bound = b;
+  }
+  if (tid < 64) {
+    Sums x{-INFINITY, 0.f, 0.f};
+    for (int i = lane; i < segs; i += 64) {
+      const float4 p = out.part[row * segs + i];
+      add(x, Sums{p.x, p.y, p.z}, c);
+    }
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      // the lower lane's first, in both: the same sum in the same order
+      const Sums y{__shfl_xor(x.m, off, 64), __shfl_xor(x.s, off, 64), __shfl_xor(x.u, off, 64)};
+      Sums lower = lane & off ? y : x;
+      add(lower, lane & off ? x : y, c);
+      x = lower;
+    }
+    if (lane == 0) {
+      all = x;
+      row_result<T>(a, row, x, out.logp, out.entropy, out.stats);
+    }
+  }
+  __syncthreads();
+  if (a.K == 0) return;
+  const uint64_t bound = (uint64_t)t.bound << 32;
+  for (int i = tid; i < total; i += 256) {
+    const uint64_t p = pairs[i];
+    if (p >= bound && p != 0) {
+      const int at = atomicAdd(&t.count, 1);
+      if (at < kMost) t.found[at] = p;
+    }
+  }
+  __syncthreads();
+  int n = t.count;
+  if (n > kMost) {  // many equal logits: pairs differ all the same
+    uint64_t lo = bound, hi = ~0ull;
+    int turn = 0;
+    while (n > kMost) {
+      const uint64_t mid = lo + (hi - lo) / 2;
+      int k = 0;
+      for (int i = tid; i < total; i += 256) k += pairs[i] >= mid && pairs[i] != 0;
+      k = count_all(t, k, turn++);
+      if (k >= a.K)
+        lo = mid, n = k;
+      else
+        hi = mid;
+    }
+    __syncthreads();
+    if (tid == 0) t.count = 0;
+    __syncthreads();
+    for (int i = tid; i < total; i += 256) {
+      const uint64_t p = pairs[i];
+      if (p >= lo && p != 0) {
+        const int at = atomicAdd(&t.count, 1);
+        if (at < kMost) t.found[at] = p;
+      }
+    }
+    __syncthreads();
+    n = min(t.count, kMost);
+  }
+  const Result r(all, a.tau);
+  rank_top<256>(t, n, a.K, [&](int rank, uint64_t pair) {
+    out.idx[row * a.K + rank] = place_of(pair);
+    out.top[row * a.K + rank] = r.logp(of_key((uint32_t)(pair >> 32)));
+  });
+}
+
+// ---- gradient ------------------------------------------------------------------
+constexpr int kGradThreads = 256;
+
+// Segment blockIdx.x of a row of the gradient.  z and gz may be the same memory: a thread reads the logits it
+// writes the gradients of, and the named places' are read before.
+template <class T>
+__global__ __launch_bounds__(kGradThreads) void k_logprobs_grad(fdc_token_logprobs_args a, const float *__restrict__ stats,
+                                                                const float *__restrict__ glogp,
+                                                                const float *__restrict__ gentropy,
+                                                                const int32_t *__restrict__ idx,
+                                                                const float *__restrict__ gtop, void *gz_,
+                                                                int64_t gz_stride, int seg) {
+  constexpr int V = kLogitV<T>;
+  __shared__ int place[kLogprobMaxTop + 1];
+  __shared__ float target[kLogprobMaxTop + 1], logit[kLogprobMaxTop + 1];
+  const int64_t row = (int64_t)blockIdx.y + (int64_t)blockIdx.z * 32768;
+  if (row >= a.R) return;
+  const int tid = threadIdx.x, K = gtop != nullptr ? a.K : 0;
+  const T *z = static_cast<const T *>(a.z) + row * a.z_stride;
+  T *gz = static_cast<T *>(gz_) + row * gz_stride;
+  // entry 0 is the token
+  for (int k = tid; k <= K; k += kGradThreads) {
+    const int v = k == 0 ? (glogp != nullptr ? a.tokens[row] : -1) : idx[row * a.K + k - 1];
+    place[k] = v;
+    target[k] = v < 0 ? 0.f : k == 0 ? glogp[row] : gtop[row * a.K + k - 1];
+    logit[k] = v >= 0 && v < a.V ? (float)z[v] : 0.f;
+  }
+  __syncthreads();
+  float alike = 0.f;
+  bool any = false, over = false;
+  for (int k = 0; k <= K; ++k) {
+    alike += target[k];
+    any = any || target[k] != 0.f;
+    over = over || place[k] >= a.V;
+  }
+  const float gh = gentropy != nullptr ? gentropy[row] : 0.f;
+  const int begin = blockIdx.x * seg, end = min(a.V, begin + seg);
+  if (!any && gh == 0.f) {
+    const float o[V] = {};
+    for (int at = begin + tid * V; at < end; at += kGradThreads * V) store_some<T, V>(gz + at, o, min(V, end - at));
+    return;
+  }
+  const float *p = stats + kLogprobStats * row;
+  const float per = 1.f / a.tau, c = kLog2e / a.tau, m = p[0], f = over ? NAN : per / p[1];
+  // p (l + entropy) with l = (z - m) / tau - log s
+  const float shift = p[2] - __builtin_amdgcn_logf(p[1]) * kLn2;
+  const float c0 = fmaf(gh, shift, alike), c1 = gh * per;
+  auto grad = [&](float x) {
+    const float d = x - m;
+    return -f * exp2_fast(d * c) * fmaf(c1, fmaxf(d, kLowest), c0);
+  };
+  for (int at = begin + tid * V; at < end; at += kGradThreads * V) {
+    const int n = min(V, end - at);
+    const Pack<T, V> x = load_some<T, V>(z + at, n);
+    float o[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) o[i] = grad(x.at(i));
+    store_some<T, V>(gz + at, o, n);
+  }
+  __syncthreads();
+  // the named places: the first entry of a place adds all of its targets
+  for (int k = tid; k <= K; k += kGradThreads) {
+    const int v = place[k];
+    if (v < begin || v >= end) continue;
+    float sum = 0.f;
+    bool first = true;
+    for (int j = 0; j <= K; ++j) {
+      const bool same = place[j] == v;
+      sum += same ? target[j] : 0.f;
+      first = first && !(same && j < k);
+    }
+    if (first) gz[v] = (T)(fmaf(sum, per, grad(logit[k])));
+  }
+}
+
+// ---- host ----------------------------------------------------------------------
+struct Segments {
+  int seg, segs;
+};
+// A row a workgroup where it fits the registers (16 pieces of 16 bytes in 512 threads, 8 where segments are cut) and
+// there are rows for every compute unit; else segments, of 1024 pieces at least.
+Segments segments(int dtype, int64_t R, int V) {
+  const int piece = 16 / (int)dtype_size(dtype);
+  const long long pieces = ceil_div(V, piece);
+  long long segs = 1;
+  if (pieces > 512 * 16) segs = ceil_div(pieces, 512 * 8);
+  while (R * segs < 512 && ceil_div(pieces, segs) > 1024) ++segs;
+  Segments s;
+  s.seg = (int)ceil_div(ceil_div(V, segs), piece) * piece;
+  s.segs = (int)ceil_div(V, s.seg);
+  return s;
+}
+Segments grad_segments(int dtype, int64_t R, int V) {
+  const int unit = kGradThreads * 16 / (int)dtype_size(dtype);
+  long long per = ceil_div(V, unit);
+  while (per > 1 && R * ceil_div(V, per * unit) < 2048) per = ceil_div(per, 2);
+  Segments s;
+  s.seg = (int)(per * unit);
+  s.segs = (int)ceil_div(V, s.seg);
+  return s;
+}
+dim3 wide_grid(long long n) { return dim3((unsigned)std::min<long long>(n, 32768), (unsigned)ceil_div(n, 32768)); }
+
+// f(threads, pieces a thread) for segments of `vecs` 16-byte pieces (at most 512 * 16).
+template <class F>
+hipError_t by_pieces(long long vecs, F &&f) {
+  using std::integral_constant;
+#define FDC_ROW(TH, NV) \
+  if (vecs <= TH * NV) return f(integral_constant<int, TH>{}, integral_constant<int, NV>{});
+  FDC_ROW(64, 1)
+  FDC_ROW(128, 2)
+  FDC_ROW(256, 4)
+  FDC_ROW(512, 4)
+  FDC_ROW(512, 8)
+#undef FDC_ROW
+  return f(integral_constant<int, 512>{}, integral_constant<int, 16>{});
+}
+
+}  // namespace
+
+size_t token_logprobs_ws(int dtype, int64_t R, int V, int K) {
+  const Segments sg = segments(dtype, R, V);
+  return sg.segs == 1 ? 0 : (size_t)R * sg.segs * (sizeof(float4) + K * sizeof(uint64_t));
+}
+
+hipError_t launch_token_logprobs(const fdc_token_logprobs_args &a, float *logp, float *entropy, int32_t *idx, float *top,
+                                 float *stats, void *ws, hipStream_t s) {
+  const Segments sg = segments(a.dtype, a.R, a.V);
+  float4 *part = static_cast<float4 *>(ws);
+  const Out out{logp, entropy, idx, top, stats, part, reinterpret_cast<uint64_t *>(part + a.R * sg.segs)};
+  return by_dtype(a.dtype, [&](auto tag) {
+    using T = decltype(tag);
+    if (hipError_t e = by_pieces(ceil_div(sg.seg, kLogitV<T>), [&](auto threads, auto pieces) {
+          constexpr int TH = decltype(threads)::value, NV = decltype(pieces)::value;
+          return timed_launch("logprobs", a.K > 0 ? k_logprobs<T, TH, NV, true> : k_logprobs<T, TH, NV, false>,
+                              wide_grid(a.R * sg.segs), dim3(TH), 0, s, a, out, sg.seg, sg.segs);
+        }))
+      return e;
+    if (sg.segs == 1) return hipSuccess;
+    return timed_launch("logprobs_join", k_logprobs_join<T>, wide_grid(a.R), dim3(256), 0, s, a, out, sg.segs);
+  });
+}
+
+hipError_t launch_token_logprobs_bwd(const fdc_token_logprobs_args &a, const float *stats, const float *glogp,
+                                     const float *gentropy, const int32_t *idx, const float *gtop, void *gz,
+                                     int64_t gz_stride, hipStream_t s) {
+  const Segments sg = grad_segments(a.dtype, a.R, a.V);
+  const dim3 grid((unsigned)sg.segs, (unsigned)std::min<int64_t>(a.R, 32768), (unsigned)ceil_div(a.R, 32768));
+  return by_dtype(a.dtype, [&](auto tag) {
+    return timed_launch("logprobs_grad", k_logprobs_grad<decltype(tag)>, grid, dim3(kGradThreads), 0, s, a, stats, glogp,
+                        gentropy, idx, gtop, gz, gz_stride, sg.seg);
+  });
+}
+
+}  // namespace fdc

@@ -6,8 +6,14 @@ the loss it is trained with, on tokens of D channels.
   block_norm_*    norm of a block's output, gate, residual scale, and the norm before the next block
   distill_*       loss against a teacher's top logits and labels
 
-Activations are float32, bfloat16 or float16, of shape [B, L, D] (or [B, D] for one token) with any
-strides whose last dimension is dense; parameters, states and losses are float32 and contiguous.
+and what it reads an image's tokens and scores its answers with:
+
+  rotary_*            rotary positions of several axes
+  cross_attention_*   attention to states of another length
+  token_logprobs_*    log probabilities of given tokens, entropy, top alternatives
+
+Activations are float32, bfloat16 or float16, of shape [B, L, D] (or [B, D] for one token; [B, L, H, D] or [B, H, D]
+where they have heads) with any strides whose last dimension is dense; parameters, states and losses are float32 and contiguous.
 Every call runs on the current stream of the current device, which the tensors have to be on, and
 allocates its outputs and workspace there; an output that is given is other memory than the inputs
 unless a function says that it may be the same.  include/fdc.h defines each operation.
@@ -20,7 +26,8 @@ from functools import lru_cache
 import torch
 
 from . import _lib
-from ._lib import ConvArgs, DistillArgs, NormArgs, NormGrads, ScanArgs, Tokens, call
+from ._lib import (ConvArgs, CrossAttentionArgs, CrossAttentionGrads, DistillArgs, Heads, NormArgs, NormGrads,
+                   RotaryArgs, ScanArgs, TokenLogprobsArgs, Tokens, call)
 from .layers import _ptr, _stream
 
 _DTYPES = {torch.float32: _lib.DTYPE_F32, torch.bfloat16: _lib.DTYPE_BF16, torch.float16: _lib.DTYPE_F16}
@@ -29,6 +36,8 @@ _ABSENT = Tokens(None, 0, 0)
 
 ScanGradients = namedtuple("ScanGradients", "x dt A B C skip gate dt_bias")
 NormGradients = namedtuple("NormGradients", "x f gate scale w_post w_pre")
+AttentionGradients = namedtuple("AttentionGradients", "q k v")
+TokenLogprobs = namedtuple("TokenLogprobs", "logp entropy idx top stats")
 
 
 # Calls on single tokens are bound by this file's own work, so a tensor that passes its check costs one
@@ -75,6 +84,12 @@ def _tokens_groups(t, ref, shape, name):
     if s[-2] != shape[-1] and shape[-2] > 1:
         raise ValueError(f"{name}'s groups must be dense")
     return Tokens(t.data_ptr(), s[0], s[1] if len(s) > 3 else 0)
+
+
+def _heads(t, ref, shape, name):
+    """[B, L, heads, D], or [B, heads, D] of one token."""
+    s = _strides(t, ref, shape, name)
+    return Heads(t.data_ptr(), s[0], s[1], s[2]) if len(s) == 4 else Heads(t.data_ptr(), s[0], 0, s[1])
 
 
 def _rows(t, ref, shape, name):
@@ -343,3 +358,152 @@ def distill_forward_backward(gloss, z, idx, teacher, temperature=1.0, labels=Non
     call("fdc_distill_forward_backward", a, _f32(gloss, z, (a.R,), "gloss"), _ptr(loss), _ptr(stats), gp, gs, ws,
          size, _stream())
     return loss, gz
+
+
+# ----------------------------------------------------------------------------
+# rotary positions
+# ----------------------------------------------------------------------------
+def _rotary(x, positions, freqs, sections, interleaved, lengths, y, inverse):
+    dt = _kind(x, "x")
+    shape = x.shape
+    if len(shape) not in (3, 4):
+        raise ValueError(f"x must be [B, L, H, D] or [B, H, D] (got {tuple(shape)})")
+    B, L, (H, D) = shape[0], shape[1] if len(shape) == 4 else 1, shape[-2:]
+    sections = (freqs.shape[0],) if sections is None and freqs.dim() == 1 else tuple(sections or ())
+    if not 1 <= len(sections) <= 4 or freqs.dim() != 1 or freqs.shape[0] != sum(sections):
+        raise ValueError(f"sections are the pairs of 1 to 4 axes, and freqs has one a pair (got {sections}, {tuple(freqs.shape)})")
+    want = shape[:-2] + (len(sections),)
+    one = positions.dim() == 2 and len(shape) == 4  # the same for every sequence
+    if positions.dtype != torch.int32 or positions.device != x.device or positions.shape != (want[1:] if one else want):
+        _wrong(positions, torch.int32, x.device, want, "positions")
+    s = positions.stride()
+    if s[-1] != 1 and want[-1] > 1:
+        raise ValueError("positions' last dimension must be dense")
+    y = _like(x) if y is None else y
+    a = RotaryArgs(dt, B, L, H, D, len(sections), interleaved, inverse, (ctypes.c_int * 4)(*sections),
+                   _heads(x, x, shape, "x"), _heads(y, x, shape, "y"), positions.data_ptr(), 0 if one else s[0],
+                   s[-2] if len(shape) == 4 else 0, _f32(freqs, x, freqs.shape, "freqs"), _i32(lengths, x, (B,), "lengths"))
+    call("fdc_rotary", a, _stream())
+    return y
+
+
+def rotary_forward(x, positions, freqs, sections=None, interleaved=False, lengths=None, y=None):
+    """x [B, L, H, D] (or [B, H, D], one token) with each pair of channels turned by position * frequency (fdc_rotary) -> y.
+    positions [B, L, axes] or [L, axes] ([B, axes]) int32; sections: the number of pairs of each axis (None: one
+    axis); freqs [pairs] float32, in the sections' order.  Pairs are the channels (i, pairs + i), or (2 i, 2 i + 1) if
+    interleaved; other channels are copied.  y may be x itself."""
+    return _rotary(x, positions, freqs, sections, interleaved, lengths, y, False)
+
+
+def rotary_backward(gy, positions, freqs, sections=None, interleaved=False, lengths=None, gx=None):
+    """-> gx from gy: the turn back (gx may be gy itself)."""
+    return _rotary(gy, positions, freqs, sections, interleaved, lengths, gx, True)
+
+
+# ----------------------------------------------------------------------------
+# cross attention
+# ----------------------------------------------------------------------------
+def _attention_args(q, k, v, scale, q_lengths, lengths, mask, y):
+    dt = _kind(q, "q")
+    shape, kept = q.shape, k.shape
+    if len(shape) not in (3, 4) or len(kept) != 4:
+        raise ValueError(f"q must be [B, Lq, H, D] or [B, H, D], k and v [B, Lk, G, D] (got {tuple(shape)}, {tuple(kept)})")
+    B, (H, D) = shape[0], shape[-2:]
+    kept = (B, kept[1], kept[2], D)
+    if mask is None:
+        mp, ms = None, 0
+    else:
+        if mask.dtype not in (torch.bool, torch.uint8):
+            raise ValueError(f"mask must be bool or uint8 (got {mask.dtype})")
+        if mask.device != q.device or mask.shape != kept[:2]:
+            _wrong(mask, mask.dtype, q.device, kept[:2], "mask")
+        mp, (ms, inner) = mask.data_ptr(), mask.stride()
+        if inner != 1 and kept[1] > 1:
+            raise ValueError("mask's last dimension must be dense")
+    return CrossAttentionArgs(dt, B, shape[1] if len(shape) == 4 else 1, kept[1], H, kept[2], D,
+                              D ** -0.5 if scale is None else scale, _heads(q, q, shape, "q"), _heads(k, q, kept, "k"),
+                              _heads(v, q, kept, "v"), _heads(y, q, shape, "y"), _i32(q_lengths, q, (B,), "q_lengths"),
+                              _i32(lengths, q, (B,), "lengths"), mp, ms)
+
+
+def _attention_ws(a, ref, which):
+    return _scratch(_bytes("fdc_cross_attention_workspace_size", a.dtype, a.B, a.Lq, a.Lk, a.H, a.G, a.D, which=which, of=2),
+                    ref)
+
+
+def cross_attention_forward(q, k, v, scale=None, q_lengths=None, lengths=None, mask=None, save=False, y=None):
+    """Attention of q [B, Lq, H, D] to k and v [B, Lk, G, D], whose heads H / G adjacent ones of q share -> (y, lse)
+    (fdc_cross_attention_forward).  scale: D ** -0.5 if None.  A sequence's keys are those before lengths [B] (int32) whose
+    mask [B, Lk] (bool or uint8) is true, its queries those before q_lengths [B]; a row without keys is 0.
+    lse [B, H, Lq] float32, what cross_attention_backward needs, if `save` is asked for, else None."""
+    if q.dim() != 4:
+        raise ValueError(f"q must be [B, Lq, H, D] (got {tuple(q.shape)})")
+    y = _like(q) if y is None else y
+    a = _attention_args(q, k, v, scale, q_lengths, lengths, mask, y)
+    lse = _empty((a.B, a.H, a.Lq), q, torch.float32) if save else None
+    ws, size, keep = _attention_ws(a, q, 0)
+    call("fdc_cross_attention_forward", a, _ptr(lse), ws, size, _stream())
+    return y, lse
+
+
+def cross_attention_step(q, k, v, scale=None, lengths=None, mask=None, y=None):
+    """One token q [B, H, D] of every sequence -> y."""
+    if q.dim() != 3:
+        raise ValueError(f"q must be [B, H, D] (got {tuple(q.shape)})")
+    y = _like(q) if y is None else y
+    a = _attention_args(q, k, v, scale, None, lengths, mask, y)
+    ws, size, keep = _attention_ws(a, q, 0)
+    call("fdc_cross_attention_forward", a, None, ws, size, _stream())
+    return y
+
+
+def cross_attention_backward(gy, y, lse, q, k, v, scale=None, q_lengths=None, lengths=None, mask=None):
+    """Gradients of q, k and v from gy and cross_attention_forward's y and lse."""
+    if q.dim() != 4:
+        raise ValueError(f"q must be [B, Lq, H, D] (got {tuple(q.shape)})")
+    a = _attention_args(q, k, v, scale, q_lengths, lengths, mask, y)
+    g = AttentionGradients(_like(q), _like(k), _like(v))
+    s = CrossAttentionGrads(_heads(gy, q, q.shape, "gy"), _heads(g.q, q, q.shape, "gq"), _heads(g.k, q, k.shape, "gk"),
+                            _heads(g.v, q, v.shape, "gv"))
+    ws, size, keep = _attention_ws(a, q, 1)
+    call("fdc_cross_attention_backward", a, _f32(lse, q, (a.B, a.H, a.Lq), "lse"), s, ws, size, _stream())
+    return g
+
+
+# ----------------------------------------------------------------------------
+# token log probabilities
+# ----------------------------------------------------------------------------
+def _logprobs_args(z, tokens, K, temperature):
+    dt = _kind(z, "z")
+    if z.dim() != 2:
+        raise ValueError(f"z must be [rows, vocabulary] (got {tuple(z.shape)})")
+    return TokenLogprobsArgs(dt, z.shape[1], K, z.shape[0], temperature, *_rows(z, z, z.shape, "z"),
+                             _i32(tokens, z, (z.shape[0],), "tokens"))
+
+
+def token_logprobs_forward(z, tokens=None, top=0, temperature=1.0):
+    """Of each row of z [rows, V] at a temperature (fdc_token_logprobs_forward): logp [rows], the log probability of
+    tokens [rows] (int32, -1: none, which has 0; None without tokens), the entropy [rows], and the `top` best alternatives, idx
+    [rows, top] (int32) and their log probabilities top [rows, top], from high to low, equal ones by place
+    (None where top is 0) -> TokenLogprobs(logp, entropy, idx, top, stats)."""
+    a = _logprobs_args(z, tokens, top, temperature)
+    logp = None if tokens is None else _empty((a.R,), z, torch.float32)
+    entropy, stats = _empty((a.R,), z, torch.float32), _empty((a.R, 3), z, torch.float32)
+    idx, best = (_empty((a.R, top), z, torch.int32), _empty((a.R, top), z, torch.float32)) if top > 0 else (None, None)
+    ws, size, keep = _scratch(_bytes("fdc_token_logprobs_workspace_size", a.dtype, a.R, a.V, a.K), z)
+    call("fdc_token_logprobs_forward", a, _ptr(logp), _ptr(entropy), _ptr(idx), _ptr(best), _ptr(stats), ws, size, _stream())
+    return TokenLogprobs(logp, entropy, idx, best, stats)
+
+
+def token_logprobs_backward(stats, z, tokens=None, glogp=None, gentropy=None, idx=None, gtop=None, temperature=1.0,
+                            gz=None):
+    """Gradient of z from those of logp, entropy and top (None: 0; gtop with the forward's idx) and
+    token_logprobs_forward's stats (gz may be z itself)."""
+    K = 0 if gtop is None or idx is None or idx.dim() != 2 else idx.shape[1]
+    a = _logprobs_args(z, tokens, K, temperature)
+    gz = _like(z) if gz is None else gz
+    gp, gs = _rows(gz, z, z.shape, "gz")
+    named = (None, None) if gtop is None else (_i32(idx, z, (a.R, K), "idx"), _f32(gtop, z, (a.R, K), "gtop"))
+    call("fdc_token_logprobs_backward", a, _f32(stats, z, (a.R, 3), "stats"), _f32(glogp, z, (a.R,), "glogp"),
+         _f32(gentropy, z, (a.R,), "gentropy"), *named, gp, gs, _stream())
+    return gz
