@@ -599,9 +599,11 @@ fdc_status fdc_rotary(const fdc_rotary_args *a, hipStream_t stream);
  * heads of queries, G heads of keys and values that H / G adjacent query heads share:
  *   s[j] = scale q[b][t][h] . k[b][j][h / (H / G)],   y[b][t][h] = sum_j softmax(s)[j] v[b][j][h / (H / G)]
  * over the keys j that sequence b has: j < lengths[b] and mask[b * mask_stride + j] != 0 (either NULL: no such limit).
- * What k and v hold at other keys is never used, NaN included.  A row without keys has y = 0 and lse = -inf.
+ * What k and v hold at other keys is never used, NaN included.  A row without keys has y = 0.
  * q, y [B][Lq][H][D]; k, v [B][Lk][G][D]; 1 <= D <= 128; scale > 0.  q_lengths [B] (NULL: Lq): the queries' lengths.
- * lse [B][H][Lq] float32 (NULL: no backward follows): log sum_j exp(s[j]), -inf past a sequence's queries.
+ * saved (NULL: no backward follows): fdc_cross_attention_saved_size bytes, 16-byte aligned, for the backward.  It begins
+ * with lse [B][H][Lq] float32: log sum_j exp(s[j]), -inf without keys and past a sequence's queries (the rest: what
+ * y's rounding lost).
  * A single token is a call with Lq = 1.  y is other memory than q, k and v.
  * ws: fdc_cross_attention_workspace_size's fwd_ws bytes. */
 typedef struct {
@@ -614,14 +616,15 @@ typedef struct {
 } fdc_cross_attention_args;
 fdc_status fdc_cross_attention_workspace_size(int dtype, int B, int Lq, int Lk, int H, int G, int D, size_t *fwd_ws,
                                               size_t *bwd_ws);
-fdc_status fdc_cross_attention_forward(const fdc_cross_attention_args *a, float *lse, void *ws, size_t ws_bytes,
+fdc_status fdc_cross_attention_saved_size(int dtype, int B, int Lq, int H, int D, size_t *bytes);
+fdc_status fdc_cross_attention_forward(const fdc_cross_attention_args *a, float *saved, void *ws, size_t ws_bytes,
                                        hipStream_t stream);
-/* From gy, the forward's inputs, its y and its lse: gq, gk, gv (type of the activations, all required; gk and gv summed
+/* From gy, the forward's inputs, its y and what it saved: gq, gk, gv (type of the activations, all required; gk and gv summed
  * over the query heads that share them, 0 at keys that a sequence does not have).  Sums run in a fixed order. */
 typedef struct {
   fdc_heads gy, gq, gk, gv;
 } fdc_cross_attention_grads;
-fdc_status fdc_cross_attention_backward(const fdc_cross_attention_args *a, const float *lse,
+fdc_status fdc_cross_attention_backward(const fdc_cross_attention_args *a, const float *saved,
                                         const fdc_cross_attention_grads *g, void *ws, size_t ws_bytes,
                                         hipStream_t stream);
 

@@ -151,6 +151,7 @@ _SIGS = {
     "fdc_distill_forward_backward": [ctypes.POINTER(DistillArgs), _P, _P, _P, _P, _I64, _P, _SZ, _P],
     "fdc_rotary": [ctypes.POINTER(RotaryArgs), _P],
     "fdc_cross_attention_workspace_size": [_I, _I, _I, _I, _I, _I, _I, _SZP, _SZP],
+    "fdc_cross_attention_saved_size": [_I, _I, _I, _I, _I, _SZP],
     "fdc_cross_attention_forward": [ctypes.POINTER(CrossAttentionArgs), _P, _P, _SZ, _P],
     "fdc_cross_attention_backward": [ctypes.POINTER(CrossAttentionArgs), _P, ctypes.POINTER(CrossAttentionGrads), _P,
                                      _SZ, _P],

@@ -563,19 +563,29 @@ fdc_status fdc_cross_attention_workspace_size(int dtype, int B, int Lq, int Lk, 
   return FDC_OK;
 }
 
-fdc_status fdc_cross_attention_forward(const fdc_cross_attention_args *a, float *lse, void *ws, size_t ws_bytes,
+fdc_status fdc_cross_attention_saved_size(int dtype, int B, int Lq, int H, int D, size_t *bytes) {
+  FDC_TRY(check_attention_sizes(dtype, B, Lq, 1, H, H, D));
+  if (!bytes) return fail(FDC_EINVAL, "bytes is NULL");
+  *bytes = fdc::cross_attention_saved(dtype, B, Lq, H, D);
+  return FDC_OK;
+}
+
+fdc_status fdc_cross_attention_forward(const fdc_cross_attention_args *a, float *saved, void *ws, size_t ws_bytes,
                                        hipStream_t s) {
   FDC_TRY(check_attention(a, true));
+  if (reinterpret_cast<uintptr_t>(saved) & 15) return fail(FDC_EINVAL, "saved must be 16-byte aligned");
   FDC_TRY(check_attention_apart(a, {a->y, "y", a->Lq, a->H}));
   FDC_TRY(check_ws(ws, ws_bytes, fdc::cross_attention_fwd_ws(a->dtype, a->B, a->Lq, a->Lk, a->H, a->G, a->D),
                    "cross attention forward"));
-  return check_hip(fdc::launch_cross_attention_fwd(*a, lse, static_cast<float *>(ws), s), "cross attention");
+  return check_hip(fdc::launch_cross_attention_fwd(*a, saved, static_cast<float *>(ws), s), "cross attention");
 }
 
-fdc_status fdc_cross_attention_backward(const fdc_cross_attention_args *a, const float *lse,
+fdc_status fdc_cross_attention_backward(const fdc_cross_attention_args *a, const float *saved,
                                         const fdc_cross_attention_grads *g, void *ws, size_t ws_bytes, hipStream_t s) {
   FDC_TRY(check_attention(a, false));
-  if (!lse || !g) return fail(FDC_EINVAL, "lse or gradients are NULL");
+  if (!g) return fail(FDC_EINVAL, "gradients are NULL");
+  if (!saved || (reinterpret_cast<uintptr_t>(saved) & 15))
+    return fail(FDC_EINVAL, "saved must be given and 16-byte aligned");
   FDC_TRY(check_heads(g->gy, "gy", a->B, a->Lq, a->H, a->D, false));
   FDC_TRY(check_heads(g->gq, "gq", a->B, a->Lq, a->H, a->D, true));
   FDC_TRY(check_heads(g->gk, "gk", a->B, a->Lk, a->G, a->D, true));
@@ -589,7 +599,7 @@ fdc_status fdc_cross_attention_backward(const fdc_cross_attention_args *a, const
   }
   FDC_TRY(check_ws(ws, ws_bytes, fdc::cross_attention_bwd_ws(a->dtype, a->B, a->Lq, a->Lk, a->H, a->G, a->D),
                    "cross attention backward"));
-  return check_hip(fdc::launch_cross_attention_bwd(*a, lse, *g, static_cast<float *>(ws), s), "cross attention backward");
+  return check_hip(fdc::launch_cross_attention_bwd(*a, saved, *g, static_cast<float *>(ws), s), "cross attention backward");
 }
 
 // ---------------------------------------------------------------------------

@@ -105,6 +105,22 @@ __device__ __forceinline__ Frag<T> score_frag(const v16f &s, int u) {
   return f;
 }
 
+// sum + the 8 values of a factor, added in float32.
+__device__ __forceinline__ float add_values(const Frag<__bf16> &f, float sum) {
+  typedef __bf16 v2 __attribute__((ext_vector_type(2)));
+  const v2 one = {(__bf16)1.f, (__bf16)1.f};
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) sum = __builtin_amdgcn_fdot2_f32_bf16(v2{f[i], f[i + 1]}, one, sum, false);
+  return sum;
+}
+__device__ __forceinline__ float add_values(const Frag<_Float16> &f, float sum) {
+  typedef _Float16 v2 __attribute__((ext_vector_type(2)));
+  const v2 one = {(_Float16)1.f, (_Float16)1.f};
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) sum = __builtin_amdgcn_fdot2(v2{f[i], f[i + 1]}, one, sum, false);
+  return sum;
+}
+
 // n (maybe <= 0) of 8 elements from memory, the others 0.
 template <class T>
 __device__ __forceinline__ Frag<T> load_frag(const T *p, int n) {
@@ -159,7 +175,14 @@ struct Attn {
   int per, R;  // query heads a key head, rows a key head
   int D4;      // channels of a partial result's row
   float c;     // scale log2(e)
+  float *lse;  // [B][H][Lq] (NULL: no backward follows)
+  void *low;   // [rows][D4], 16-bit types: what y's rounding lost, times kLowUp
 };
+// y and its low part are the sum to 16 (bfloat16) or 22 (float16) bits: delta is formed from both, since for a row that reads
+// few keys it nearly cancels against gy . v, and y's rounding alone would be the largest error of gq and gk.  The
+// factor keeps the low part among float16's normal numbers where y is.
+template <class T>
+constexpr float kLowUp = std::is_same_v<T, _Float16> ? 2048.f : 1.f;
 
 // Row r of key head g: a head and a token.
 struct Row {
@@ -195,6 +218,20 @@ __device__ __forceinline__ void each_four(const v16f (&o)[DP / 32], int D, int h
     }
 }
 
+// 4 channels of a row of y from c on, and of its low part.
+template <class T>
+__device__ __forceinline__ void store_y(const Attn &p, T *y, int64_t at_row, int c, const float (&x)[4]) {
+  store_some<T, 4>(y + c, x, p.a.D - c);
+  if constexpr (sizeof(T) == 2) {
+    if (p.low != nullptr) {
+      float rest[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) rest[i] = (x[i] - (float)(T)x[i]) * kLowUp<T>;
+      store_pack<T, 4>(static_cast<T *>(p.low) + at_row * p.D4 + c, rest);
+    }
+  }
+}
+
 // ---- forward -----------------------------------------------------------------
 // float16's probabilities are held 2^7 times as large, so that small ones keep their digits (2^-14 is its least normal
 // number); they stay below 2^15 with the largest score up to 2^8 past the one they are taken relative to.
@@ -204,10 +241,12 @@ constexpr float kLate = 8.f;
 
 // A workgroup has 32 W rows of a key head, a wave 32 of them, and goes through a run of the keys, whose
 // tiles of k and v pass through LDS in two buffers: the next tile is loaded to registers during a tile's products.
+// y is divided by the sum of the rounded probabilities, so that its weights add up to 1: for a row that reads one key
+// almost alone, y then is off by a rounding of the others' part only, and so is delta.  lse is of the sum before rounding.
 // The running maximum of a row is raised, and its sums rescaled, only when a score is 2^8 past it.
 template <class T, int DP, int W>
-__global__ __launch_bounds__(64 * W) void k_attn_fwd(Attn p, float *__restrict__ lse, float *__restrict__ part,
-                                                     int row_tiles, int splits, int run) {
+__global__ __launch_bounds__(64 * W) void k_attn_fwd(Attn p, float *__restrict__ part, int row_tiles, int splits,
+                                                     int run) {
   constexpr int KT = attn_keys(sizeof(T)), S = KT * kStride<T, DP>, NB = KT / 32;
   extern __shared__ __align__(16) char lds_[];
   T *lds = reinterpret_cast<T *>(lds_);
@@ -222,7 +261,7 @@ __global__ __launch_bounds__(64 * W) void k_attn_fwd(Attn p, float *__restrict__
   Frag<T> q[DP / 16];
   load_row<T, DP>(q, at<T>(p.a.q, b, row.t, row.head), p.a.D, half, row.live);
   v16f o[DP / 32] = {};
-  float m = -INFINITY, l = 0.f;
+  float m = -INFINITY, l = 0.f, w = 0.f;  // the sum, and that of the rounded probabilities
   const int first = split * run, last = min(first + run, (keys + KT - 1) / KT);
   if (first < last && __syncthreads_or(row.live)) {
     Staged<T, DP, 64 * W> sk, sv;
@@ -266,7 +305,7 @@ __global__ __launch_bounds__(64 * W) void k_attn_fwd(Attn p, float *__restrict__
         const bool late = top > m + kLate;
         if (__any(late)) {
           const float to = late ? top : m, f = m == to ? 1.f : exp2_fast(m - to);
-          l *= f;
+          l *= f, w *= f;
 #pragma unroll
           for (int d = 0; d < DP / 32; ++d) o[d] *= f;
           m = to;
@@ -283,6 +322,7 @@ __global__ __launch_bounds__(64 * W) void k_attn_fwd(Attn p, float *__restrict__
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
             const Frag<T> e = score_frag<T>(s[k], u);
+            if constexpr (sizeof(T) == 2) w = add_values(e, w);
 #pragma unroll
             for (int d = 0; d < DP / 32; ++d) mma(o[d], column_frag<T, DP>(vt, 32 * k + 16 * u, 32 * d, lane), e);
           }
@@ -296,25 +336,27 @@ __global__ __launch_bounds__(64 * W) void k_attn_fwd(Attn p, float *__restrict__
     }
   }
   l = halves_sum(l);
+  w = sizeof(T) == 2 ? halves_sum(w) : l;
   if (r >= p.R) return;
   if (splits > 1) {
     const int64_t at = ((int64_t)split * p.a.B * p.a.G + bg) * p.R + r;
     float *to = part + at * (p.D4 + 4);
     each_four<DP>(o, p.D4, half, 1.f, [&](int c, const float(&x)[4]) { __builtin_memcpy(to + c, x, sizeof x); });
-    if (half == 0) to[p.D4] = m, to[p.D4 + 1] = l;
+    if (half == 0) to[p.D4] = m, to[p.D4 + 1] = l, to[p.D4 + 2] = w;
     return;
   }
-  const float f = !row.live || l == 0.f ? 0.f : 1.f / l;
+  const float f = !row.live || l == 0.f ? 0.f : 1.f / w;
   T *y = at<T>(p.a.y, b, row.t, row.head);
-  each_four<DP>(o, p.a.D, half, f, [&](int c, const float(&x)[4]) { store_some<T, 4>(y + c, x, p.a.D - c); });
-  if (lse != nullptr && half == 0)
-    lse[(int64_t)bg * p.R + r] = !row.live || l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l) - kUp<T>) * kLn2;
+  const int64_t at_row = (int64_t)bg * p.R + r;
+  each_four<DP>(o, p.a.D, half, f, [&](int c, const float(&x)[4]) { store_y<T>(p, y, at_row, c, x); });
+  if (p.lse != nullptr && half == 0)
+    p.lse[at_row] = !row.live || l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l) - kUp<T>) * kLn2;
 }
 
 // The runs' results of a row, in order: a thread has 4 channels.
 template <class T>
-__global__ __launch_bounds__(256) void k_attn_join(Attn p, const float *__restrict__ part, float *__restrict__ lse,
-                                                   int splits, long long total) {
+__global__ __launch_bounds__(256) void k_attn_join(Attn p, const float *__restrict__ part, int splits,
+                                                   long long total) {
   const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
   if (id >= total) return;
   const int fours = p.D4 / 4;
@@ -324,20 +366,21 @@ __global__ __launch_bounds__(256) void k_attn_join(Attn p, const float *__restri
   const Row row = row_of(p, g, (int)(at_row - (long long)bg * p.R), length_of(p.a.q_lengths, b, p.a.Lq));
   const int64_t step = (int64_t)p.a.B * p.a.G * p.R * (p.D4 + 4);
   const float *x = part + at_row * (p.D4 + 4);
-  float m = -INFINITY, l = 0.f, o[4] = {};
+  float m = -INFINITY, l = 0.f, w = 0.f, o[4] = {};
   for (int i = 0; i < splits; ++i) m = fmaxf(m, x[i * step + p.D4]);
   for (int i = 0; i < splits; ++i) {
     const float *y = x + i * step, f = y[p.D4] == m ? 1.f : exp2_fast(y[p.D4] - m);
     l = fmaf(y[p.D4 + 1], f, l);
+    w = fmaf(y[p.D4 + 2], f, w);
 #pragma unroll
     for (int j = 0; j < 4; ++j) o[j] = fmaf(y[c + j], f, o[j]);
   }
-  const float f = !row.live || l == 0.f ? 0.f : 1.f / l;
+  const float f = !row.live || l == 0.f ? 0.f : 1.f / w;
 #pragma unroll
   for (int j = 0; j < 4; ++j) o[j] *= f;
-  store_some<T, 4>(at<T>(p.a.y, b, row.t, row.head) + c, o, p.a.D - c);
-  if (lse != nullptr && c == 0)
-    lse[at_row] = !row.live || l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l) - kUp<T>) * kLn2;
+  store_y<T>(p, at<T>(p.a.y, b, row.t, row.head), at_row, c, o);
+  if (p.lse != nullptr && c == 0)
+    p.lse[at_row] = !row.live || l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l) - kUp<T>) * kLn2;
 }
 
 // ---- backward ----------------------------------------------------------------
@@ -348,13 +391,13 @@ constexpr float kUpBack = std::is_same_v<T, _Float16> ? 15.f : 0.f;
 // [rows][2]: what a score's exponent is less by (infinity for a row without keys, or past the queries: its probabilities are 0)
 // and delta.  16 lanes a row.
 template <class T>
-__global__ __launch_bounds__(256) void k_attn_delta(Attn p, fdc_heads gy, const float *__restrict__ lse,
-                                                    float2 *__restrict__ stats, long long rows) {
+__global__ __launch_bounds__(256) void k_attn_delta(Attn p, fdc_heads gy, float2 *__restrict__ stats,
+                                                    long long rows) {
   const long long at_row = (long long)blockIdx.x * 16 + threadIdx.x / 16;
   if (at_row >= rows) return;
   const int bg = (int)(at_row / p.R), b = bg / p.a.G, g = bg - b * p.a.G, c = threadIdx.x % 16 * 8;
   const Row row = row_of(p, g, (int)(at_row - (long long)bg * p.R), length_of(p.a.q_lengths, b, p.a.Lq));
-  const float e = lse[at_row];
+  const float e = p.lse[at_row];
   const bool live = row.live && e != -INFINITY;
   float sum = 0.f;
   if (live && c < p.a.D) {
@@ -362,6 +405,13 @@ __global__ __launch_bounds__(256) void k_attn_delta(Attn p, fdc_heads gy, const 
     const Frag<T> y = load_frag<T>(at<T>(p.a.y, b, row.t, row.head) + c, p.a.D - c);
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum = fmaf((float)x[i], (float)y[i], sum);
+    if constexpr (sizeof(T) == 2) {
+      const Frag<T> rest = load_frag<T>(static_cast<const T *>(p.low) + at_row * p.D4 + c, p.a.D - c);
+      float more = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) more = fmaf((float)x[i], (float)rest[i], more);
+      sum = fmaf(more, 1.f / kLowUp<T>, sum);
+    }
   }
   sum = lane_sum<16>(sum);
   if (threadIdx.x % 16 == 0) stats[at_row] = live ? float2{e * kLog2e - kUpBack<T>, sum} : float2{INFINITY, 0.f};
@@ -654,8 +704,10 @@ struct Cuts {
   size_t kv_floats() const { return kv.splits > 1 ? (size_t)kv.splits * keys * 2 * D4 : 0; }
 };
 
-Attn attn_of(const fdc_cross_attention_args &a) {
-  return {a, a.H / a.G, a.H / a.G * a.Lq, (a.D + 3) / 4 * 4, a.scale * kLog2e};
+int64_t lse_floats(int B, int Lq, int H) { return ceil_div((int64_t)B * Lq * H, 4) * 4; }
+Attn attn_of(const fdc_cross_attention_args &a, float *saved) {
+  void *low = saved != nullptr && dtype_size(a.dtype) == 2 ? saved + lse_floats(a.B, a.Lq, a.H) : nullptr;
+  return {a, a.H / a.G, a.H / a.G * a.Lq, (a.D + 3) / 4 * 4, a.scale * kLog2e, saved, low};
 }
 
 // f(T{}, padded channels, waves) for the type, channels and waves of a call.
@@ -692,6 +744,10 @@ bool cross_attention_fits(int dtype, int B, int Lq, int Lk, int H, int G, int D)
          c.rows * c.D4 / 4 < (1LL << 32) - 256 && c.keys * 2 * c.D4 / 4 < (1LL << 32) - 256;
 }
 
+size_t cross_attention_saved(int dtype, int B, int Lq, int H, int D) {
+  const size_t low = dtype_size(dtype) == 2 ? (size_t)B * Lq * H * (ceil_div(D, 4) * 4) * 2 : 0;
+  return lse_floats(B, Lq, H) * sizeof(float) + (low + 15) / 16 * 16;
+}
 size_t cross_attention_fwd_ws(int dtype, int B, int Lq, int Lk, int H, int G, int D) {
   return Cuts(dtype, B, Lq, Lk, H, G, D).fwd_floats() * sizeof(float);
 }
@@ -700,34 +756,34 @@ size_t cross_attention_bwd_ws(int dtype, int B, int Lq, int Lk, int H, int G, in
   return (c.stats_floats() + std::max(c.q_floats(), c.kv_floats())) * sizeof(float);
 }
 
-hipError_t launch_cross_attention_fwd(const fdc_cross_attention_args &a, float *lse, float *ws, hipStream_t s) {
-  const Attn p = attn_of(a);
+hipError_t launch_cross_attention_fwd(const fdc_cross_attention_args &a, float *saved, float *ws, hipStream_t s) {
+  const Attn p = attn_of(a, saved);
   const Cuts cuts(a.dtype, a.B, a.Lq, a.Lk, a.H, a.G, a.D);
   const Cut &c = cuts.fwd;
   if (hipError_t e = by_shape(a.dtype, a.D, c.waves, [&](auto tag, auto dp, auto waves) {
         using T = decltype(tag);
         constexpr int DP = decltype(dp)::value, W = decltype(waves)::value;
         return launch_tiles<k_attn_fwd<T, DP, W>>("attn_fwd", (long long)a.B * a.G * c.tiles * c.splits, 64 * W,
-                                                  4 * tile_bytes<T, DP>(), s, p, lse, ws, c.tiles, c.splits, c.run);
+                                                  4 * tile_bytes<T, DP>(), s, p, ws, c.tiles, c.splits, c.run);
       }))
     return e;
   if (c.splits == 1) return hipSuccess;
   const long long total = cuts.rows * (p.D4 / 4);
   return by_dtype(a.dtype, [&](auto tag) {
     return timed_launch("attn_join", k_attn_join<decltype(tag)>, dim3((unsigned)ceil_div(total, 256)), dim3(256), 0, s, p,
-                        (const float *)ws, lse, c.splits, total);
+                        (const float *)ws, c.splits, total);
   });
 }
 
-hipError_t launch_cross_attention_bwd(const fdc_cross_attention_args &a, const float *lse,
+hipError_t launch_cross_attention_bwd(const fdc_cross_attention_args &a, const float *saved,
                                       const fdc_cross_attention_grads &g, float *ws, hipStream_t s) {
-  const Attn p = attn_of(a);
+  const Attn p = attn_of(a, const_cast<float *>(saved));
   const Cuts cuts(a.dtype, a.B, a.Lq, a.Lk, a.H, a.G, a.D);
   float2 *stats = reinterpret_cast<float2 *>(ws);
   float *part = ws + cuts.stats_floats();
   if (hipError_t e = by_dtype(a.dtype, [&](auto tag) {
         return timed_launch("attn_delta", k_attn_delta<decltype(tag)>, dim3((unsigned)ceil_div(cuts.rows, 16)), dim3(256),
-                            0, s, p, g.gy, lse, stats, cuts.rows);
+                            0, s, p, g.gy, stats, cuts.rows);
       }))
     return e;
   auto sum = [&](auto keys, const Cut &c, const fdc_heads &out0, const fdc_heads &out1, int n, long long total) {

@@ -55,10 +55,11 @@ hipError_t launch_distill_bwd(const fdc_distill_args &a, const float *stats, con
 hipError_t launch_rotary(const fdc_rotary_args &a, hipStream_t s);
 
 bool cross_attention_fits(int dtype, int B, int Lq, int Lk, int H, int G, int D);
+size_t cross_attention_saved(int dtype, int B, int Lq, int H, int D);  // bytes
 size_t cross_attention_fwd_ws(int dtype, int B, int Lq, int Lk, int H, int G, int D);  // bytes
 size_t cross_attention_bwd_ws(int dtype, int B, int Lq, int Lk, int H, int G, int D);
-hipError_t launch_cross_attention_fwd(const fdc_cross_attention_args &a, float *lse, float *ws, hipStream_t s);
-hipError_t launch_cross_attention_bwd(const fdc_cross_attention_args &a, const float *lse,
+hipError_t launch_cross_attention_fwd(const fdc_cross_attention_args &a, float *saved, float *ws, hipStream_t s);
+hipError_t launch_cross_attention_bwd(const fdc_cross_attention_args &a, const float *saved,
                                       const fdc_cross_attention_grads &g, float *ws, hipStream_t s);
 
 size_t token_logprobs_ws(int dtype, int64_t R, int V, int K);  // bytes

@@ -49,9 +49,12 @@ __device__ __forceinline__ void add(Sums &a, const Sums &b, float c) {
     return;
   }
   const float m = fmaxf(a.m, b.m);
-  const float fa = a.m == m ? 1.f : exp2_fast((a.m - m) * c), fb = b.m == m ? 1.f : exp2_fast((b.m - m) * c);
-  a.u = fa * (a.u + (a.m == m ? 0.f : a.s * (a.m - m))) + fb * (b.u + (b.m == m ? 0.f : b.s * (b.m - m)));
-  a.s = a.s * fa + b.s * fb;
+  // the differences as numbers, the sums scaled before they are multiplied with them: segments of the type's lowest value
+  const float da = a.m == m ? 0.f : fmaxf(a.m - m, kLowest), db = b.m == m ? 0.f : fmaxf(b.m - m, kLowest);
+  const float fa = exp2_fast(da * c), fb = exp2_fast(db * c);
+  const float sa = a.s * fa, sb = b.s * fb;
+  a.u = fmaf(sa, da, a.u * fa) + fmaf(sb, db, b.u * fb);
+  a.s = sa + sb;
   a.m = m;
 }
 
@@ -434,9 +437,10 @@ __global__ __launch_bounds__(kGradThreads) void k_logprobs_grad(fdc_token_logpro
   // p (l + entropy) with l = (z - m) / tau - log s
   const float shift = p[2] - __builtin_amdgcn_logf(p[1]) * kLn2;
   const float c0 = fmaf(gh, shift, alike), c1 = gh * per;
+  const float none = -300.f / c;  // from here on the exponential is 0: what it is multiplied with stays finite
   auto grad = [&](float x) {
     const float d = x - m;
-    return -f * exp2_fast(d * c) * fmaf(c1, fmaxf(d, kLowest), c0);
+    return -f * exp2_fast(d * c) * fmaf(c1, fmaxf(d, none), c0);
   };
   for (int at = begin + tid * V; at < end; at += kGradThreads * V) {
     const int n = min(V, end - at);

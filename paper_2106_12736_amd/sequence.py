@@ -431,19 +431,24 @@ def _attention_ws(a, ref, which):
                     ref)
 
 
+def _saved_floats(a):
+    return _bytes("fdc_cross_attention_saved_size", a.dtype, a.B, a.Lq, a.H, a.D) // 4
+
+
 def cross_attention_forward(q, k, v, scale=None, q_lengths=None, lengths=None, mask=None, save=False, y=None):
-    """Attention of q [B, Lq, H, D] to k and v [B, Lk, G, D], whose heads H / G adjacent ones of q share -> (y, lse)
+    """Attention of q [B, Lq, H, D] to k and v [B, Lk, G, D], whose heads H / G adjacent ones of q share -> (y, saved)
     (fdc_cross_attention_forward).  scale: D ** -0.5 if None.  A sequence's keys are those before lengths [B] (int32) whose
     mask [B, Lk] (bool or uint8) is true, its queries those before q_lengths [B]; a row without keys is 0.
-    lse [B, H, Lq] float32, what cross_attention_backward needs, if `save` is asked for, else None."""
+    saved (float32): what cross_attention_backward needs, if `save` is asked for, else None; its first B H Lq values are
+    the logarithms of the rows' sums of exponentials, [B, H, Lq]."""
     if q.dim() != 4:
         raise ValueError(f"q must be [B, Lq, H, D] (got {tuple(q.shape)})")
     y = _like(q) if y is None else y
     a = _attention_args(q, k, v, scale, q_lengths, lengths, mask, y)
-    lse = _empty((a.B, a.H, a.Lq), q, torch.float32) if save else None
+    saved = _empty((_saved_floats(a),), q, torch.float32) if save else None
     ws, size, keep = _attention_ws(a, q, 0)
-    call("fdc_cross_attention_forward", a, _ptr(lse), ws, size, _stream())
-    return y, lse
+    call("fdc_cross_attention_forward", a, _ptr(saved), ws, size, _stream())
+    return y, saved
 
 
 def cross_attention_step(q, k, v, scale=None, lengths=None, mask=None, y=None):
@@ -457,8 +462,8 @@ def cross_attention_step(q, k, v, scale=None, lengths=None, mask=None, y=None):
     return y
 
 
-def cross_attention_backward(gy, y, lse, q, k, v, scale=None, q_lengths=None, lengths=None, mask=None):
-    """Gradients of q, k and v from gy and cross_attention_forward's y and lse."""
+def cross_attention_backward(gy, y, saved, q, k, v, scale=None, q_lengths=None, lengths=None, mask=None):
+    """Gradients of q, k and v from gy and cross_attention_forward's y and what it saved."""
     if q.dim() != 4:
         raise ValueError(f"q must be [B, Lq, H, D] (got {tuple(q.shape)})")
     a = _attention_args(q, k, v, scale, q_lengths, lengths, mask, y)
@@ -466,7 +471,7 @@ def cross_attention_backward(gy, y, lse, q, k, v, scale=None, q_lengths=None, le
     s = CrossAttentionGrads(_heads(gy, q, q.shape, "gy"), _heads(g.q, q, q.shape, "gq"), _heads(g.k, q, k.shape, "gk"),
                             _heads(g.v, q, v.shape, "gv"))
     ws, size, keep = _attention_ws(a, q, 1)
-    call("fdc_cross_attention_backward", a, _f32(lse, q, (a.B, a.H, a.Lq), "lse"), s, ws, size, _stream())
+    call("fdc_cross_attention_backward", a, _f32(saved, q, (_saved_floats(a),), "saved"), s, ws, size, _stream())
     return g
 
 
@@ -499,7 +504,9 @@ def token_logprobs_backward(stats, z, tokens=None, glogp=None, gentropy=None, id
                             gz=None):
     """Gradient of z from those of logp, entropy and top (None: 0; gtop with the forward's idx) and
     token_logprobs_forward's stats (gz may be z itself)."""
-    K = 0 if gtop is None or idx is None or idx.dim() != 2 else idx.shape[1]
+    if gtop is not None and (idx is None or idx.dim() != 2):
+        raise ValueError("gtop goes with idx [rows, top]")
+    K = 0 if gtop is None else idx.shape[1]
     a = _logprobs_args(z, tokens, K, temperature)
     gz = _like(z) if gz is None else gz
     gp, gs = _rows(gz, z, z.shape, "gz")
