@@ -1,0 +1,396 @@
+// What the kernels of cross attention share (cross_attention.hip: forward, cross_attention_bwd_q.hip, cross_attention_bwd_kv.hip).
+//
+//   s = scale q k^T over the keys a sequence has,  p = exp(s - lse),  y = p v,  lse = log sum exp s
+//   delta = gy . y,  gv = p^T gy,  gs = p (gy v^T - delta),  gq = scale gs k,  gk = scale gs^T q
+//
+// The rows of a key head g are those of the H / G query heads that share it, head by head: row r is token
+// r % Lq of head g H / G + r / Lq, so that few tokens of many heads fill a tile too.
+//
+// Tiles are 32 x 32 products over 16 (v_mfma_f32_32x32x16 for 16-bit types, eight v_mfma_f32_32x32x2 for
+// float32): lane l holds 8 values k = 8 (l / 32) + i of row (column) l % 32 of a factor, and of the
+// result column l % 32, rows 8 (j / 4) + 4 (l / 32) + j % 4 in register j.  Scores are formed transposed, keys by
+// queries, so that a lane has its query's statistics alone to hold, and its 8 registers 8 u ... of the scores are, without
+// moving, the second factor of a product over the 16 keys 16 u + 8 (i / 4) + 4 (l / 32) + i % 4; the first
+// factor's columns are read from LDS in that order (ds_read_b64_tr_b16 turns 4 x 16 pieces).
+#pragma once
+
+#include <algorithm>
+
+#include "device.h"
+#include "lds_limit.h"
+#include "sequence.h"
+
+namespace fdc {
+
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef short v4s __attribute__((ext_vector_type(4)));
+
+namespace attention {
+
+// 8 values of a row for each lane.
+template <class T>
+struct Fragment {
+  typedef T type __attribute__((ext_vector_type(8)));
+};
+template <class T>
+using Frag = typename Fragment<T>::type;
+
+__device__ __forceinline__ void mma(v16f &c, const Frag<__bf16> &a, const Frag<__bf16> &b) {
+  c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ void mma(v16f &c, const Frag<_Float16> &a, const Frag<_Float16> &b) {
+  c = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ void mma(v16f &c, const Frag<float> &a, const Frag<float> &b) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[i], c, 0, 0, 0);
+}
+
+// The values of the lanes l % 32 and l % 32 + 32, in both.
+struct Halves {
+  float lo, hi;
+};
+__device__ __forceinline__ Halves halves(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return {__uint_as_float(r[0]), __uint_as_float(r[1])};
+}
+__device__ __forceinline__ float halves_max(float v) {
+  const Halves h = halves(v);
+  return fmaxf(h.lo, h.hi);
+}
+__device__ __forceinline__ float halves_sum(float v) {
+  const Halves h = halves(v);
+  return h.lo + h.hi;
+}
+
+constexpr int attn_keys(size_t size) { return size == 2 ? 64 : 32; }  // rows of an LDS tile
+// A tile's rows are 32 bytes longer than their channels: 8 rows then begin at 8 different sets of 8 banks.
+template <class T, int DP>
+constexpr int kStride = DP + 32 / (int)sizeof(T);
+template <class T, int DP>
+constexpr size_t tile_bytes() {
+  return (size_t)attn_keys(sizeof(T)) * kStride<T, DP> * sizeof(T);
+}
+
+// Row `row` of a tile, channels 16 s ... 16 s + 15 of which this lane's half.
+template <class T, int DP>
+__device__ __forceinline__ Frag<T> row_frag(const T *tile, int row, int s, int half) {
+  return *reinterpret_cast<const Frag<T> *>(tile + row * kStride<T, DP> + 16 * s + 8 * half);
+}
+// Channel d0 + l % 32 of 16 rows of a tile from row0, in the order of the scores' registers.
+template <class T, int DP>
+__device__ __forceinline__ Frag<T> column_frag(const T *tile, int row0, int d0, int lane) {
+  constexpr int S = kStride<T, DP>;
+  const int half = lane >> 5;
+  if constexpr (sizeof(T) == 2) {
+    typedef __attribute__((address_space(3))) v4s *lds_t;
+    const T *p = tile + (row0 + 4 * half + (lane & 15) / 4) * S + d0 + (lane & 16) + (lane & 3) * 4;
+    struct {
+      v4s lo, hi;
+    } x{__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)p), __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)(p + 8 * S))};
+    return __builtin_bit_cast(Frag<T>, x);
+  } else {
+    const T *p = tile + (row0 + 4 * half) * S + d0 + (lane & 31);
+    Frag<T> f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = p[(8 * (i / 4) + i % 4) * S];
+    return f;
+  }
+}
+// The rows row0 + l % 32 of a tile, `COUNT` steps of 16 channels from step `from` on.  A 16-bit product takes 32 cycles
+// and its factor's way from LDS over 100, so that fragments are read some products ahead, and the order of reads and products
+// is kept from being changed (ahead()); float32's eight instructions a product cover it.
+template <class T, int DP, int COUNT>
+struct Rows {
+  Frag<T> f[COUNT];
+  __device__ __forceinline__ void load(const T *tile, int row0, int from, int lane) {
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) f[i] = row_frag<T, DP>(tile, row0 + (lane & 31), from + i, lane >> 5);
+  }
+};
+// The columns of 32 rows of a tile from row0, all channels.
+template <class T, int DP>
+struct Columns {
+  Frag<T> f[2][DP / 32];
+  __device__ __forceinline__ void load(const T *tile, int row0, int lane) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d) f[u][d] = column_frag<T, DP>(tile, row0 + 16 * u, 32 * d, lane);
+  }
+  // o[d] += the columns' products with 32 values of the other factor
+  __device__ __forceinline__ void add_to(v16f (&o)[DP / 32], const Frag<T> (&e)[2]) const {
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d) mma(o[d], f[u][d], e[u]);
+  }
+};
+template <class T>
+__device__ __forceinline__ void ahead() {
+  if constexpr (sizeof(T) == 2) __builtin_amdgcn_sched_barrier(0);
+}
+
+// Registers 8 u ... 8 u + 7 of a tile of scores, rounded to the activations' type: at most half a step of each factor
+// of a sum, as its other factors are.
+template <class T>
+__device__ __forceinline__ Frag<T> score_frag(const v16f &s, int u) {
+  Frag<T> f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = (T)s[8 * u + i];
+  return f;
+}
+
+// sum + the 8 values of a factor, added in float32.
+__device__ __forceinline__ float add_values(const Frag<__bf16> &f, float sum) {
+  typedef __bf16 v2 __attribute__((ext_vector_type(2)));
+  const v2 one = {(__bf16)1.f, (__bf16)1.f};
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) sum = __builtin_amdgcn_fdot2_f32_bf16(v2{f[i], f[i + 1]}, one, sum, false);
+  return sum;
+}
+__device__ __forceinline__ float add_values(const Frag<_Float16> &f, float sum) {
+  typedef _Float16 v2 __attribute__((ext_vector_type(2)));
+  const v2 one = {(_Float16)1.f, (_Float16)1.f};
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) sum = __builtin_amdgcn_fdot2(v2{f[i], f[i + 1]}, one, sum, false);
+  return sum;
+}
+
+// n (maybe <= 0) of 8 elements from memory, the others 0.
+template <class T>
+__device__ __forceinline__ Frag<T> load_frag(const T *p, int n) {
+  if (n >= 8) {
+    Frag<T> f;
+    __builtin_memcpy(&f, p, sizeof f);
+    return f;
+  }
+  Frag<T> f{};
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (i < n) f[i] = p[i];
+  return f;
+}
+// The channels of a row of D as the factor of a product over channels; p is memory whether the row is there or not.
+// whole: D is a number of 16-byte pieces, so that all loads are under way at once.
+template <class T, int DP>
+__device__ __forceinline__ void load_row(Frag<T> (&f)[DP / 16], const T *p, int D, bool whole, int half, bool there) {
+  if (whole) {
+    constexpr int V = 16 / (int)sizeof(T);
+    Pack<T, V> x[DP / 16][8 / V];
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s)
+#pragma unroll
+      for (int i = 0; i < 8 / V; ++i) {
+        const int c = 16 * s + 8 * half + i * V;
+        x[s][i] = load_pack<T, V>(p + (c < D ? c : 0));
+      }
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s) {
+#pragma unroll
+      for (int i = 0; i < 8 / V; ++i)
+        if (!there || 16 * s + 8 * half + i * V >= D) x[s][i] = Pack<T, V>{};
+      f[s] = __builtin_bit_cast(Frag<T>, x[s]);
+    }
+    return;
+  }
+#pragma unroll
+  for (int s = 0; s < DP / 16; ++s) {
+    f[s] = Frag<T>{};
+    if (there) f[s] = load_frag<T>(p + 16 * s + 8 * half, D - 16 * s - 8 * half);
+  }
+}
+
+// A tile on its way from memory to LDS, in 16-byte pieces of its rows; rows whose bit of `there` is not set are 0.
+template <class T, int DP, int TH, int ROWS = attn_keys(sizeof(T))>
+struct Staged {
+  static constexpr int V = 16 / (int)sizeof(T), PR = DP / V, COUNT = ROWS * PR, N = (COUNT + TH - 1) / TH;
+  Pack<T, V> x[N];
+  static __device__ __forceinline__ int row_of(int i) { return ((int)threadIdx.x + i * TH) / PR; }
+  static __device__ __forceinline__ int channel_of(int i) { return ((int)threadIdx.x + i * TH) % PR * V; }
+  // at(i): where the row of piece i begins (memory whether the row is there or not)
+  template <class At>
+  __device__ __forceinline__ void load(At &&at, int D, bool whole, uint64_t there) {
+    if (whole) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] = load_pack<T, V>(at(i) + (channel_of(i) < D ? channel_of(i) : 0));
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int c = channel_of(i);
+        x[i] = Pack<T, V>{};
+        if ((COUNT % TH == 0 || row_of(i) < COUNT / PR) && c < D && (there >> row_of(i) & 1))
+          x[i] = load_some<T, V>(at(i) + c, D - c);
+      }
+    }
+  }
+  __device__ __forceinline__ void store(T *tile, int D, uint64_t there) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if (!(there >> (row_of(i) & 63) & 1) || channel_of(i) >= D) x[i] = Pack<T, V>{};
+      if (COUNT % TH == 0 || row_of(i) < COUNT / PR)
+        *reinterpret_cast<Pack<T, V> *>(tile + row_of(i) * kStride<T, DP> + channel_of(i)) = x[i];
+    }
+  }
+};
+
+// What the kernels share of a call.
+struct Attn {
+  fdc_cross_attention_args a;
+  int per, R;  // query heads a key head, rows a key head
+  int D4;      // channels of a partial result's row
+  float c;     // scale log2(e)
+  bool whole;  // D is a number of 16-byte pieces
+  float *lse;  // [B][H][Lq] (NULL: no backward follows)
+  void *low;   // [rows][D4], 16-bit types: what y's rounding lost, times kLowUp
+};
+// y and its low part are the sum to 16 (bfloat16) or 22 (float16) bits: delta is formed from both, since for a row that reads
+// few keys it nearly cancels against gy . v, and y's rounding alone would be the largest error of gq and gk.  The
+// factor keeps the low part among float16's normal numbers where y is.
+template <class T>
+constexpr float kLowUp = std::is_same_v<T, _Float16> ? 2048.f : 1.f;
+
+// Row r of key head g: a head and a token.
+struct Row {
+  int head, t;
+  bool live;
+};
+__device__ __forceinline__ Row row_of(const Attn &p, int g, int r, int queries) {
+  const int in = min(r, p.R - 1), hh = in / p.a.Lq, t = in - hh * p.a.Lq;
+  return {g * p.per + hh, t, r < p.R && t < queries};
+}
+template <class T>
+__device__ __forceinline__ T *at(const fdc_heads &x, int b, int64_t t, int64_t h) {
+  return static_cast<T *>(x.p) + b * x.batch_stride + t * x.token_stride + h * x.head_stride;
+}
+
+// Which of the 64 keys from key0 sequence b has, the same in every lane.
+__device__ __forceinline__ uint64_t keys_there(const Attn &p, int b, int key0, int keys, int lane, int width) {
+  const int key = key0 + lane;
+  bool there = lane < width && key < keys;
+  if (there && p.a.mask != nullptr) there = p.a.mask[b * p.a.mask_stride + key] != 0;
+  return __ballot(there);
+}
+
+template <int DP, class F>
+__device__ __forceinline__ void each_four(const v16f (&o)[DP / 32], int D, int half, float f, F &&store) {
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int c = 32 * d + 8 * j + 4 * half;
+      const float x[4] = {o[d][4 * j] * f, o[d][4 * j + 1] * f, o[d][4 * j + 2] * f, o[d][4 * j + 3] * f};
+      if (c < D) store(c, x);
+    }
+}
+
+// ---- backward ----------------------------------------------------------------
+// float16's probabilities times 2^15 (at most 2^15): 2^-14 is its least normal number.
+template <class T>
+constexpr float kUpBack = std::is_same_v<T, _Float16> ? 15.f : 0.f;
+
+// The gradients of scores as the factor of a product.  In float16 a column of them is scaled by a power of two
+// of its own, chosen by its largest value so far, so that neither small gradients lose their digits nor large ones overflow;
+// the sums made with them carry it.
+template <class T>
+struct Scaled {
+  float f = 1.f;
+  template <int N>
+  __device__ __forceinline__ void fit(v16f &, v16f (&)[N]) {}
+  __device__ __forceinline__ float undo() const { return 1.f; }
+};
+template <>
+struct Scaled<_Float16> {
+  float f = 0x1p100f;
+  template <int N>
+  __device__ __forceinline__ void fit(v16f &s, v16f (&sums)[N]) {
+    float top = 0.f;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) top = fmaxf(top, fabsf(s[j]));
+    top = halves_max(top);
+    if (__any(top * f > 32768.f)) {
+      // to 2^10 ... 2^11: room for 16 times as large ones
+      const float to = top * f > 32768.f ? ldexpf(1.f, 11 - __builtin_amdgcn_frexp_expf(top)) : f, by = to / f;
+#pragma unroll
+      for (int d = 0; d < N; ++d) sums[d] *= by;
+      f = to;
+    }
+    s *= f;
+  }
+  __device__ __forceinline__ float undo() const { return 1.f / f; }
+};
+
+// ---- host ----------------------------------------------------------------------
+// Workgroups of `waves` waves that have 32 rows (or keys) each, and runs of the tiles they go through.
+struct Cut {
+  int waves, tiles, splits, run;
+};
+inline Cut cut(long long heads, long long own, long long through, int tile, bool eight) {
+  Cut c;
+  c.waves = eight && own > 192 ? 8 : own > 64 ? 4 : 2;
+  c.tiles = (int)ceil_div(own, 32 * c.waves);
+  // two waves a SIMD (2048 on the chip)
+  const long long steps = ceil_div(through, tile), blocks = heads * c.tiles;
+  const long long splits = std::max(1LL, std::min(ceil_div(c.waves == 8 ? 256 : 512, blocks), steps / 2));
+  c.run = (int)ceil_div(steps, splits);
+  c.splits = (int)ceil_div(steps, c.run);
+  return c;
+}
+struct Cuts {
+  Cut fwd, q, kv;
+  long long rows, keys, D4;
+  Cuts(int dtype, int B, int Lq, int Lk, int H, int G, int D) {
+    const long long heads = (long long)B * G, R = (long long)H / G * Lq;
+    const int tile = attn_keys(dtype_size(dtype));
+    // float32's factors are twice as many registers: eight waves of 256 hold 64 channels
+    const bool eight = dtype_size(dtype) == 2 || D <= 64;
+    fwd = q = cut(heads, R, Lk, tile, eight);
+    kv = cut(heads, Lk, R, tile, D <= 64);
+    rows = heads * R, keys = heads * Lk, D4 = ceil_div(D, 4) * 4;
+  }
+  size_t fwd_floats() const { return fwd.splits > 1 ? (size_t)fwd.splits * rows * (D4 + 4) : 0; }
+  size_t stats_floats() const { return (size_t)ceil_div(rows * 2, 4) * 4; }
+  size_t q_floats() const { return q.splits > 1 ? (size_t)q.splits * rows * D4 : 0; }
+  size_t kv_floats() const { return kv.splits > 1 ? (size_t)kv.splits * keys * 2 * D4 : 0; }
+};
+
+inline int64_t lse_floats(int B, int Lq, int H) { return ceil_div((int64_t)B * Lq * H, 4) * 4; }
+inline Attn attn_of(const fdc_cross_attention_args &a, float *saved) {
+  void *low = saved != nullptr && dtype_size(a.dtype) == 2 ? saved + lse_floats(a.B, a.Lq, a.H) : nullptr;
+  return {a, a.H / a.G, a.H / a.G * a.Lq, (a.D + 3) / 4 * 4, a.scale * kLog2e, a.D * dtype_size(a.dtype) % 16 == 0, saved, low};
+}
+
+// f(T{}, padded channels, waves) for the type, channels and waves of a call.
+template <class F>
+hipError_t by_shape(int dtype, int D, int waves, F &&f) {
+  using std::integral_constant;
+  return by_dtype(dtype, [&](auto tag) {
+    auto with = [&](auto dp) {
+      if constexpr (sizeof(tag) == 2 || decltype(dp)::value <= 64)
+        if (waves == 8) return f(tag, dp, integral_constant<int, 8>{});
+      if (waves == 4) return f(tag, dp, integral_constant<int, 4>{});
+      return f(tag, dp, integral_constant<int, 2>{});
+    };
+    if (D <= 32) return with(integral_constant<int, 32>{});
+    if (D <= 64) return with(integral_constant<int, 64>{});
+    if (D <= 96) return with(integral_constant<int, 96>{});
+    return with(integral_constant<int, 128>{});
+  });
+}
+template <auto Kern, class... Args>
+hipError_t launch_tiles(const char *name, long long blocks, int threads, size_t lds, hipStream_t s, Args... args) {
+  if (lds > 65536)
+    if (hipError_t e = allow_lds<Kern>(lds)) return e;
+  return timed_launch(name, Kern, dim3((unsigned)blocks), dim3(threads), lds, s, args...);
+}
+
+}  // namespace attention
+
+// The parts of the backward, in cross_attention_bwd_*.hip.
+hipError_t launch_attention_bwd_q(const attention::Attn &p, const attention::Cut &c, const fdc_heads &gy, const fdc_heads &gq,
+                                  const float2 *stats, float *part, hipStream_t s);
+hipError_t launch_attention_bwd_kv(const attention::Attn &p, const attention::Cut &c, const fdc_heads &gy,
+                                   const fdc_heads &gk, const fdc_heads &gv, const float2 *stats, float *part,
+                                   hipStream_t s);
+
+}  // namespace fdc

@@ -1,0 +1,120 @@
+// Cross attention: the gradient of the queries.
+#include "cross_attention.h"
+
+namespace fdc {
+
+using namespace attention;
+
+namespace {
+
+// gq: a workgroup has 32 W rows and goes through a run of the keys, as the forward does.
+template <class T, int DP, int W>
+__global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_q(Attn p, fdc_heads gy, fdc_heads gq, const float2 *__restrict__ stats,
+                                                       float *__restrict__ part, int row_tiles, int splits, int run) {
+  constexpr int KT = attn_keys(sizeof(T)), S = KT * kStride<T, DP>, NB = KT / 32;
+  extern __shared__ __align__(16) char lds_[];
+  T *lds = reinterpret_cast<T *>(lds_);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+  int id = xcd_remap(blockIdx.x, gridDim.x);
+  const int rt = id % row_tiles;
+  id /= row_tiles;
+  const int split = id % splits, bg = id / splits, b = bg / p.a.G, g = bg - b * p.a.G;
+  const int keys = length_of(p.a.lengths, b, p.a.Lk), queries = length_of(p.a.q_lengths, b, p.a.Lq);
+  const int r = (rt * W + wave) * 32 + (lane & 31);
+  const Row row = row_of(p, g, r, queries);
+  const float2 st = r < p.R ? stats[(int64_t)bg * p.R + r] : float2{INFINITY, 0.f};
+  const bool live = st.x != INFINITY;
+  Frag<T> q[DP / 16], go[DP / 16];
+  load_row<T, DP>(q, at<T>(p.a.q, b, row.t, row.head), p.a.D, p.whole, half, live);
+  load_row<T, DP>(go, at<T>(gy, b, row.t, row.head), p.a.D, p.whole, half, live);
+  v16f o[DP / 32] = {};
+  Scaled<T> scaled;
+  const int first = split * run, last = min(first + run, (keys + KT - 1) / KT);
+  if (first < last && __syncthreads_or(live)) {
+    Staged<T, DP, 64 * W> sk, sv;
+    auto load = [&](int tile, uint64_t there) {
+      const T *k0 = at<T>(p.a.k, b, (int64_t)tile * KT, g), *v0 = at<T>(p.a.v, b, (int64_t)tile * KT, g);
+      const int most = p.a.Lk - 1 - tile * KT;
+      sk.load([&](int i) { return k0 + min(sk.row_of(i), most) * p.a.k.token_stride; }, p.a.D, p.whole, there);
+      sv.load([&](int i) { return v0 + min(sv.row_of(i), most) * p.a.v.token_stride; }, p.a.D, p.whole, there);
+    };
+    uint64_t there = keys_there(p, b, first * KT, keys, lane, KT), next = keys_there(p, b, (first + 1) * KT, keys, lane, KT);
+    load(first, there);
+    sk.store(lds, p.a.D, there), sv.store(lds + S, p.a.D, there);
+    for (int tile = first; tile < last; ++tile) {
+      const T *kt = lds + (tile - first & 1) * 2 * S, *vt = kt + S;
+      __syncthreads();
+      const bool more = tile + 1 < last;
+      uint64_t after = 0;
+      if (more) {
+        load(tile + 1, next);
+        after = keys_there(p, b, (tile + 2) * KT, keys, lane, KT);
+      }
+      if (there != 0) {
+        const bool whole = there == (KT == 64 ? ~0ull : (1ull << KT) - 1);
+        const uint64_t mine = there >> (4 * half);
+#pragma unroll
+        for (int k = 0; k < NB; ++k) {
+          v16f s = {}, e = {};
+          constexpr int H = DP / 32;  // half the steps: at most 32 registers on their way from LDS
+          Rows<T, DP, H> r0, r1;
+          r0.load(kt, 32 * k, 0, lane);
+          r1.load(kt, 32 * k, H, lane);
+          ahead<T>();
+#pragma unroll
+          for (int i = 0; i < H; ++i) mma(s, r0.f[i], q[i]);
+          r0.load(vt, 32 * k, 0, lane);
+          ahead<T>();
+#pragma unroll
+          for (int i = 0; i < H; ++i) mma(s, r1.f[i], q[H + i]);
+          r1.load(vt, 32 * k, H, lane);
+          ahead<T>();
+#pragma unroll
+          for (int i = 0; i < H; ++i) mma(e, r0.f[i], go[i]);
+          Columns<T, DP> cols;
+          cols.load(kt, 32 * k, lane);
+          ahead<T>();
+#pragma unroll
+          for (int i = 0; i < H; ++i) mma(e, r1.f[i], go[H + i]);
+#pragma unroll
+          for (int j = 0; j < 16; ++j) s[j] = exp2_fast(fmaf(s[j], p.c, -st.x)) * (e[j] - st.y);
+          if (!whole) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+              if (!(mine >> (32 * k + 8 * (j / 4) + j % 4) & 1)) s[j] = 0.f;
+          }
+          scaled.fit(s, o);
+          cols.add_to(o, {score_frag<T>(s, 0), score_frag<T>(s, 1)});
+        }
+      }
+      if (more) {
+        T *to = lds + (tile + 1 - first & 1) * 2 * S;
+        sk.store(to, p.a.D, next), sv.store(to + S, p.a.D, next);
+      }
+      there = next, next = after;
+    }
+  }
+  if (r >= p.R) return;
+  const float f = p.a.scale * exp2f(-kUpBack<T>) * scaled.undo();
+  if (splits > 1) {
+    float *to = part + (((int64_t)split * p.a.B * p.a.G + bg) * p.R + r) * p.D4;
+    each_four<DP>(o, p.D4, half, f, [&](int c, const float(&x)[4]) { __builtin_memcpy(to + c, x, sizeof x); });
+    return;
+  }
+  T *to = at<T>(gq, b, row.t, row.head);
+  each_four<DP>(o, p.a.D, half, f, [&](int c, const float(&x)[4]) { store_some<T, 4>(to + c, x, p.a.D - c); });
+}
+
+}  // namespace
+
+hipError_t launch_attention_bwd_q(const Attn &p, const Cut &c, const fdc_heads &gy, const fdc_heads &gq,
+                                  const float2 *stats, float *part, hipStream_t s) {
+  return by_shape(p.a.dtype, p.a.D, c.waves, [&](auto tag, auto dp, auto waves) {
+    using T = decltype(tag);
+    constexpr int DP = decltype(dp)::value, W = decltype(waves)::value;
+    return launch_tiles<k_attn_bwd_q<T, DP, W>>("attn_bwd_q", (long long)p.a.B * p.a.G * c.tiles * c.splits, 64 * W,
+                                                4 * tile_bytes<T, DP>(), s, p, gy, gq, stats, part, c.tiles, c.splits, c.run);
+  });
+}
+
+}  // namespace fdc

@@ -708,4 +708,4 @@ def test_refusals():
     with pytest.raises(ValueError, match="gtop goes with idx"):
         seq.token_logprobs_backward(r.stats, z, gtop=m.f32(3, 2))
     with pytest.raises(FdcError, match="gz shares memory"):
-        seq.token_logprobs_backward(r.stats, z[:2], gentropy=m.f32(2), gz=z[1:])
+        seq.token_logprobs_backward(r.stats[:2], z[:2], gentropy=m.f32(2), gz=z[1:])
