@@ -67,9 +67,10 @@ constexpr int attn_keys(size_t size) { return size == 2 ? 64 : 32; }  // rows of
 // A tile's rows are 32 bytes longer than their channels: 8 rows then begin at 8 different sets of 8 banks.
 template <class T, int DP>
 constexpr int kStride = DP + 32 / (int)sizeof(T);
-template <class T, int DP>
-constexpr size_t tile_bytes() {
-  return (size_t)attn_keys(sizeof(T)) * kStride<T, DP> * sizeof(T);
+// LDS: two buffers of two tiles, and at its beginning and end 32 rows for each wave.
+template <class T, int DP, int W>
+constexpr size_t tiles_bytes() {
+  return (size_t)(4 * attn_keys(sizeof(T)) > 32 * W ? 4 * attn_keys(sizeof(T)) : 32 * W) * kStride<T, DP> * sizeof(T);
 }
 
 // Row `row` of a tile, channels 16 s ... 16 s + 15 of which this lane's half.
@@ -171,34 +172,78 @@ __device__ __forceinline__ Frag<T> load_frag(const T *p, int n) {
     if (i < n) f[i] = p[i];
   return f;
 }
-// The channels of a row of D as the factor of a product over channels; p is memory whether the row is there or not.
-// whole: D is a number of 16-byte pieces, so that all loads are under way at once.
+// A wave's 32 rows between memory and registers, through its own rows of LDS (`area`): memory is read and written in whole
+// lines, 16 bytes a lane, a row's neighbours side by side.  Each lane knows where row l % 32 begins (`offset`, in elements
+// from `base`) and whether it is there.
 template <class T, int DP>
-__device__ __forceinline__ void load_row(Frag<T> (&f)[DP / 16], const T *p, int D, bool whole, int half, bool there) {
-  if (whole) {
-    constexpr int V = 16 / (int)sizeof(T);
-    Pack<T, V> x[DP / 16][8 / V];
+struct WaveRows {
+  static constexpr int V = 16 / (int)sizeof(T), PR = DP / V, N = 32 * PR / 64, S = kStride<T, DP>;
+  // f = the channels of row l % 32 as the factor of a product over channels, 0 where the row is not there (but memory).
+  // whole: D is a number of 16-byte pieces, so that all loads are under way at once.
+  static __device__ __forceinline__ void load(Frag<T> (&f)[DP / 16], T *area, const T *base, int64_t offset, int D, bool whole,
+                                              bool there, int lane) {
+    const uint64_t live = __ballot(there);
+    Pack<T, V> x[N];
+    if (whole) {
 #pragma unroll
-    for (int s = 0; s < DP / 16; ++s)
-#pragma unroll
-      for (int i = 0; i < 8 / V; ++i) {
-        const int c = 16 * s + 8 * half + i * V;
-        x[s][i] = load_pack<T, V>(p + (c < D ? c : 0));
+      for (int i = 0; i < N; ++i) {
+        const int row = (lane + 64 * i) / PR, c = (lane + 64 * i) % PR * V;
+        x[i] = load_pack<T, V>(base + __shfl(offset, row, 64) + (c < D ? c : 0));
       }
+    } else {
 #pragma unroll
-    for (int s = 0; s < DP / 16; ++s) {
-#pragma unroll
-      for (int i = 0; i < 8 / V; ++i)
-        if (!there || 16 * s + 8 * half + i * V >= D) x[s][i] = Pack<T, V>{};
-      f[s] = __builtin_bit_cast(Frag<T>, x[s]);
+      for (int i = 0; i < N; ++i) {
+        const int row = (lane + 64 * i) / PR, c = (lane + 64 * i) % PR * V;
+        const int64_t at = __shfl(offset, row, 64);
+        x[i] = Pack<T, V>{};
+        if (c < D && (live >> row & 1)) x[i] = load_some<T, V>(base + at + c, D - c);
+      }
     }
-    return;
-  }
 #pragma unroll
-  for (int s = 0; s < DP / 16; ++s) {
-    f[s] = Frag<T>{};
-    if (there) f[s] = load_frag<T>(p + 16 * s + 8 * half, D - 16 * s - 8 * half);
+    for (int i = 0; i < N; ++i) {
+      const int row = (lane + 64 * i) / PR, c = (lane + 64 * i) % PR * V;
+      if (!(live >> row & 1) || c >= D) x[i] = Pack<T, V>{};
+      *reinterpret_cast<Pack<T, V> *>(area + row * S + c) = x[i];
+    }
+    wave_sync();
+#pragma unroll
+    for (int i = 0; i < DP / 16; ++i) f[i] = row_frag<T, DP>(area, lane & 31, i, lane >> 5);
+    wave_sync();
   }
+  // Row l % 32 = value(d, j), the lane's four channels 32 d + 8 j + 4 (l / 32) ..., rounded; `there`: whether it is written.
+  template <class F>
+  static __device__ __forceinline__ void store(T *area, T *base, int64_t offset, int D, bool there, int lane, F &&value) {
+    const uint64_t live = __ballot(there);
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float4 x = value(d, j);
+        const float y[4] = {x.x, x.y, x.z, x.w};
+        store_pack<T, 4>(area + (lane & 31) * S + 32 * d + 8 * j + 4 * (lane >> 5), y);
+      }
+    wave_sync();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int row = (lane + 64 * i) / PR, c = (lane + 64 * i) % PR * V;
+      const int64_t at = __shfl(offset, row, 64);
+      const Pack<T, V> x = *reinterpret_cast<const Pack<T, V> *>(area + row * S + c);
+      if (c >= D || !(live >> row & 1)) continue;
+      if (c + V <= D) {
+        __builtin_memcpy(base + at + c, &x, sizeof x);
+      } else {
+        const T *e = area + row * S + c;
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+          if (c + k < D) base[at + c + k] = e[k];
+      }
+    }
+    wave_sync();
+  }
+};
+template <int DP>
+__device__ __forceinline__ float4 four(const v16f (&o)[DP / 32], int d, int j, float f) {
+  return {o[d][4 * j] * f, o[d][4 * j + 1] * f, o[d][4 * j + 2] * f, o[d][4 * j + 3] * f};
 }
 
 // A tile on its way from memory to LDS, in 16-byte pieces of its rows; rows whose bit of `there` is not set are 0.
@@ -258,6 +303,9 @@ struct Row {
 __device__ __forceinline__ Row row_of(const Attn &p, int g, int r, int queries) {
   const int in = min(r, p.R - 1), hh = in / p.a.Lq, t = in - hh * p.a.Lq;
   return {g * p.per + hh, t, r < p.R && t < queries};
+}
+__device__ __forceinline__ int64_t offset_of(const fdc_heads &x, int b, int64_t t, int64_t h) {
+  return b * x.batch_stride + t * x.token_stride + h * x.head_stride;
 }
 template <class T>
 __device__ __forceinline__ T *at(const fdc_heads &x, int b, int64_t t, int64_t h) {

@@ -7,18 +7,10 @@ using namespace attention;
 
 namespace {
 
-// 4 channels of a row of y from c on, and of its low part.
+// What x's rounding loses, as it is kept.
 template <class T>
-__device__ __forceinline__ void store_y(const Attn &p, T *y, int64_t at_row, int c, const float (&x)[4]) {
-  store_some<T, 4>(y + c, x, p.a.D - c);
-  if constexpr (sizeof(T) == 2) {
-    if (p.low != nullptr) {
-      float rest[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) rest[i] = (x[i] - (float)(T)x[i]) * kLowUp<T>;
-      store_pack<T, 4>(static_cast<T *>(p.low) + at_row * p.D4 + c, rest);
-    }
-  }
+__device__ __forceinline__ float low_of(float x) {
+  return (x - (float)(T)x) * kLowUp<T>;
 }
 
 // ---- forward -----------------------------------------------------------------
@@ -48,7 +40,10 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_fwd(Attn p, float *__res
   const int r = (rt * W + wave) * 32 + (lane & 31);
   const Row row = row_of(p, g, r, queries);
   Frag<T> q[DP / 16];
-  load_row<T, DP>(q, at<T>(p.a.q, b, row.t, row.head), p.a.D, p.whole, half, row.live);
+  T *area = lds + wave * 32 * kStride<T, DP>;
+  WaveRows<T, DP>::load(q, area, static_cast<const T *>(p.a.q.p), offset_of(p.a.q, b, row.t, row.head), p.a.D, p.whole, row.live,
+                        lane);
+  __syncthreads();
   v16f o[DP / 32] = {};
   float m = -INFINITY, l = 0.f, w = 0.f;  // the sum, and that of the rounded probabilities
   const int first = split * run, last = min(first + run, (keys + KT - 1) / KT);
@@ -131,8 +126,8 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_fwd(Attn p, float *__res
   }
   l = halves_sum(l);
   w = sizeof(T) == 2 ? halves_sum(w) : l;
-  if (r >= p.R) return;
   if (splits > 1) {
+    if (r >= p.R) return;
     const int64_t at = ((int64_t)split * p.a.B * p.a.G + bg) * p.R + r;
     float *to = part + at * (p.D4 + 4);
     each_four<DP>(o, p.D4, half, 1.f, [&](int c, const float(&x)[4]) { __builtin_memcpy(to + c, x, sizeof x); });
@@ -140,10 +135,18 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_fwd(Attn p, float *__res
     return;
   }
   const float f = !row.live || l == 0.f ? 0.f : 1.f / w;
-  T *y = at<T>(p.a.y, b, row.t, row.head);
   const int64_t at_row = (int64_t)bg * p.R + r;
-  each_four<DP>(o, p.a.D, half, f, [&](int c, const float(&x)[4]) { store_y<T>(p, y, at_row, c, x); });
-  if (p.lse != nullptr && half == 0)
+  __syncthreads();
+  WaveRows<T, DP>::store(area, static_cast<T *>(p.a.y.p), offset_of(p.a.y, b, row.t, row.head), p.a.D, r < p.R, lane,
+                         [&](int d, int j) { return four<DP>(o, d, j, f); });
+  if constexpr (sizeof(T) == 2) {
+    if (p.low != nullptr)
+      WaveRows<T, DP>::store(area, static_cast<T *>(p.low), at_row * p.D4, p.a.D, r < p.R, lane, [&](int d, int j) {
+        const float4 x = four<DP>(o, d, j, f);
+        return float4{low_of<T>(x.x), low_of<T>(x.y), low_of<T>(x.z), low_of<T>(x.w)};
+      });
+  }
+  if (p.lse != nullptr && half == 0 && r < p.R)
     p.lse[at_row] = !row.live || l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l) - kUp<T>) * kLn2;
 }
 
@@ -172,7 +175,13 @@ __global__ __launch_bounds__(256) void k_attn_join(Attn p, const float *__restri
   const float f = !row.live || l == 0.f ? 0.f : 1.f / w;
 #pragma unroll
   for (int j = 0; j < 4; ++j) o[j] *= f;
-  store_y<T>(p, at<T>(p.a.y, b, row.t, row.head), at_row, c, o);
+  store_some<T, 4>(at<T>(p.a.y, b, row.t, row.head) + c, o, p.a.D - c);
+  if constexpr (sizeof(T) == 2) {
+    if (p.low != nullptr) {
+      const float rest[4] = {low_of<T>(o[0]), low_of<T>(o[1]), low_of<T>(o[2]), low_of<T>(o[3])};
+      store_pack<T, 4>(static_cast<T *>(p.low) + at_row * p.D4 + c, rest);
+    }
+  }
   if (p.lse != nullptr && c == 0)
     p.lse[at_row] = !row.live || l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l) - kUp<T>) * kLn2;
 }
@@ -266,7 +275,7 @@ hipError_t launch_cross_attention_fwd(const fdc_cross_attention_args &a, float *
         using T = decltype(tag);
         constexpr int DP = decltype(dp)::value, W = decltype(waves)::value;
         return launch_tiles<k_attn_fwd<T, DP, W>>("attn_fwd", (long long)a.B * a.G * c.tiles * c.splits, 64 * W,
-                                                  4 * tile_bytes<T, DP>(), s, p, ws, c.tiles, c.splits, c.run);
+                                                  tiles_bytes<T, DP, W>(), s, p, ws, c.tiles, c.splits, c.run);
       }))
     return e;
   if (c.splits == 1) return hipSuccess;

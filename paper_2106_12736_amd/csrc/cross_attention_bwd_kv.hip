@@ -13,7 +13,7 @@ namespace {
 // among the products of another.
 template <class T, int DP, int W>
 constexpr size_t bwd_kv_lds() {
-  return 4 * tile_bytes<T, DP>() + 2 * attn_keys(sizeof(T)) * sizeof(float2);
+  return tiles_bytes<T, DP, W>() + 2 * attn_keys(sizeof(T)) * sizeof(float2);
 }
 template <class T, int DP, int W>
 __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_kv(
@@ -22,7 +22,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_kv(
   constexpr int QT = attn_keys(sizeof(T)), S = QT * kStride<T, DP>, NB = QT / 32, NS = DP / 16;
   extern __shared__ __align__(16) char lds_[];
   T *lds = reinterpret_cast<T *>(lds_);
-  float2 *lst = reinterpret_cast<float2 *>(lds + 4 * S);  // the rows' stats, two buffers
+  float2 *lst = reinterpret_cast<float2 *>(lds_ + tiles_bytes<T, DP, W>());  // the rows' stats, two buffers
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
   int id = xcd_remap(blockIdx.x, gridDim.x);
   const int kt = id % key_tiles;
@@ -33,8 +33,10 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_kv(
   const bool there = key < keys && (p.a.mask == nullptr || p.a.mask[b * p.a.mask_stride + key] != 0);
   Frag<T> k[NS], v[NS];
   const int in = min(key, p.a.Lk - 1);
-  load_row<T, DP>(k, at<T>(p.a.k, b, in, g), p.a.D, p.whole, half, there);
-  load_row<T, DP>(v, at<T>(p.a.v, b, in, g), p.a.D, p.whole, half, there);
+  T *area = lds + wave * 32 * kStride<T, DP>;
+  WaveRows<T, DP>::load(k, area, static_cast<const T *>(p.a.k.p), offset_of(p.a.k, b, in, g), p.a.D, p.whole, there, lane);
+  WaveRows<T, DP>::load(v, area, static_cast<const T *>(p.a.v.p), offset_of(p.a.v, b, in, g), p.a.D, p.whole, there, lane);
+  __syncthreads();
   v16f ok[DP / 32] = {}, ov[DP / 32] = {};
   Scaled<T> scaled;
   const int first = split * run, last = min(first + run, (p.R + QT - 1) / QT);
@@ -108,21 +110,23 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_kv(
       live = live_next, next = after;
     }
   }
-  if (key >= p.a.Lk) return;
   if (!there) {  // whatever its zeros for k and v have led to
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) ok[d] = ov[d] = v16f{};
   }
   const float fv = exp2f(-kUpBack<T>), fk = p.a.scale * fv * scaled.undo();
   if (splits > 1) {
+    if (key >= p.a.Lk) return;
     float *to = part + (((int64_t)split * p.a.B * p.a.G + bg) * p.a.Lk + key) * 2 * p.D4;
     each_four<DP>(ok, p.D4, half, fk, [&](int c, const float(&x)[4]) { __builtin_memcpy(to + c, x, sizeof x); });
     each_four<DP>(ov, p.D4, half, fv, [&](int c, const float(&x)[4]) { __builtin_memcpy(to + p.D4 + c, x, sizeof x); });
     return;
   }
-  T *tk = at<T>(gk, b, key, g), *tv = at<T>(gv, b, key, g);
-  each_four<DP>(ok, p.a.D, half, fk, [&](int c, const float(&x)[4]) { store_some<T, 4>(tk + c, x, p.a.D - c); });
-  each_four<DP>(ov, p.a.D, half, fv, [&](int c, const float(&x)[4]) { store_some<T, 4>(tv + c, x, p.a.D - c); });
+  __syncthreads();
+  WaveRows<T, DP>::store(area, static_cast<T *>(gk.p), offset_of(gk, b, in, g), p.a.D, key < p.a.Lk, lane,
+                         [&](int d, int j) { return four<DP>(ok, d, j, fk); });
+  WaveRows<T, DP>::store(area, static_cast<T *>(gv.p), offset_of(gv, b, in, g), p.a.D, key < p.a.Lk, lane,
+                         [&](int d, int j) { return four<DP>(ov, d, j, fv); });
 }
 
 }  // namespace

@@ -25,8 +25,11 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_q(Attn p, fdc_heads 
   const float2 st = r < p.R ? stats[(int64_t)bg * p.R + r] : float2{INFINITY, 0.f};
   const bool live = st.x != INFINITY;
   Frag<T> q[DP / 16], go[DP / 16];
-  load_row<T, DP>(q, at<T>(p.a.q, b, row.t, row.head), p.a.D, p.whole, half, live);
-  load_row<T, DP>(go, at<T>(gy, b, row.t, row.head), p.a.D, p.whole, half, live);
+  T *area = lds + wave * 32 * kStride<T, DP>;
+  WaveRows<T, DP>::load(q, area, static_cast<const T *>(p.a.q.p), offset_of(p.a.q, b, row.t, row.head), p.a.D, p.whole, live,
+                        lane);
+  WaveRows<T, DP>::load(go, area, static_cast<const T *>(gy.p), offset_of(gy, b, row.t, row.head), p.a.D, p.whole, live, lane);
+  __syncthreads();
   v16f o[DP / 32] = {};
   Scaled<T> scaled;
   const int first = split * run, last = min(first + run, (keys + KT - 1) / KT);
@@ -94,15 +97,16 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_q(Attn p, fdc_heads 
       there = next, next = after;
     }
   }
-  if (r >= p.R) return;
   const float f = p.a.scale * exp2f(-kUpBack<T>) * scaled.undo();
   if (splits > 1) {
+    if (r >= p.R) return;
     float *to = part + (((int64_t)split * p.a.B * p.a.G + bg) * p.R + r) * p.D4;
     each_four<DP>(o, p.D4, half, f, [&](int c, const float(&x)[4]) { __builtin_memcpy(to + c, x, sizeof x); });
     return;
   }
-  T *to = at<T>(gq, b, row.t, row.head);
-  each_four<DP>(o, p.a.D, half, f, [&](int c, const float(&x)[4]) { store_some<T, 4>(to + c, x, p.a.D - c); });
+  __syncthreads();
+  WaveRows<T, DP>::store(area, static_cast<T *>(gq.p), offset_of(gq, b, row.t, row.head), p.a.D, r < p.R, lane,
+                         [&](int d, int j) { return four<DP>(o, d, j, f); });
 }
 
 }  // namespace
@@ -113,7 +117,7 @@ hipError_t launch_attention_bwd_q(const Attn &p, const Cut &c, const fdc_heads &
     using T = decltype(tag);
     constexpr int DP = decltype(dp)::value, W = decltype(waves)::value;
     return launch_tiles<k_attn_bwd_q<T, DP, W>>("attn_bwd_q", (long long)p.a.B * p.a.G * c.tiles * c.splits, 64 * W,
-                                                4 * tile_bytes<T, DP>(), s, p, gy, gq, stats, part, c.tiles, c.splits, c.run);
+                                                tiles_bytes<T, DP, W>(), s, p, gy, gq, stats, part, c.tiles, c.splits, c.run);
   });
 }
 
