@@ -64,9 +64,11 @@ __device__ __forceinline__ float halves_sum(float v) {
 }
 
 constexpr int attn_keys(size_t size) { return size == 2 ? 64 : 32; }  // rows of an LDS tile
-// A tile's rows are 32 bytes longer than their channels: 8 rows then begin at 8 different sets of 8 banks.
+// A tile's rows are longer than their channels, so that what is read at once lies in different ones of LDS's 64 banks: for
+// 16-byte reads of a row a lane an odd number of 4 words (at 72 words instead of 76 they take 1.8 times as long), for the
+// transposed reads 4 rows' 8 words apart.
 template <class T, int DP>
-constexpr int kStride = DP + 32 / (int)sizeof(T);
+constexpr int kStride = DP + (sizeof(T) == 4 ? 8 : DP == 32 || DP == 128 ? 24 : 8);
 // LDS: two buffers of two tiles, and at its beginning and end 32 rows for each wave.
 template <class T, int DP, int W>
 constexpr size_t tiles_bytes() {

@@ -67,7 +67,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_fwd(Attn p, float *__res
         load(tile + 1, next);
         after = keys_there(p, b, (tile + 2) * KT, keys, lane, KT);
       }
-      if (there != 0) {
+      {
         v16f s[NB] = {};
         Rows<T, DP, DP / 16> rows[NB];
 #pragma unroll

@@ -44,13 +44,28 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_kv(
   const float2 none{INFINITY, 0.f};
   if (first < last && __syncthreads_or(there)) {
     Staged<T, DP, 64 * W> sq, sg;
-    auto load = [&](int tile, uint64_t live) {
-      auto row_at = [&](const fdc_heads &x, int i) {
-        const Row row = row_of(p, g, tile * QT + sq.row_of(i), 0);
-        return at<T>(x, b, row.t, row.head);
-      };
-      sq.load([&](int i) { return row_at(p.a.q, i); }, p.a.D, p.whole, live);
-      sg.load([&](int i) { return row_at(gy, i); }, p.a.D, p.whole, live);
+    // where the pieces' rows are: a tile further on, as long as that is within the head
+    constexpr int N = Staged<T, DP, 64 * W>::N;
+    int token[N];
+    int64_t q_at[N], g_at[N];
+    auto locate = [&](int i, int r) {
+      const Row row = row_of(p, g, r, 0);
+      token[i] = row.t;
+      q_at[i] = offset_of(p.a.q, b, row.t, row.head), g_at[i] = offset_of(gy, b, row.t, row.head);
+    };
+#pragma unroll
+    for (int i = 0; i < N; ++i) locate(i, first * QT + sq.row_of(i));
+    auto load = [&](uint64_t live) {
+      sq.load([&](int i) { return static_cast<const T *>(p.a.q.p) + q_at[i]; }, p.a.D, p.whole, live);
+      sg.load([&](int i) { return static_cast<const T *>(gy.p) + g_at[i]; }, p.a.D, p.whole, live);
+    };
+    auto advance = [&](int tile) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        token[i] += QT;
+        q_at[i] += QT * p.a.q.token_stride, g_at[i] += QT * gy.token_stride;
+        if (token[i] >= p.a.Lq) locate(i, tile * QT + sq.row_of(i));
+      }
     };
     auto stats_of = [&](int tile) {
       const int r = tile * QT + lane;
@@ -58,7 +73,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_kv(
     };
     float2 st = stats_of(first), next = stats_of(first + 1);
     uint64_t live = __ballot(st.x != INFINITY);
-    load(first, live);
+    load(live);
     sq.store(lds, p.a.D, live), sg.store(lds + S, p.a.D, live);
     if (wave == 0 && lane < QT) lst[lane] = st;
     for (int tile = first; tile < last; ++tile) {
@@ -70,36 +85,44 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_kv(
       const uint64_t live_next = __ballot(next.x != INFINITY);
       float2 after = none;
       if (more) {
-        load(tile + 1, live_next);
+        advance(tile + 1);
+        load(live_next);
         after = stats_of(tile + 2);
       }
-      if (live != 0) {
-        v16f s[NB] = {}, e[NB] = {};
-        Rows<T, DP, NS> rq, rg;
+      {
 #pragma unroll
         for (int q = 0; q < NB; ++q) {
-          rq.load(qt, 32 * q, 0, lane);
-          rg.load(gt, 32 * q, 0, lane);
-          if (q == 0) ahead<T>();
+          v16f s = {}, e = {};
+          constexpr int H = NS / 2;
+          Rows<T, DP, H> r0, r1;
+          r0.load(qt, 32 * q, 0, lane);
+          r1.load(qt, 32 * q, H, lane);
+          ahead<T>();
 #pragma unroll
-          for (int i = 0; i < NS; ++i) mma(s[q], rq.f[i], k[i]);
+          for (int i = 0; i < H; ++i) mma(s, r0.f[i], k[i]);
+          r0.load(gt, 32 * q, 0, lane);
+          ahead<T>();
 #pragma unroll
-          for (int i = 0; i < NS; ++i) mma(e[q], rg.f[i], v[i]);
-        }
+          for (int i = 0; i < H; ++i) mma(s, r1.f[i], k[H + i]);
+          r1.load(gt, 32 * q, H, lane);
+          ahead<T>();
 #pragma unroll
-        for (int q = 0; q < NB; ++q) {
+          for (int i = 0; i < H; ++i) mma(e, r0.f[i], v[i]);
           Columns<T, DP> cols;
           cols.load(gt, 32 * q, lane);
+          ahead<T>();
+#pragma unroll
+          for (int i = 0; i < H; ++i) mma(e, r1.f[i], v[H + i]);
 #pragma unroll
           for (int j = 0; j < 16; ++j) {
             const float2 w = stt[32 * q + 8 * (j / 4) + 4 * half + j % 4];
-            s[q][j] = exp2_fast(fmaf(s[q][j], p.c, -w.x));
-            e[q][j] = s[q][j] * (e[q][j] - w.y);
+            s[j] = exp2_fast(fmaf(s[j], p.c, -w.x));
+            e[j] = s[j] * (e[j] - w.y);
           }
-          cols.add_to(ov, {score_frag<T>(s[q], 0), score_frag<T>(s[q], 1)});
+          cols.add_to(ov, {score_frag<T>(s, 0), score_frag<T>(s, 1)});
           cols.load(qt, 32 * q, lane);
-          scaled.fit(e[q], ok);
-          cols.add_to(ok, {score_frag<T>(e[q], 0), score_frag<T>(e[q], 1)});
+          scaled.fit(e, ok);
+          cols.add_to(ok, {score_frag<T>(e, 0), score_frag<T>(e, 1)});
         }
       }
       if (more) {

@@ -53,7 +53,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_q(Attn p, fdc_heads 
         load(tile + 1, next);
         after = keys_there(p, b, (tile + 2) * KT, keys, lane, KT);
       }
-      if (there != 0) {
+      {
         const bool whole = there == (KT == 64 ? ~0ull : (1ull << KT) - 1);
         const uint64_t mine = there >> (4 * half);
 #pragma unroll
