@@ -11,6 +11,20 @@ namespace {
 // whose q and gy pass through LDS.  k, v and both sums are in registers: 192 of a wave's for 16-bit keys of 128 channels, so that
 // it has a SIMD to itself; the blocks of a tile are independent up to the sums, and the scores of one are formed
 // among the products of another.
+// An order for COUNT products and the vector work that they are independent of: some instructions after each product, which
+// the matrix unit takes 32 cycles for.
+template <class T, int COUNT>
+__device__ __forceinline__ void between() {
+  if constexpr (std::is_same_v<T, __bf16>) {  // float16's scaling branches
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a product
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);  // reads from LDS
+      __builtin_amdgcn_sched_group_barrier(0x402, 6, 0);  // vector instructions
+    }
+  }
+}
+
 template <class T, int DP, int W>
 constexpr size_t bwd_kv_lds() {
   return tiles_bytes<T, DP, W>() + 2 * attn_keys(sizeof(T)) * sizeof(float2);
@@ -22,7 +36,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_kv(
   constexpr int QT = attn_keys(sizeof(T)), S = QT * kStride<T, DP>, NB = QT / 32, NS = DP / 16;
   extern __shared__ __align__(16) char lds_[];
   T *lds = reinterpret_cast<T *>(lds_);
-  float2 *lst = reinterpret_cast<float2 *>(lds_ + tiles_bytes<T, DP, W>());  // the rows' stats, two buffers
+  float *lst = reinterpret_cast<float *>(lds_ + tiles_bytes<T, DP, W>());  // the rows' stats [2][QT], two buffers
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
   int id = xcd_remap(blockIdx.x, gridDim.x);
   const int kt = id % key_tiles;
@@ -75,11 +89,11 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_kv(
     uint64_t live = __ballot(st.x != INFINITY);
     load(live);
     sq.store(lds, p.a.D, live), sg.store(lds + S, p.a.D, live);
-    if (wave == 0 && lane < QT) lst[lane] = st;
+    if (wave == 0 && lane < QT) lst[lane] = st.x, lst[QT + lane] = st.y;
     for (int tile = first; tile < last; ++tile) {
       const int buf = tile - first & 1;
       const T *qt = lds + buf * 2 * S, *gt = qt + S;
-      const float2 *stt = lst + buf * QT;
+      const float *stt = lst + buf * 2 * QT;
       __syncthreads();
       const bool more = tile + 1 < last;
       const uint64_t live_next = __ballot(next.x != INFINITY);
@@ -90,45 +104,72 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_kv(
         after = stats_of(tile + 2);
       }
       {
+        // The vector work of a block (probabilities, gradients of scores) stands among the products of its neighbours: block 0's
+        // among block 1's scores, block 1's among block 0's sums.
+        v16f s[NB], e[NB];
+        Rows<T, DP, NS> rq[NB], rg[NB];
+        Columns<T, DP> cg, cq;
+        float4 lse[4], delta[4];
+        auto read = [&](int q) { rq[q].load(qt, 32 * q, 0, lane), rg[q].load(gt, 32 * q, 0, lane); };
+        auto read_stats = [&](int q) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            lse[i] = *reinterpret_cast<const float4 *>(stt + 32 * q + 8 * i + 4 * half);
+            delta[i] = *reinterpret_cast<const float4 *>(stt + QT + 32 * q + 8 * i + 4 * half);
+          }
+        };
+        auto scores = [&](int q) {
+          s[q] = v16f{}, e[q] = v16f{};
+#pragma unroll
+          for (int i = 0; i < NS; ++i) {
+            mma(s[q], rq[q].f[i], k[i]);
+            mma(e[q], rg[q].f[i], v[i]);
+          }
+        };
+        auto gradients = [&](int q) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float w[4] = {lse[i].x, lse[i].y, lse[i].z, lse[i].w}, y[4] = {delta[i].x, delta[i].y, delta[i].z, delta[i].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              s[q][4 * i + j] = exp2_fast(fmaf(s[q][4 * i + j], p.c, -w[j]));
+              e[q][4 * i + j] = s[q][4 * i + j] * (e[q][4 * i + j] - y[j]);
+            }
+          }
+        };
+        read(0);
+        read_stats(0);
+        ahead<T>();
+        if constexpr (NB > 1) read(NB - 1);
+        scores(0);
+        ahead<T>();
+        cg.load(gt, 0, lane);
+        if constexpr (NB > 1) scores(NB - 1);
+        gradients(0);
+        if constexpr (NB > 1) between<T, 2 * NS>();
+        ahead<T>();
 #pragma unroll
         for (int q = 0; q < NB; ++q) {
-          v16f s = {}, e = {};
-          constexpr int H = NS / 2;
-          Rows<T, DP, H> r0, r1;
-          r0.load(qt, 32 * q, 0, lane);
-          r1.load(qt, 32 * q, H, lane);
-          ahead<T>();
-#pragma unroll
-          for (int i = 0; i < H; ++i) mma(s, r0.f[i], k[i]);
-          r0.load(gt, 32 * q, 0, lane);
-          ahead<T>();
-#pragma unroll
-          for (int i = 0; i < H; ++i) mma(s, r1.f[i], k[H + i]);
-          r1.load(gt, 32 * q, H, lane);
-          ahead<T>();
-#pragma unroll
-          for (int i = 0; i < H; ++i) mma(e, r0.f[i], v[i]);
-          Columns<T, DP> cols;
-          cols.load(gt, 32 * q, lane);
-          ahead<T>();
-#pragma unroll
-          for (int i = 0; i < H; ++i) mma(e, r1.f[i], v[H + i]);
-#pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const float2 w = stt[32 * q + 8 * (j / 4) + 4 * half + j % 4];
-            s[j] = exp2_fast(fmaf(s[j], p.c, -w.x));
-            e[j] = s[j] * (e[j] - w.y);
+          cq.load(qt, 32 * q, lane);
+          if (q + 1 < NB) read_stats(q + 1);
+          cg.add_to(ov, {score_frag<T>(s[q], 0), score_frag<T>(s[q], 1)});
+          if (q + 1 < NB) cg.load(gt, 32 * (q + 1), lane);
+          scaled.fit(e[q], ok);
+          cq.add_to(ok, {score_frag<T>(e[q], 0), score_frag<T>(e[q], 1)});
+          if (q + 1 < NB) {
+            gradients(q + 1);
+            between<T, DP / 8>();
+            ahead<T>();
           }
-          cols.add_to(ov, {score_frag<T>(s, 0), score_frag<T>(s, 1)});
-          cols.load(qt, 32 * q, lane);
-          scaled.fit(e, ok);
-          cols.add_to(ok, {score_frag<T>(e, 0), score_frag<T>(e, 1)});
         }
       }
       if (more) {
         T *to = lds + (buf ^ 1) * 2 * S;
         sq.store(to, p.a.D, live_next), sg.store(to + S, p.a.D, live_next);
-        if (wave == 0 && lane < QT) lst[(buf ^ 1) * QT + lane] = next;
+        if (wave == 0 && lane < QT) {
+          float *to_stats = lst + (buf ^ 1) * 2 * QT + lane;
+          to_stats[0] = next.x, to_stats[QT] = next.y;
+        }
       }
       live = live_next, next = after;
     }
