@@ -4,14 +4,16 @@
 //   l[v] = d[v] - log s,   entropy = log s - u / s  (two terms that are not negative: nothing cancels)
 //   gz[v] = 1/tau ([v = token] glogp + sum_k [v = idx_k] gtop_k - p[v] (glogp + sum gtop) - gentropy p[v] (l[v] + entropy))
 //
-// The forward is a pass over z (HBM-bound): a workgroup holds a row, or a segment of one, in its registers as the 16-byte
-// pieces it loaded.  The K best of them: every thread's largest logit is known from the maximum, and the K-th
-// largest of these is a lower bound of the row's K-th (K threads have one that large), below which all but a few more than
-// K logits lie; those above go to LDS, where each finds its place by counting the ones before it.  Rows where
-// too many lie above (many equal logits) raise the bound by bisection until few enough do; equal logits are told
-// apart by their places.
+// The forward is one pass over z: a workgroup goes through a row, or a segment of one, in chunks of four 16-byte pieces a
+// thread, the next chunk's loads under way; every thread holds the running maximum and sums of its own logits, which
+// are joined at the end.  The K best: of the first chunk every thread's largest logit is known, and the K-th
+// largest of these is a lower bound of the K-th best (K threads have one that large), below which all but a few more
+// than K logits lie; those above go to LDS, where each finds its place by counting the ones before it.  From then on only
+// logits above the K-th best so far are looked at (a chunk's largest logit tells whether there are any), K / j of the
+// j-th chunk where they come in no order.  Where too many lie above (many equal logits, rising ones), the bound is raised by
+// bisection until few enough do; equal logits are told apart by their places.
 //
-// Many rows: a workgroup each; few rows or rows that do not fit: segments, joined by a workgroup a row.
+// Many rows: a workgroup each; few rows: segments, joined by a workgroup a row.
 #include <algorithm>
 
 #include "sequence.h"
@@ -61,7 +63,7 @@ __device__ __forceinline__ void add(Sums &a, const Sums &b, float c) {
 template <int TH>
 struct TopScratch {
   uint32_t maxima[TH];
-  uint64_t found[kMost];
+  uint64_t found[2][kMost];
   int count;
   uint32_t bound;
   int red[2][TH / 64];
@@ -100,81 +102,91 @@ __device__ __forceinline__ int count_all(TopScratch<TH> &t, int n, int turn) {
   return sum;
 }
 
-// Fills t.found with the candidates (at most kMost, the K best among them) and returns how many they are; t.bound and
-// t.count (0) have been written before a barrier.  each(f) calls f(logit, place) for the thread's logits, `largest` is the
-// largest of them, `best` that of the row, odd: the row has NaN.
-template <int TH, class Each>
-__device__ __forceinline__ int find_top(TopScratch<TH> &t, int K, float largest, float best, bool odd, Each &&each) {
-  uint32_t bound = t.bound;
-  if (odd || key_of(largest) >= bound)
+// The logits that are not below a bound: above f, or equal to it and at places up to `last`; NaN is above all, and with `odd`
+// itself the bound.
+struct Bound {
+  float f;
+  bool odd;
+  int last;
+  __device__ __forceinline__ Bound(uint32_t key, int last_) : last(last_) {
+    odd = key > kInfKey;
+    f = key < ~kInfKey ? -INFINITY : of_key(key);
+  }
+  __device__ __forceinline__ bool has(float x, int place) const {
+    const bool early = place <= last, nan = x != x;
+    return (nan & (early | !odd)) | (!odd & ((x > f) | ((x == f) & early)));
+  }
+};
+
+// Adds a chunk's logits from the bound on to t.found[set], which holds `kept`, at least the K best of them where they are
+// too many, and returns how many it holds.  `bound` and t.count (kept) have been written before a barrier.  The chunk is
+// z[from] ... z[end - 1]; largest: the thread's largest, odd: it has NaN; above(f, put) calls put(logit, place) for the thread's
+// logits that are not below f.  What is rare reads the chunk again, so that the registers are those of the common way.
+template <class T, int TH, class Above>
+__device__ __forceinline__ int add_top(TopScratch<TH> &t, int set, int kept, uint32_t bound, int K, float largest, bool odd,
+                                       const T *z, int from, int end, Above &&above) {
+  auto put = [&](float x, int place) {
+    const int at = atomicAdd(&t.count, 1);
+    if (at < kMost) t.found[set][at] = pair_of(key_of(x), place);
+  };
+  auto each = [&](auto &&f) {
+    for (int at = from + (int)threadIdx.x; at < end; at += TH) f((float)z[at], at);
+  };
+  const Bound first(bound, end - 1);
+  if (first.odd || first.f == -INFINITY)
     each([&](float x, int place) {
-      const uint32_t key = key_of(x);
-      if (key >= bound) {
-        const int at = atomicAdd(&t.count, 1);
-        if (at < kMost) t.found[at] = pair_of(key, place);
-      }
+      if (first.has(x, place)) put(x, place);
     });
+  else if (odd || largest >= first.f)
+    above(first.f, put);
   __syncthreads();
   int n = t.count;
   if (n <= kMost) return n;
-  // bisection: K or more logits are not below lo, fewer than K not below hi
-  uint64_t lo = bound, hi = odd ? 1ull << 32 : (uint64_t)key_of(best) + 1;
+  // bisection: K or more logits of the chunk are not below lo, fewer than K not below hi
+  const int most = kMost - kept;
+  n -= kept;
+  uint64_t lo = bound, hi = 1ull << 32;
   int turn = 0;
-  while (hi - lo > 1 && n > kMost) {
-    const uint32_t mid = (uint32_t)((lo + hi) / 2);
-    const float f = of_key(mid);
+  auto count = [&](const Bound &b) {
     int c = 0;
-    if (mid > kInfKey)
-      each([&](float x, int) { c += x != x; });
-    else
-      each([&](float x, int) { c += !(x < f); });
-    c = count_all(t, c, turn++);
+    each([&](float x, int place) { c += b.has(x, place); });
+    return count_all(t, c, turn++);
+  };
+  while (hi - lo > 1 && n > most) {
+    const uint32_t mid = (uint32_t)((lo + hi) / 2);
+    const int c = count(Bound(mid, end - 1));
     if (c >= K)
       lo = mid, n = c;
     else
       hi = mid;
   }
   // too many equal ones: the places up to `last` are enough
-  uint32_t last = 0xffffffffu;
-  if (n > kMost) {
-    const uint32_t key = (uint32_t)lo;
-    uint32_t none = 0;  // the places below `none` are too few
-    last = 1u << 24;
-    while (last > none && n > kMost) {
-      const uint32_t mid = (none + last) / 2;
-      int c = 0;
-      each([&](float x, int place) {
-        const uint32_t k = key_of(x);
-        c += k > key || (k == key && (uint32_t)place <= mid);
-      });
-      c = count_all(t, c, turn++);
-      if (c >= K)
-        last = mid, n = c;
-      else
-        none = mid + 1;
-    }
+  int none = 0, last = end - 1;  // the places below `none` are too few
+  while (last > none && n > most) {
+    const int mid = none + (last - none) / 2, c = count(Bound((uint32_t)lo, mid));
+    if (c >= K)
+      last = mid, n = c;
+    else
+      none = mid + 1;
   }
   __syncthreads();
-  if (threadIdx.x == 0) t.count = 0;
+  if (threadIdx.x == 0) t.count = kept;
   __syncthreads();
+  const Bound b((uint32_t)lo, last);
   each([&](float x, int place) {
-    const uint32_t key = key_of(x);
-    if (key > lo || (key == lo && (uint32_t)place <= last)) {
-      const int at = atomicAdd(&t.count, 1);
-      if (at < kMost) t.found[at] = pair_of(key, place);
-    }
+    if (b.has(x, place)) put(x, place);
   });
   __syncthreads();
   return min(t.count, kMost);
 }
 
-// put(rank, pair) for the K best of the n candidates, each from one thread.
+// put(rank, pair) for the K best of n pairs, each from one thread.
 template <int TH, class Put>
-__device__ __forceinline__ void rank_top(const TopScratch<TH> &t, int n, int K, Put &&put) {
+__device__ __forceinline__ void rank_top(const uint64_t *found, int n, int K, Put &&put) {
   for (int i = threadIdx.x; i < n; i += TH) {
-    const uint64_t mine = t.found[i];
+    const uint64_t mine = found[i];
     int rank = 0;
-    for (int j = 0; j < n; ++j) rank += t.found[j] > mine;
+    for (int j = 0; j < n; ++j) rank += found[j] > mine;
     if (rank < K) put(rank, mine);
   }
 }
@@ -213,62 +225,157 @@ struct Out {
   uint64_t *pairs;  // [R][segments][K]
 };
 
+// Keeps the compiler from holding what one pass over the pieces forms of them (floats, keys) for the next.
+template <class T, int V>
+__device__ __forceinline__ void keep_packed(Pack<T, V> &x) {
+  asm volatile("" : "+v"(x.w[0]), "+v"(x.w[1]), "+v"(x.w[2]), "+v"(x.w[3]));
+}
+
 // A workgroup a segment (of `seg` logits, `segs` a row).
 template <class T, int TH, int NV, bool Top>
 __global__ __launch_bounds__(TH) void k_logprobs(fdc_token_logprobs_args a, Out out, int seg, int segs) {
-  constexpr int V = kLogitV<T>, W = TH / 64;
+  constexpr int V = kLogitV<T>, W = TH / 64, CHUNK = TH * NV * V;
   __shared__ float rmax[W], rs[W], ru[W];
   __shared__ std::conditional_t<Top, TopScratch<TH>, int> scratch;
   const int64_t id = (int64_t)blockIdx.y * 32768 + blockIdx.x;
   const int64_t row = id / segs;
   if (row >= a.R) return;
-  const int part = (int)(id - row * segs), begin = part * seg, count = min(a.V - begin, seg);
+  const int begin = (int)(id - row * segs) * seg, end = min(a.V, begin + seg);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const float c = kLog2e / a.tau;
-  const T *z = static_cast<const T *>(a.z) + row * a.z_stride + begin;
-  Pack<T, V> x[NV];
+  const T *z = static_cast<const T *>(a.z) + row * a.z_stride;
+  // A piece past the end is all -inf; one that the end lies in begins earlier, V logits before the end, and what belongs to
+  // another piece of it is -inf.  (Rows of less than a piece have one, loaded logit by logit.)
+  auto place_of_piece = [&](int at) { return TH == 64 || at + V <= end ? at : end - V; };
+  auto load = [&](Pack<T, V>(&x)[NV], int from) {
+    const unsigned none = sizeof(T) == 4 ? element_bits<T>((T)-INFINITY) : element_bits<T>((T)-INFINITY) * 0x10001u;
+    if (from + CHUNK <= end) {
 #pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    const int at = (k * TH + tid) * V, n = count - at;
-    if (n > 0) {
-      x[k] = load_some<T, V>(z + at, n, -INFINITY);
+      for (int k = 0; k < NV; ++k) x[k] = load_pack<T, V>(z + from + (k * TH + tid) * V);
+    } else if constexpr (TH == 64) {
+      const int n = end - from - tid * V;
+      x[0] = {none, none, none, none};
+      if (n > 0) x[0] = load_some<T, V>(z + from + tid * V, n, -INFINITY);
     } else {
-      const unsigned none = element_bits<T>((T)-INFINITY);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[k].w[i] = sizeof(T) == 4 ? none : none | none << 16;
+      for (int k = 0; k < NV; ++k) x[k] = load_pack<T, V>(z + place_of_piece(from + (k * TH + tid) * V));
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        const int at = from + (k * TH + tid) * V, skip = min(V, at - place_of_piece(at));
+        constexpr int E = 4 / (int)sizeof(T);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (i * E < skip) x[k].w[i] = E == 2 && i * E + 1 >= skip ? (x[k].w[i] & 0xffff0000u) | (none & 0xffffu) : none;
+        }
+      }
     }
-  }
-  float mine = -INFINITY;
-#pragma unroll
-  for (int k = 0; k < NV; ++k)
-#pragma unroll
-    for (int i = 0; i < V; ++i) mine = fmaxf(mine, x[k].at(i));
-  const float wave_best = wave_max(mine);
-  if (lane == 0) rmax[wave] = wave_best;
-  if constexpr (Top) {
-    scratch.maxima[tid] = key_of(mine);
-    if (tid == 0) scratch.count = 0;
-  }
-  __syncthreads();
+  };
+  Pack<T, V> x[NV], next[NV];
+  load(x, begin);
   Sums t{-INFINITY, 0.f, 0.f};
+  int kept = 0, set = 0;
+  uint32_t bound = 0;
+  for (int from = begin; from < end; from += CHUNK) {
+    const bool more = from + CHUNK < end;
+    if (more) load(next, from + CHUNK);
+    float largest = -INFINITY;
 #pragma unroll
-  for (int w = 0; w < W; ++w) t.m = fmaxf(t.m, rmax[w]);
-  if constexpr (Top) {
-    if (wave == W - 1) {
-      const uint32_t b = bound_of<TH>(scratch.maxima, a.K, lane);
-      if (lane == 0) scratch.bound = b;
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int i = 0; i < V; ++i) largest = fmaxf(largest, x[k].at(i));
+    if constexpr (Top) {
+      if (from == begin) {
+        scratch.maxima[tid] = key_of(largest);
+        if (tid == 0) scratch.count = 0;
+        __syncthreads();
+        if (wave == W - 1) {
+          const uint32_t b = bound_of<TH>(scratch.maxima, a.K, lane);
+          if (lane == 0) scratch.bound = b;
+        }
+      }
     }
+    if (largest > t.m) {
+      const float d = t.m == -INFINITY ? 0.f : fmaxf(t.m - largest, kLowest), f = exp2_fast(d * c);
+      t.s *= f;
+      t.u = fmaf(t.s, d, t.u * f);
+      t.m = largest;
+    }
+    // of -inf alone so far (or with NaN): each term is 0 (or NaN)
+    const float base = t.m == -INFINITY ? 0.f : t.m;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      keep_packed(x[k]);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const float d = x[k].at(i) - base, e = exp2_fast(d * c);
+        t.s += e;
+        t.u = fmaf(e, fmaxf(d, kLowest), t.u);  // a place of -inf: 0 times a number
+      }
+      asm volatile("" : "+v"(t.s), "+v"(t.u));  // a piece at a time: its floats die with it
+    }
+    if constexpr (Top) {
+      if (from == begin) {
+        __syncthreads();
+        bound = scratch.bound;
+      }
+      const bool odd = t.s != t.s;
+      if (__syncthreads_or(odd || key_of(largest) >= bound)) {
+        // a bit a logit, 32 at a time; the few that are set find their logits in memory again, not in registers by number
+        auto above = [&](float f, auto &&put) {
+          constexpr int GROUP = 32 / V < NV ? 32 / V : NV;
+#pragma unroll
+          for (int k0 = 0; k0 < NV; k0 += GROUP) {
+            uint32_t bits = 0;
+#pragma unroll
+            for (int k = k0; k < k0 + GROUP; ++k) {
+              keep_packed(x[k]);
+#pragma unroll
+              for (int i = 0; i < V; ++i) bits |= !(x[k].at(i) < f) ? 1u << ((k - k0) * V + i) : 0u;
+              asm volatile("" : "+v"(bits));
+            }
+            while (bits != 0) {
+              const int bit = __builtin_ctz(bits);
+              bits &= bits - 1;
+              const int place = place_of_piece(from + ((k0 + bit / V) * TH + tid) * V) + bit % V;
+              put((float)z[place], place);
+            }
+          }
+        };
+        const int n = add_top<T, TH>(scratch, set, kept, bound, a.K, largest, odd, z, from, min(end, from + CHUNK), above);
+        kept = n;
+        // the K best so far, and the K-th as the bound: later logits have to be above it
+        if (n > a.K + 64 || (from == begin && n >= a.K && more)) {
+          rank_top<TH>(scratch.found[set], n, a.K, [&](int rank, uint64_t pair) {
+            scratch.found[set ^ 1][rank] = pair;
+            if (rank == a.K - 1) {
+              const uint32_t key = (uint32_t)(pair >> 32);
+              scratch.bound = key == 0xffffffffu ? key : key + 1;
+            }
+          });
+          kept = a.K;
+          set ^= 1;
+          __syncthreads();
+          bound = scratch.bound;
+          if (tid == 0) scratch.count = kept;
+        }
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < NV; ++k) x[k] = next[k];
   }
-  // of -inf alone (or with NaN): each term is 0 (or NaN)
-  const float base = t.m == -INFINITY ? 0.f : t.m;
+  // the threads' sums, relative to the largest of all
+  float m = wave_max(t.m);
+  if (lane == 0) rmax[wave] = m;
+  __syncthreads();
+  m = rmax[0];
 #pragma unroll
-  for (int k = 0; k < NV; ++k)
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const float d = x[k].at(i) - base, e = exp2_fast(d * c);
-      t.s += e;
-      t.u = fmaf(e, fmaxf(d, kLowest), t.u);  // a place of -inf: 0 times a number
-    }
+  for (int w = 1; w < W; ++w) m = fmaxf(m, rmax[w]);
+  if (t.m != m && !(t.s == 0.f)) {
+    const float d = t.m == -INFINITY ? 0.f : fmaxf(t.m - m, kLowest), f = exp2_fast(d * c);
+    t.s *= f;
+    t.u = fmaf(t.s, d, t.u * f);
+  }
+  t.m = m;
   t.s = wave_sum(t.s);
   t.u = wave_sum(t.u);
   if (lane == 0) rs[wave] = t.s, ru[wave] = t.u;
@@ -283,25 +390,17 @@ __global__ __launch_bounds__(TH) void k_logprobs(fdc_token_logprobs_args a, Out 
       out.part[id] = {t.m, t.s, t.u, 0.f};
   }
   if constexpr (Top) {
-    const int n = find_top<TH>(scratch, a.K, mine, t.m, t.s != t.s, [&](auto &&f) {
-#pragma unroll
-      for (int k = 0; k < NV; ++k) {
-        const int at = (k * TH + tid) * V;
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-          if (at + i < count) f(x[k].at(i), begin + at + i);
-      }
-    });
+    const uint64_t *found = scratch.found[set];
     if (segs == 1) {
       const Result r(t, a.tau);
-      rank_top<TH>(scratch, n, a.K, [&](int rank, uint64_t pair) {
+      rank_top<TH>(found, kept, a.K, [&](int rank, uint64_t pair) {
         out.idx[row * a.K + rank] = place_of(pair);
         out.top[row * a.K + rank] = r.logp(of_key((uint32_t)(pair >> 32)));
       });
     } else {
       uint64_t *to = out.pairs + id * a.K;
-      rank_top<TH>(scratch, n, a.K, [&](int rank, uint64_t pair) { to[rank] = pair; });
-      for (int k = n + tid; k < a.K; k += TH) to[k] = 0;  // a segment of less than K
+      rank_top<TH>(found, kept, a.K, [&](int rank, uint64_t pair) { to[rank] = pair; });
+      for (int k = kept + tid; k < a.K; k += TH) to[k] = 0;  // a segment of less than K
     }
   }
 }
@@ -352,7 +451,7 @@ __global__ __launch_bounds__(256) void k_logprobs_join(fdc_token_logprobs_args a
     const uint64_t p = pairs[i];
     if (p >= bound && p != 0) {
       const int at = atomicAdd(&t.count, 1);
-      if (at < kMost) t.found[at] = p;
+      if (at < kMost) t.found[0][at] = p;
     }
   }
   __syncthreads();
@@ -377,14 +476,14 @@ __global__ __launch_bounds__(256) void k_logprobs_join(fdc_token_logprobs_args a
       const uint64_t p = pairs[i];
       if (p >= lo && p != 0) {
         const int at = atomicAdd(&t.count, 1);
-        if (at < kMost) t.found[at] = p;
+        if (at < kMost) t.found[0][at] = p;
       }
     }
     __syncthreads();
     n = min(t.count, kMost);
   }
   const Result r(all, a.tau);
-  rank_top<256>(t, n, a.K, [&](int rank, uint64_t pair) {
+  rank_top<256>(t.found[0], n, a.K, [&](int rank, uint64_t pair) {
     out.idx[row * a.K + rank] = place_of(pair);
     out.top[row * a.K + rank] = r.logp(of_key((uint32_t)(pair >> 32)));
   });
@@ -470,16 +569,14 @@ __global__ __launch_bounds__(kGradThreads) void k_logprobs_grad(fdc_token_logpro
 struct Segments {
   int seg, segs;
 };
-// A row a workgroup where it fits the registers (16 pieces of 16 bytes in 512 threads, 8 where segments are cut) and
-// there are rows for every compute unit; else segments, of 1024 pieces at least.
+constexpr int kThreads = 256, kPieces = 4;  // of a chunk
+// A row a workgroup where there are rows for every compute unit; else segments of one chunk or more.
 Segments segments(int dtype, int64_t R, int V) {
-  const int piece = 16 / (int)dtype_size(dtype);
-  const long long pieces = ceil_div(V, piece);
-  long long segs = 1;
-  if (pieces > 512 * 16) segs = ceil_div(pieces, 512 * 8);
-  while (R * segs < 512 && ceil_div(pieces, segs) > 1024) ++segs;
+  const int piece = 16 / (int)dtype_size(dtype), chunk = kThreads * kPieces * piece;
+  const long long chunks = ceil_div(V, chunk);
+  const long long per = std::max(1LL, std::min<long long>(chunks, R * chunks / 1024));  // chunks a segment
   Segments s;
-  s.seg = (int)ceil_div(ceil_div(V, segs), piece) * piece;
+  s.seg = (int)(per * chunk);
   s.segs = (int)ceil_div(V, s.seg);
   return s;
 }
@@ -494,19 +591,13 @@ Segments grad_segments(int dtype, int64_t R, int V) {
 }
 dim3 wide_grid(long long n) { return dim3((unsigned)std::min<long long>(n, 32768), (unsigned)ceil_div(n, 32768)); }
 
-// f(threads, pieces a thread) for segments of `vecs` 16-byte pieces (at most 512 * 16).
+// f(threads, pieces a thread) of a chunk, for segments of `vecs` 16-byte pieces.
 template <class F>
 hipError_t by_pieces(long long vecs, F &&f) {
   using std::integral_constant;
-#define FDC_ROW(TH, NV) \
-  if (vecs <= TH * NV) return f(integral_constant<int, TH>{}, integral_constant<int, NV>{});
-  FDC_ROW(64, 1)
-  FDC_ROW(128, 2)
-  FDC_ROW(256, 4)
-  FDC_ROW(512, 4)
-  FDC_ROW(512, 8)
-#undef FDC_ROW
-  return f(integral_constant<int, 512>{}, integral_constant<int, 16>{});
+  if (vecs <= 64) return f(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+  if (vecs <= kThreads) return f(integral_constant<int, kThreads>{}, integral_constant<int, 1>{});
+  return f(integral_constant<int, kThreads>{}, integral_constant<int, kPieces>{});
 }
 
 }  // namespace
@@ -523,7 +614,7 @@ hipError_t launch_token_logprobs(const fdc_token_logprobs_args &a, float *logp, 
   const Out out{logp, entropy, idx, top, stats, part, reinterpret_cast<uint64_t *>(part + a.R * sg.segs)};
   return by_dtype(a.dtype, [&](auto tag) {
     using T = decltype(tag);
-    if (hipError_t e = by_pieces(ceil_div(sg.seg, kLogitV<T>), [&](auto threads, auto pieces) {
+    if (hipError_t e = by_pieces(ceil_div(std::min(sg.seg, a.V), kLogitV<T>), [&](auto threads, auto pieces) {
           constexpr int TH = decltype(threads)::value, NV = decltype(pieces)::value;
           return timed_launch("logprobs", a.K > 0 ? k_logprobs<T, TH, NV, true> : k_logprobs<T, TH, NV, false>,
                               wide_grid(a.R * sg.segs), dim3(TH), 0, s, a, out, sg.seg, sg.segs);
