@@ -1,4 +1,5 @@
-// What the kernels of cross attention share (cross_attention.hip: forward, cross_attention_bwd_q.hip, cross_attention_bwd_kv.hip).
+// What the kernels of cross attention share (cross_attention.hip: forward, cross_attention_few.hip: forward for few rows,
+// cross_attention_bwd_q.hip, cross_attention_bwd_kv.hip: backward).
 //
 //   s = scale q k^T over the keys a sequence has,  p = exp(s - lse),  y = p v,  lse = log sum exp s
 //   delta = gy . y,  gv = p^T gy,  gs = p (gy v^T - delta),  gq = scale gs k,  gk = scale gs^T q
@@ -335,6 +336,37 @@ __device__ __forceinline__ void each_four(const v16f (&o)[DP / 32], int D, int h
 }
 
 // ---- backward ----------------------------------------------------------------
+// float16's probabilities are held 2^7 times as large, so that small ones keep their digits (2^-14 is its least normal
+// number); they stay below 2^15 with the largest score up to 2^8 past the one they are taken relative to.
+template <class T>
+constexpr float kUp = std::is_same_v<T, _Float16> ? 7.f : 0.f;
+constexpr float kLate = 8.f;
+
+// What x's rounding loses, as it is kept.
+template <class T>
+__device__ __forceinline__ float low_of(float x) {
+  return (x - (float)(T)x) * kLowUp<T>;
+}
+
+// Four channels c ... of a finished row r: its y, what that loses, and its lse, from the sums relative to m.
+template <class T>
+__device__ __forceinline__ void store_row_part(const Attn &p, int g, int b, int64_t at_row, int r, int queries, int c,
+                                               float (&o)[4], float m, float l, float w) {
+  const Row row = row_of(p, g, r, queries);
+  const float f = !row.live || l == 0.f ? 0.f : 1.f / w;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) o[j] *= f;
+  store_some<T, 4>(at<T>(p.a.y, b, row.t, row.head) + c, o, p.a.D - c);
+  if constexpr (sizeof(T) == 2) {
+    if (p.low != nullptr) {
+      const float rest[4] = {low_of<T>(o[0]), low_of<T>(o[1]), low_of<T>(o[2]), low_of<T>(o[3])};
+      store_pack<T, 4>(static_cast<T *>(p.low) + at_row * p.D4 + c, rest);
+    }
+  }
+  if (p.lse != nullptr && c == 0)
+    p.lse[at_row] = !row.live || l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l) - kUp<T>) * kLn2;
+}
+
 // float16's probabilities times 2^15 (at most 2^15): 2^-14 is its least normal number.
 template <class T>
 constexpr float kUpBack = std::is_same_v<T, _Float16> ? 15.f : 0.f;
@@ -375,18 +407,41 @@ struct Scaled<_Float16> {
 struct Cut {
   int waves, tiles, splits, run;
 };
-inline Cut cut(long long heads, long long own, long long through, int tile, bool eight) {
+// together: how many workgroups of four waves a compute unit holds.
+inline Cut cut(long long heads, long long own, long long through, int tile, bool eight, int together) {
   Cut c;
   c.waves = eight && own > 192 ? 8 : own > 64 ? 4 : 2;
   c.tiles = (int)ceil_div(own, 32 * c.waves);
-  // two waves a SIMD (2048 on the chip)
-  const long long steps = ceil_div(through, tile), blocks = heads * c.tiles;
-  const long long splits = std::max(1LL, std::min(ceil_div(c.waves == 8 ? 256 : 512, blocks), steps / 2));
+  // as many as run at once on 256 compute units, not more: what is left over would take as long as the first round
+  const long long steps = ceil_div(through, tile), blocks = heads * c.tiles, most = 256 * (c.waves == 8 ? 1 : together);
+  const long long splits = std::max(1LL, std::min(most / blocks, steps / 2));
   c.run = (int)ceil_div(steps, splits);
   c.splits = (int)ceil_div(steps, c.run);
   return c;
 }
+// Waves of a workgroup of the form for few rows: as many as their registers allow (two a SIMD, four with 16-bit heads of at
+// most 64 channels, one with wide float32 ones).
+template <class T>
+constexpr int few_waves(int DP) {
+  return sizeof(T) == 2 ? 8 : DP <= 32 ? 8 : 4;
+}
+constexpr int kFewRows = 32;
+// Runs of blocks of 32 keys: one launch where a workgroup's keys are at most 512 KB or there are two workgroups for every
+// compute unit, else runs of at least two blocks a wave.
+inline Cut cut_few(int dtype, long long heads, long long keys, int D) {
+  Cut c;
+  const int DP = D <= 32 ? 32 : D <= 64 ? 64 : D <= 96 ? 96 : 128;
+  c.waves = dtype_size(dtype) == 2 ? few_waves<short>(DP) : few_waves<float>(DP);
+  c.tiles = 1;
+  const long long blocks = ceil_div(keys, 32), bytes = keys * D * 2 * (long long)dtype_size(dtype);
+  long long splits = 1;
+  if (bytes > (512 << 10)) splits = std::max(1LL, std::min(ceil_div(512, heads), blocks / (2 * c.waves)));
+  c.run = (int)ceil_div(blocks, splits);
+  c.splits = (int)ceil_div(blocks, c.run);
+  return c;
+}
 struct Cuts {
+  bool few;
   Cut fwd, q, kv;
   long long rows, keys, D4;
   Cuts(int dtype, int B, int Lq, int Lk, int H, int G, int D) {
@@ -394,8 +449,10 @@ struct Cuts {
     const int tile = attn_keys(dtype_size(dtype));
     // float32's factors are twice as many registers: eight waves of 256 hold 64 channels
     const bool eight = dtype_size(dtype) == 2 || D <= 64;
-    fwd = q = cut(heads, R, Lk, tile, eight);
-    kv = cut(heads, Lk, R, tile, D <= 64);
+    q = cut(heads, R, Lk, tile, eight, eight ? 2 : 1);
+    few = R <= kFewRows;
+    fwd = few ? cut_few(dtype, heads, Lk, D) : q;
+    kv = cut(heads, Lk, R, tile, D <= 64, D <= 64 ? 2 : 1);
     rows = heads * R, keys = heads * Lk, D4 = ceil_div(D, 4) * 4;
   }
   size_t fwd_floats() const { return fwd.splits > 1 ? (size_t)fwd.splits * rows * (D4 + 4) : 0; }
@@ -436,7 +493,8 @@ hipError_t launch_tiles(const char *name, long long blocks, int threads, size_t 
 
 }  // namespace attention
 
-// The parts of the backward, in cross_attention_bwd_*.hip.
+// The forward for few rows, in cross_attention_few.hip, and the parts of the backward, in cross_attention_bwd_*.hip.
+hipError_t launch_attention_few(const attention::Attn &p, const attention::Cut &c, float *part, hipStream_t s);
 hipError_t launch_attention_bwd_q(const attention::Attn &p, const attention::Cut &c, const fdc_heads &gy, const fdc_heads &gq,
                                   const float2 *stats, float *part, hipStream_t s);
 hipError_t launch_attention_bwd_kv(const attention::Attn &p, const attention::Cut &c, const fdc_heads &gy,

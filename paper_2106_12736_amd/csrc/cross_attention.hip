@@ -7,19 +7,7 @@ using namespace attention;
 
 namespace {
 
-// What x's rounding loses, as it is kept.
-template <class T>
-__device__ __forceinline__ float low_of(float x) {
-  return (x - (float)(T)x) * kLowUp<T>;
-}
-
 // ---- forward -----------------------------------------------------------------
-// float16's probabilities are held 2^7 times as large, so that small ones keep their digits (2^-14 is its least normal
-// number); they stay below 2^15 with the largest score up to 2^8 past the one they are taken relative to.
-template <class T>
-constexpr float kUp = std::is_same_v<T, _Float16> ? 7.f : 0.f;
-constexpr float kLate = 8.f;
-
 // A workgroup has 32 W rows of a key head, a wave 32 of them, and goes through a run of the keys, whose
 // tiles of k and v pass through LDS in two buffers: the next tile is loaded to registers during a tile's products.
 // y is divided by the sum of the rounded probabilities, so that its weights add up to 1: for a row that reads one key
@@ -159,31 +147,21 @@ __global__ __launch_bounds__(256) void k_attn_join(Attn p, const float *__restri
   const int fours = p.D4 / 4;
   const long long at_row = id / fours;
   const int c = (int)(id - at_row * fours) * 4;
-  const int bg = (int)(at_row / p.R), b = bg / p.a.G, g = bg - b * p.a.G;
-  const Row row = row_of(p, g, (int)(at_row - (long long)bg * p.R), length_of(p.a.q_lengths, b, p.a.Lq));
+  const int bg = (int)(at_row / p.R), b = bg / p.a.G, g = bg - b * p.a.G, r = (int)(at_row - (long long)bg * p.R);
   const int64_t step = (int64_t)p.a.B * p.a.G * p.R * (p.D4 + 4);
   const float *x = part + at_row * (p.D4 + 4);
   float m = -INFINITY, l = 0.f, w = 0.f, o[4] = {};
+#pragma unroll 8
   for (int i = 0; i < splits; ++i) m = fmaxf(m, x[i * step + p.D4]);
+#pragma unroll 8
   for (int i = 0; i < splits; ++i) {
-    const float *y = x + i * step, f = y[p.D4] == m ? 1.f : exp2_fast(y[p.D4] - m);
-    l = fmaf(y[p.D4 + 1], f, l);
-    w = fmaf(y[p.D4 + 2], f, w);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) o[j] = fmaf(y[c + j], f, o[j]);
+    const float4 st = *reinterpret_cast<const float4 *>(x + i * step + p.D4), y = *reinterpret_cast<const float4 *>(x + i * step + c);
+    const float f = st.x == m ? 1.f : exp2_fast(st.x - m);
+    l = fmaf(st.y, f, l);
+    w = fmaf(st.z, f, w);
+    o[0] = fmaf(y.x, f, o[0]), o[1] = fmaf(y.y, f, o[1]), o[2] = fmaf(y.z, f, o[2]), o[3] = fmaf(y.w, f, o[3]);
   }
-  const float f = !row.live || l == 0.f ? 0.f : 1.f / w;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) o[j] *= f;
-  store_some<T, 4>(at<T>(p.a.y, b, row.t, row.head) + c, o, p.a.D - c);
-  if constexpr (sizeof(T) == 2) {
-    if (p.low != nullptr) {
-      const float rest[4] = {low_of<T>(o[0]), low_of<T>(o[1]), low_of<T>(o[2]), low_of<T>(o[3])};
-      store_pack<T, 4>(static_cast<T *>(p.low) + at_row * p.D4 + c, rest);
-    }
-  }
-  if (p.lse != nullptr && c == 0)
-    p.lse[at_row] = !row.live || l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l) - kUp<T>) * kLn2;
+  store_row_part<T>(p, g, b, at_row, r, length_of(p.a.q_lengths, b, p.a.Lq), c, o, m, l, w);
 }
 
 // ---- backward ----------------------------------------------------------------
@@ -229,10 +207,11 @@ __global__ __launch_bounds__(256) void k_attn_sum(Attn p, const float *__restric
   const int bg = (int)(at_row / n), b = bg / p.a.G, g = bg - b * p.a.G, r = (int)(at_row - (long long)bg * n);
   const float *x = part + at_row * (fours * 4) + c;
   float o[4] = {};
+  const int64_t step = (int64_t)p.a.B * p.a.G * n * fours * 4;
+#pragma unroll 8
   for (int i = 0; i < splits; ++i) {
-    const float *y = x + i * ((int64_t)p.a.B * p.a.G * n * fours * 4);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) o[j] += y[j];
+    const float4 y = *reinterpret_cast<const float4 *>(x + i * step);
+    o[0] += y.x, o[1] += y.y, o[2] += y.z, o[3] += y.w;
   }
   if constexpr (Keys) {
     const bool second = c >= p.D4;
@@ -249,7 +228,7 @@ __global__ __launch_bounds__(256) void k_attn_sum(Attn p, const float *__restric
 // The largest number of workgroups of a launch: below 2^31, and below 2^32 threads.
 bool cross_attention_fits(int dtype, int B, int Lq, int Lk, int H, int G, int D) {
   const Cuts c(dtype, B, Lq, Lk, H, G, D);
-  const long long most = (1LL << 32) / 512 - 1, heads = (long long)B * G;
+  const long long most = (1LL << 32) / 1024 - 1, heads = (long long)B * G;
   if (c.rows >= 1LL << 36 || c.keys >= 1LL << 36) return false;
   return heads * c.fwd.tiles * c.fwd.splits <= most && heads * c.kv.tiles * c.kv.splits <= most &&
          c.rows * c.D4 / 4 < (1LL << 32) - 256 && c.keys * 2 * c.D4 / 4 < (1LL << 32) - 256;
@@ -271,13 +250,16 @@ hipError_t launch_cross_attention_fwd(const fdc_cross_attention_args &a, float *
   const Attn p = attn_of(a, saved);
   const Cuts cuts(a.dtype, a.B, a.Lq, a.Lk, a.H, a.G, a.D);
   const Cut &c = cuts.fwd;
-  if (hipError_t e = by_shape(a.dtype, a.D, c.waves, [&](auto tag, auto dp, auto waves) {
+  if (cuts.few) {
+    if (hipError_t e = launch_attention_few(p, c, ws, s)) return e;
+  } else if (hipError_t e = by_shape(a.dtype, a.D, c.waves, [&](auto tag, auto dp, auto waves) {
         using T = decltype(tag);
         constexpr int DP = decltype(dp)::value, W = decltype(waves)::value;
         return launch_tiles<k_attn_fwd<T, DP, W>>("attn_fwd", (long long)a.B * a.G * c.tiles * c.splits, 64 * W,
                                                   tiles_bytes<T, DP, W>(), s, p, ws, c.tiles, c.splits, c.run);
-      }))
+             })) {
     return e;
+  }
   if (c.splits == 1) return hipSuccess;
   const long long total = cuts.rows * (p.D4 / 4);
   return by_dtype(a.dtype, [&](auto tag) {

@@ -119,8 +119,9 @@ hipError_t launch_rotary(const fdc_rotary_args &a, hipStream_t s) {
     int P = 0;
     for (int i = 0; i < a.axes; ++i) P += a.pairs[i];
     const int turned = (int)ceil_div(P, VP), pieces = turned + (int)ceil_div(a.D - 2 * P, 2 * VP);
-    // as many heads a thread as leave the chip's 256 compute units four waves each of their 16
-    int heads = a.H;
+    // up to 4 heads a thread (32768 tokens of 16 x 128 bf16: 64 us, with 16 heads 78, with 2 63), fewer for what would not
+    // fill the chip's 256 compute units with 16 waves each
+    int heads = std::min(a.H, 4);
     while (heads > 1 && (long long)a.B * a.L * pieces * ceil_div(a.H, heads) < 256 * 16 * 64) heads = (heads + 1) / 2;
     const int runs = (int)ceil_div(a.H, heads);
     const long long total = (long long)a.B * a.L * pieces * runs, blocks = ceil_div(total, kRotaryThreads);

@@ -60,9 +60,13 @@ __device__ __forceinline__ void add(Sums &a, const Sums &b, float c) {
   a.m = m;
 }
 
+// The largest logits that a first bound is found from: of every thread, or of four adjacent ones.
+template <int TH>
+constexpr int kMaxima = TH < 256 ? TH : 256;
+
 template <int TH>
 struct TopScratch {
-  uint32_t maxima[TH];
+  uint32_t maxima[kMaxima<TH>];
   uint64_t found[2][kMost];
   int count;
   uint32_t bound;
@@ -72,8 +76,8 @@ struct TopScratch {
 // By one wave: a key that at least K of the maxima are not below, few of them if there is one (0: all).
 template <int TH>
 __device__ __forceinline__ uint32_t bound_of(const uint32_t *maxima, int K, int lane) {
-  constexpr int N = TH / 64;
-  if (K > TH) return 0;
+  constexpr int N = kMaxima<TH> / 64;
+  if (K > kMaxima<TH>) return 0;
   uint32_t mine[N], bound = 0;
 #pragma unroll
   for (int i = 0; i < N; ++i) mine[i] = maxima[i * 64 + lane];
@@ -233,7 +237,7 @@ __device__ __forceinline__ void keep_packed(Pack<T, V> &x) {
 
 // A workgroup a segment (of `seg` logits, `segs` a row).
 template <class T, int TH, int NV, bool Top>
-__global__ __launch_bounds__(TH) void k_logprobs(fdc_token_logprobs_args a, Out out, int seg, int segs) {
+__global__ __launch_bounds__(TH, NV > 1 ? 8 : 1) void k_logprobs(fdc_token_logprobs_args a, Out out, int seg, int segs) {
   constexpr int V = kLogitV<T>, W = TH / 64, CHUNK = TH * NV * V;
   __shared__ float rmax[W], rs[W], ru[W];
   __shared__ std::conditional_t<Top, TopScratch<TH>, int> scratch;
@@ -285,7 +289,13 @@ __global__ __launch_bounds__(TH) void k_logprobs(fdc_token_logprobs_args a, Out 
       for (int i = 0; i < V; ++i) largest = fmaxf(largest, x[k].at(i));
     if constexpr (Top) {
       if (from == begin) {
-        scratch.maxima[tid] = key_of(largest);
+        if constexpr (TH == 1024) {
+          float four = fmaxf(largest, dpp<0xB1>(largest));
+          four = fmaxf(four, dpp<0x4E>(four));
+          if (tid % 4 == 0) scratch.maxima[tid / 4] = key_of(four);
+        } else {
+          scratch.maxima[tid] = key_of(largest);
+        }
         if (tid == 0) scratch.count = 0;
         __syncthreads();
         if (wave == W - 1) {
@@ -568,14 +578,18 @@ __global__ __launch_bounds__(kGradThreads) void k_logprobs_grad(fdc_token_logpro
 // ---- host ----------------------------------------------------------------------
 struct Segments {
   int seg, segs;
+  bool wide;
 };
-constexpr int kThreads = 256, kPieces = 4;  // of a chunk
-// A row a workgroup where there are rows for every compute unit; else segments of one chunk or more.
+constexpr int kThreads = 256, kManyThreads = 1024, kPieces = 4;  // of a chunk
+// A row a workgroup where there are rows for every compute unit, and for fewer ones of at most 256 KB, in workgroups of 1024
+// threads (7 rows of 50021 f32: one launch without a workspace instead of two); else segments of one chunk or more.
 Segments segments(int dtype, int64_t R, int V) {
   const int piece = 16 / (int)dtype_size(dtype), chunk = kThreads * kPieces * piece;
   const long long chunks = ceil_div(V, chunk);
-  const long long per = std::max(1LL, std::min<long long>(chunks, R * chunks / 1024));  // chunks a segment
+  long long per = std::max(1LL, std::min<long long>(chunks, R * chunks / 1024));  // chunks a segment
   Segments s;
+  s.wide = per < chunks && V * (long long)dtype_size(dtype) <= 256 << 10;
+  if (s.wide) per = chunks;
   s.seg = (int)(per * chunk);
   s.segs = (int)ceil_div(V, s.seg);
   return s;
@@ -584,7 +598,7 @@ Segments grad_segments(int dtype, int64_t R, int V) {
   const int unit = kGradThreads * 16 / (int)dtype_size(dtype);
   long long per = ceil_div(V, unit);
   while (per > 1 && R * ceil_div(V, per * unit) < 2048) per = ceil_div(per, 2);
-  Segments s;
+  Segments s{};
   s.seg = (int)(per * unit);
   s.segs = (int)ceil_div(V, s.seg);
   return s;
@@ -593,8 +607,9 @@ dim3 wide_grid(long long n) { return dim3((unsigned)std::min<long long>(n, 32768
 
 // f(threads, pieces a thread) of a chunk, for segments of `vecs` 16-byte pieces.
 template <class F>
-hipError_t by_pieces(long long vecs, F &&f) {
+hipError_t by_pieces(long long vecs, bool wide, F &&f) {
   using std::integral_constant;
+  if (wide) return f(integral_constant<int, kManyThreads>{}, integral_constant<int, kPieces>{});
   if (vecs <= 64) return f(integral_constant<int, 64>{}, integral_constant<int, 1>{});
   if (vecs <= kThreads) return f(integral_constant<int, kThreads>{}, integral_constant<int, 1>{});
   return f(integral_constant<int, kThreads>{}, integral_constant<int, kPieces>{});
@@ -614,7 +629,7 @@ hipError_t launch_token_logprobs(const fdc_token_logprobs_args &a, float *logp, 
   const Out out{logp, entropy, idx, top, stats, part, reinterpret_cast<uint64_t *>(part + a.R * sg.segs)};
   return by_dtype(a.dtype, [&](auto tag) {
     using T = decltype(tag);
-    if (hipError_t e = by_pieces(ceil_div(std::min(sg.seg, a.V), kLogitV<T>), [&](auto threads, auto pieces) {
+    if (hipError_t e = by_pieces(ceil_div(std::min(sg.seg, a.V), kLogitV<T>), sg.wide, [&](auto threads, auto pieces) {
           constexpr int TH = decltype(threads)::value, NV = decltype(pieces)::value;
           return timed_launch("logprobs", a.K > 0 ? k_logprobs<T, TH, NV, true> : k_logprobs<T, TH, NV, false>,
                               wide_grid(a.R * sg.segs), dim3(TH), 0, s, a, out, sg.seg, sg.segs);
