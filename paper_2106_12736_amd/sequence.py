@@ -363,27 +363,42 @@ def distill_forward_backward(gloss, z, idx, teacher, temperature=1.0, labels=Non
 # ----------------------------------------------------------------------------
 # rotary positions
 # ----------------------------------------------------------------------------
+@lru_cache(maxsize=4096)
+def _pairs(sections, freqs_shape):
+    """The number of axes and the pairs of each, as the C ABI takes them."""
+    if sections is None and len(freqs_shape) == 1:
+        sections = tuple(freqs_shape)
+    if sections is None or not 1 <= len(sections) <= 4 or tuple(freqs_shape) != (sum(sections),):
+        raise ValueError(f"sections are the pairs of 1 to 4 axes, and freqs has one a pair (got {sections}, {tuple(freqs_shape)})")
+    return len(sections), (ctypes.c_int * 4)(*sections)
+
+
 def _rotary(x, positions, freqs, sections, interleaved, lengths, y, inverse):
     dt = _kind(x, "x")
     shape = x.shape
-    if len(shape) not in (3, 4):
+    if len(shape) == 4:
+        B, L, H, D = shape
+    elif len(shape) == 3:
+        (B, H, D), L = shape, 1
+    else:
         raise ValueError(f"x must be [B, L, H, D] or [B, H, D] (got {tuple(shape)})")
-    B, L, (H, D) = shape[0], shape[1] if len(shape) == 4 else 1, shape[-2:]
-    sections = (freqs.shape[0],) if sections is None and freqs.dim() == 1 else tuple(sections or ())
-    if not 1 <= len(sections) <= 4 or freqs.dim() != 1 or freqs.shape[0] != sum(sections):
-        raise ValueError(f"sections are the pairs of 1 to 4 axes, and freqs has one a pair (got {sections}, {tuple(freqs.shape)})")
-    want = shape[:-2] + (len(sections),)
-    one = positions.dim() == 2 and len(shape) == 4  # the same for every sequence
-    if positions.dtype != torch.int32 or positions.device != x.device or positions.shape != (want[1:] if one else want):
+    axes, pairs = _pairs(sections if sections is None else tuple(sections), freqs.shape)
+    got, s = positions.shape, positions.stride()
+    want = (B, L, axes) if len(shape) == 4 else (B, axes)
+    if len(shape) == 3:
+        batch, token = s[0], 0
+    elif len(got) == 2:  # the same for every sequence
+        want, batch, token = (L, axes), 0, s[0]
+    else:
+        batch, token = s[0], s[1] if len(s) > 1 else 0
+    if got != want or positions.dtype != torch.int32 or positions.get_device() != x.get_device():
         _wrong(positions, torch.int32, x.device, want, "positions")
-    s = positions.stride()
-    if s[-1] != 1 and want[-1] > 1:
+    if s[-1] != 1 and axes > 1:
         raise ValueError("positions' last dimension must be dense")
     y = _like(x) if y is None else y
-    a = RotaryArgs(dt, B, L, H, D, len(sections), interleaved, inverse, (ctypes.c_int * 4)(*sections),
-                   _heads(x, x, shape, "x"), _heads(y, x, shape, "y"), positions.data_ptr(), 0 if one else s[0],
-                   s[-2] if len(shape) == 4 else 0, _f32(freqs, x, freqs.shape, "freqs"), _i32(lengths, x, (B,), "lengths"))
-    call("fdc_rotary", a, _stream())
+    call("fdc_rotary", RotaryArgs(dt, B, L, H, D, axes, interleaved, inverse, pairs, _heads(x, x, shape, "x"),
+                                  _heads(y, x, shape, "y"), positions.data_ptr(), batch, token,
+                                  _f32(freqs, x, freqs.shape, "freqs"), _i32(lengths, x, (B,), "lengths")), _stream())
     return y
 
 
@@ -406,21 +421,25 @@ def rotary_backward(gy, positions, freqs, sections=None, interleaved=False, leng
 def _attention_args(q, k, v, scale, q_lengths, lengths, mask, y):
     dt = _kind(q, "q")
     shape, kept = q.shape, k.shape
-    if len(shape) not in (3, 4) or len(kept) != 4:
-        raise ValueError(f"q must be [B, Lq, H, D] or [B, H, D], k and v [B, Lk, G, D] (got {tuple(shape)}, {tuple(kept)})")
-    B, (H, D) = shape[0], shape[-2:]
-    kept = (B, kept[1], kept[2], D)
+    if len(kept) != 4:
+        raise ValueError(f"k and v must be [B, Lk, G, D] (got {tuple(kept)})")
+    _, Lk, G, _ = kept
+    if len(shape) == 4:
+        B, Lq, H, D = shape
+    else:
+        (B, H, D), Lq = shape, 1
+    kept = (B, Lk, G, D)
     if mask is None:
         mp, ms = None, 0
     else:
         if mask.dtype not in (torch.bool, torch.uint8):
             raise ValueError(f"mask must be bool or uint8 (got {mask.dtype})")
-        if mask.device != q.device or mask.shape != kept[:2]:
-            _wrong(mask, mask.dtype, q.device, kept[:2], "mask")
+        if mask.get_device() != q.get_device() or mask.shape != (B, Lk):
+            _wrong(mask, mask.dtype, q.device, (B, Lk), "mask")
         mp, (ms, inner) = mask.data_ptr(), mask.stride()
-        if inner != 1 and kept[1] > 1:
+        if inner != 1 and Lk > 1:
             raise ValueError("mask's last dimension must be dense")
-    return CrossAttentionArgs(dt, B, shape[1] if len(shape) == 4 else 1, kept[1], H, kept[2], D,
+    return CrossAttentionArgs(dt, B, Lq, Lk, H, G, D,
                               D ** -0.5 if scale is None else scale, _heads(q, q, shape, "q"), _heads(k, q, kept, "k"),
                               _heads(v, q, kept, "v"), _heads(y, q, shape, "y"), _i32(q_lengths, q, (B,), "q_lengths"),
                               _i32(lengths, q, (B,), "lengths"), mp, ms)
