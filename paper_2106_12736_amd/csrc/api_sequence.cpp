@@ -1,5 +1,6 @@
 // C ABI of the sequence operators: argument validation and workspaces.  Every entry point
 // validates on the host first and returns before enqueuing anything when an argument is wrong.
+#include <algorithm>
 #include <cmath>
 #include <cstdlib>
 #include <utility>
@@ -100,7 +101,8 @@ fdc_status check_heads(const fdc_heads &x, const char *name, int B, int L, int h
   if (x.batch_stride < 0 || x.token_stride < 0 || x.head_stride < 0)
     return fail(FDC_EINVAL, "%s: strides must not be negative (got %lld, %lld, %lld)", name, (long long)x.batch_stride,
                 (long long)x.token_stride, (long long)x.head_stride);
-  if (x.token_stride >= kMaxTokenStride || x.head_stride >= kMaxHeadStride || x.batch_stride >= kMaxElements)
+  if ((L > 1 && x.token_stride >= kMaxTokenStride) || (heads > 1 && x.head_stride >= kMaxHeadStride) ||
+      (B > 1 && x.batch_stride >= kMaxElements))
     return fail(FDC_EUNSUPPORTED, "%s: strides %lld, %lld, %lld too large", name, (long long)x.batch_stride,
                 (long long)x.token_stride, (long long)x.head_stride);
   if (output) {
@@ -118,7 +120,8 @@ fdc_status check_heads(const fdc_heads &x, const char *name, int B, int L, int h
 }
 
 // Whether an output of these heads (whose elements are apart) and an input of the same strides share memory: as for
-// fdc_tokens, with one more axis, and numbers of tokens and heads of their own.
+// fdc_tokens, with one more axis, and numbers of tokens and heads of their own.  With other strides, and where the input's
+// elements are not apart either, only the same address is seen.
 struct HeadShape {
   const fdc_heads &x;
   const char *name;
@@ -144,6 +147,12 @@ fdc_status check_heads_apart(const HeadShape &out, const HeadShape &in, int64_t 
     for (int i = 0; i < 2; ++i)
       for (int j = 0; j < 2 - i; ++j)
         if (axes[j].stride < axes[j + 1].stride) std::swap(axes[j], axes[j + 1]);
+    int64_t extent = D * size;
+    for (int i = 2; i >= 0; --i) {
+      if (axes[i].stride == 0) continue;
+      if (axes[i].stride < extent) return FDC_OK;
+      extent += (std::max(axes[i].outs, axes[i].ins) - 1) * axes[i].stride;
+    }
     // a step along an axis, either way, that leaves less than its stride of a distance
     auto meets = [&](auto &&self, int i, int64_t distance) -> bool {
       if (i == 3) return distance < D * size && -distance < D * size;

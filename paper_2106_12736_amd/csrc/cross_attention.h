@@ -467,13 +467,14 @@ inline Attn attn_of(const fdc_cross_attention_args &a, float *saved) {
   return {a, a.H / a.G, a.H / a.G * a.Lq, (a.D + 3) / 4 * 4, a.scale * kLog2e, a.D * dtype_size(a.dtype) % 16 == 0, saved, low};
 }
 
-// f(T{}, padded channels, waves) for the type, channels and waves of a call.
-template <class F>
+// f(T{}, padded channels, waves) for the type, channels and waves of a call; `Eight`: eight waves with 16-bit heads of over 64
+// channels, too.
+template <bool Eight, class F>
 hipError_t by_shape(int dtype, int D, int waves, F &&f) {
   using std::integral_constant;
   return by_dtype(dtype, [&](auto tag) {
     auto with = [&](auto dp) {
-      if constexpr (sizeof(tag) == 2 || decltype(dp)::value <= 64)
+      if constexpr ((Eight && sizeof(tag) == 2) || decltype(dp)::value <= 64)
         if (waves == 8) return f(tag, dp, integral_constant<int, 8>{});
       if (waves == 4) return f(tag, dp, integral_constant<int, 4>{});
       return f(tag, dp, integral_constant<int, 2>{});

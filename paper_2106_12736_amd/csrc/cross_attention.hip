@@ -252,7 +252,7 @@ hipError_t launch_cross_attention_fwd(const fdc_cross_attention_args &a, float *
   const Cut &c = cuts.fwd;
   if (cuts.few) {
     if (hipError_t e = launch_attention_few(p, c, ws, s)) return e;
-  } else if (hipError_t e = by_shape(a.dtype, a.D, c.waves, [&](auto tag, auto dp, auto waves) {
+  } else if (hipError_t e = by_shape<true>(a.dtype, a.D, c.waves, [&](auto tag, auto dp, auto waves) {
         using T = decltype(tag);
         constexpr int DP = decltype(dp)::value, W = decltype(waves)::value;
         return launch_tiles<k_attn_fwd<T, DP, W>>("attn_fwd", (long long)a.B * a.G * c.tiles * c.splits, 64 * W,

@@ -197,7 +197,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_kv(
 
 hipError_t launch_attention_bwd_kv(const Attn &p, const Cut &c, const fdc_heads &gy, const fdc_heads &gk,
                                    const fdc_heads &gv, const float2 *stats, float *part, hipStream_t s) {
-  return by_shape(p.a.dtype, p.a.D, c.waves, [&](auto tag, auto dp, auto waves) {
+  return by_shape<false>(p.a.dtype, p.a.D, c.waves, [&](auto tag, auto dp, auto waves) {
     using T = decltype(tag);
     constexpr int DP = decltype(dp)::value, W = decltype(waves)::value;
     return launch_tiles<k_attn_bwd_kv<T, DP, W>>("attn_bwd_kv", (long long)p.a.B * p.a.G * c.tiles * c.splits, 64 * W,

@@ -113,7 +113,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_q(Attn p, fdc_heads 
 
 hipError_t launch_attention_bwd_q(const Attn &p, const Cut &c, const fdc_heads &gy, const fdc_heads &gq,
                                   const float2 *stats, float *part, hipStream_t s) {
-  return by_shape(p.a.dtype, p.a.D, c.waves, [&](auto tag, auto dp, auto waves) {
+  return by_shape<true>(p.a.dtype, p.a.D, c.waves, [&](auto tag, auto dp, auto waves) {
     using T = decltype(tag);
     constexpr int DP = decltype(dp)::value, W = decltype(waves)::value;
     return launch_tiles<k_attn_bwd_q<T, DP, W>>("attn_bwd_q", (long long)p.a.B * p.a.G * c.tiles * c.splits, 64 * W,

@@ -527,13 +527,15 @@ __global__ __launch_bounds__(kGradThreads) void k_logprobs_grad(fdc_token_logpro
     logit[k] = v >= 0 && v < a.V ? (float)z[v] : 0.f;
   }
   __syncthreads();
+  // every wave for itself: the entries' sum, and whether one is not 0, or names a place past the vocabulary
   float alike = 0.f;
-  bool any = false, over = false;
-  for (int k = 0; k <= K; ++k) {
+  int flags = 0;
+  for (int k = tid & 63; k <= K; k += 64) {
     alike += target[k];
-    any = any || target[k] != 0.f;
-    over = over || place[k] >= a.V;
+    flags |= (target[k] != 0.f ? 1 : 0) | (place[k] >= a.V ? 2 : 0);
   }
+  alike = wave_sum(alike);
+  const bool any = __any(flags & 1), over = __any(flags & 2);
   const float gh = gentropy != nullptr ? gentropy[row] : 0.f;
   const int begin = blockIdx.x * seg, end = min(a.V, begin + seg);
   if (!any && gh == 0.f) {
