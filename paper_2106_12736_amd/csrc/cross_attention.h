@@ -181,12 +181,10 @@ __device__ __forceinline__ Frag<T> load_frag(const T *p, int n) {
 template <class T, int DP>
 struct WaveRows {
   static constexpr int V = 16 / (int)sizeof(T), PR = DP / V, N = 32 * PR / 64, S = kStride<T, DP>;
-  // f = the channels of row l % 32 as the factor of a product over channels, 0 where the row is not there (but memory).
-  // whole: D is a number of 16-byte pieces, so that all loads are under way at once.
-  static __device__ __forceinline__ void load(Frag<T> (&f)[DP / 16], T *area, const T *base, int64_t offset, int D, bool whole,
-                                              bool there, int lane) {
-    const uint64_t live = __ballot(there);
-    Pack<T, V> x[N];
+  Pack<T, V> x[N];
+  // whole: D is a number of 16-byte pieces, so that all loads are under way at once; rows that are not there are memory all
+  // the same.  What a kernel reads first is issued before any of it is waited for.
+  __device__ __forceinline__ void issue(const T *base, int64_t offset, int D, bool whole, bool there, int lane) {
     if (whole) {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
@@ -194,6 +192,7 @@ struct WaveRows {
         x[i] = load_pack<T, V>(base + __shfl(offset, row, 64) + (c < D ? c : 0));
       }
     } else {
+      const uint64_t live = __ballot(there);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const int row = (lane + 64 * i) / PR, c = (lane + 64 * i) % PR * V;
@@ -202,6 +201,10 @@ struct WaveRows {
         if (c < D && (live >> row & 1)) x[i] = load_some<T, V>(base + at + c, D - c);
       }
     }
+  }
+  // f = the channels of row l % 32 as the factor of a product over channels, 0 where the row is not there.
+  __device__ __forceinline__ void land(Frag<T> (&f)[DP / 16], T *area, int D, bool there, int lane) {
+    const uint64_t live = __ballot(there);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int row = (lane + 64 * i) / PR, c = (lane + 64 * i) % PR * V;

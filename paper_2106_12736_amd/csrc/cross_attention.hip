@@ -29,9 +29,8 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_fwd(Attn p, float *__res
   const Row row = row_of(p, g, r, queries);
   Frag<T> q[DP / 16];
   T *area = lds + wave * 32 * kStride<T, DP>;
-  WaveRows<T, DP>::load(q, area, static_cast<const T *>(p.a.q.p), offset_of(p.a.q, b, row.t, row.head), p.a.D, p.whole, row.live,
-                        lane);
-  __syncthreads();
+  WaveRows<T, DP> wq;
+  wq.issue(static_cast<const T *>(p.a.q.p), offset_of(p.a.q, b, row.t, row.head), p.a.D, p.whole, row.live, lane);
   v16f o[DP / 32] = {};
   float m = -INFINITY, l = 0.f, w = 0.f;  // the sum, and that of the rounded probabilities
   const int first = split * run, last = min(first + run, (keys + KT - 1) / KT);
@@ -45,6 +44,8 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_fwd(Attn p, float *__res
     };
     uint64_t there = keys_there(p, b, first * KT, keys, lane, KT), next = keys_there(p, b, (first + 1) * KT, keys, lane, KT);
     load(first, there);
+    wq.land(q, area, p.a.D, row.live, lane);
+    __syncthreads();
     sk.store(lds, p.a.D, there), sv.store(lds + S, p.a.D, there);
     for (int tile = first; tile < last; ++tile) {
       const T *kt = lds + (tile - first & 1) * 2 * S, *vt = kt + S;

@@ -48,9 +48,9 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_kv(
   Frag<T> k[NS], v[NS];
   const int in = min(key, p.a.Lk - 1);
   T *area = lds + wave * 32 * kStride<T, DP>;
-  WaveRows<T, DP>::load(k, area, static_cast<const T *>(p.a.k.p), offset_of(p.a.k, b, in, g), p.a.D, p.whole, there, lane);
-  WaveRows<T, DP>::load(v, area, static_cast<const T *>(p.a.v.p), offset_of(p.a.v, b, in, g), p.a.D, p.whole, there, lane);
-  __syncthreads();
+  WaveRows<T, DP> wk, wv;
+  wk.issue(static_cast<const T *>(p.a.k.p), offset_of(p.a.k, b, in, g), p.a.D, p.whole, there, lane);
+  wv.issue(static_cast<const T *>(p.a.v.p), offset_of(p.a.v, b, in, g), p.a.D, p.whole, there, lane);
   v16f ok[DP / 32] = {}, ov[DP / 32] = {};
   Scaled<T> scaled;
   const int first = split * run, last = min(first + run, (p.R + QT - 1) / QT);
@@ -88,6 +88,9 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_kv(
     float2 st = stats_of(first), next = stats_of(first + 1);
     uint64_t live = __ballot(st.x != INFINITY);
     load(live);
+    wk.land(k, area, p.a.D, there, lane);
+    wv.land(v, area, p.a.D, there, lane);
+    __syncthreads();
     sq.store(lds, p.a.D, live), sg.store(lds + S, p.a.D, live);
     if (wave == 0 && lane < QT) lst[lane] = st.x, lst[QT + lane] = st.y;
     for (int tile = first; tile < last; ++tile) {

@@ -26,10 +26,9 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_q(Attn p, fdc_heads 
   const bool live = st.x != INFINITY;
   Frag<T> q[DP / 16], go[DP / 16];
   T *area = lds + wave * 32 * kStride<T, DP>;
-  WaveRows<T, DP>::load(q, area, static_cast<const T *>(p.a.q.p), offset_of(p.a.q, b, row.t, row.head), p.a.D, p.whole, live,
-                        lane);
-  WaveRows<T, DP>::load(go, area, static_cast<const T *>(gy.p), offset_of(gy, b, row.t, row.head), p.a.D, p.whole, live, lane);
-  __syncthreads();
+  WaveRows<T, DP> wq, wg;
+  wq.issue(static_cast<const T *>(p.a.q.p), offset_of(p.a.q, b, row.t, row.head), p.a.D, p.whole, live, lane);
+  wg.issue(static_cast<const T *>(gy.p), offset_of(gy, b, row.t, row.head), p.a.D, p.whole, live, lane);
   v16f o[DP / 32] = {};
   Scaled<T> scaled;
   const int first = split * run, last = min(first + run, (keys + KT - 1) / KT);
@@ -43,6 +42,9 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_q(Attn p, fdc_heads 
     };
     uint64_t there = keys_there(p, b, first * KT, keys, lane, KT), next = keys_there(p, b, (first + 1) * KT, keys, lane, KT);
     load(first, there);
+    wq.land(q, area, p.a.D, live, lane);
+    wg.land(go, area, p.a.D, live, lane);
+    __syncthreads();
     sk.store(lds, p.a.D, there), sv.store(lds + S, p.a.D, there);
     for (int tile = first; tile < last; ++tile) {
       const T *kt = lds + (tile - first & 1) * 2 * S, *vt = kt + S;

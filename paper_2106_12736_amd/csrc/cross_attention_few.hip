@@ -25,6 +25,8 @@ __global__ __launch_bounds__(64 * W) void k_attn_few(Attn p, float *__restrict__
   const int keys = length_of(p.a.lengths, b, p.a.Lk), queries = length_of(p.a.q_lengths, b, p.a.Lq);
   T *area = reinterpret_cast<T *>(lds_) + wave * 32 * S;
   const Row row = row_of(p, g, lane & 31, queries);
+  WaveRows<T, DP> wq;
+  wq.issue(static_cast<const T *>(p.a.q.p), offset_of(p.a.q, b, row.t, row.head), p.a.D, p.whole, row.live, lane);
   v16f o[DP / 32] = {};
   float m = -INFINITY, l = 0.f, w = 0.f;  // the sum, and that of the rounded probabilities
   const int first = split * run, last = min(first + run, (keys + 31) / 32);
@@ -64,8 +66,7 @@ __global__ __launch_bounds__(64 * W) void k_attn_few(Attn p, float *__restrict__
     load(xv, p.a.v, block, there);
   }
   Frag<T> q[DP / 16];
-  WaveRows<T, DP>::load(q, area, static_cast<const T *>(p.a.q.p), offset_of(p.a.q, b, row.t, row.head), p.a.D, p.whole, row.live,
-                        lane);
+  wq.land(q, area, p.a.D, row.live, lane);
   for (; block < last; block += W) {
     const bool more = block + W < last;
     const uint64_t next = more ? keys_there(p, b, (block + W) * 32, keys, lane, 32) : 0;
