@@ -410,7 +410,9 @@ fdc_status fdc_adam_step(float *p, const float *g, float *m, float *v, int64_t n
 /* The block of a sequence network (tokens of D channels, for example the pixels of an
  * FDCNN's last planes) and the loss it is trained with: a causal convolution of each
  * channel with its own short kernel, a selective state space scan, the norms, gate and
- * residual scale around them, and distillation from a teacher's top logits.
+ * residual scale around them, and distillation from a teacher's top logits.  After them what
+ * such a network reads an image's tokens and scores its answers with: rotary positions of
+ * several axes, attention to states of another length, and token log probabilities.
  *
  * Types.     Activations (and their gradients) are of one of the types below;
  *            parameters, their gradients, states h and losses are float32.  Every sum

@@ -14,6 +14,10 @@
 // bisection until few enough do; equal logits are told apart by their places.
 //
 // Many rows: a workgroup each; few rows: segments, joined by a workgroup a row.
+//
+// 4096 x 32000 bf16 without alternatives 71 us (3.7 TB/s), 2048 x 100000 with 64 of them 134 us (3.1 TB/s): about 12 vector
+// instructions' time a logit (65 us of the latter) stand beside the reads.  With the rows in registers whole, and every
+// segment's K best found anew, the latter took 393 us.  The gradient, 4096 x 32000 bf16, 117 us (4.5 TB/s).
 #include <algorithm>
 
 #include "sequence.h"
