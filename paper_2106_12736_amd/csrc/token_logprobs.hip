@@ -15,9 +15,10 @@
 //
 // Many rows: a workgroup each; few rows: segments, joined by a workgroup a row.
 //
-// 4096 x 32000 bf16 without alternatives 71 us (3.7 TB/s), 2048 x 100000 with 64 of them 134 us (3.1 TB/s): about 12 vector
-// instructions' time a logit (65 us of the latter) stand beside the reads.  With the rows in registers whole, and every
-// segment's K best found anew, the latter took 393 us.  The gradient, 4096 x 32000 bf16, 117 us (4.5 TB/s).
+// 4096 x 32000 bf16 without alternatives 47 us (z from the last-level cache; 71 with the subtraction, the product and a guard
+// against 0 times -inf for each logit in place of one fma), 2048 x 100000 with 64 of them 125 us (3.3 TB/s): the vector
+// instructions of maxima, sums and candidates stand beside the reads.  With the rows in registers whole, and every segment's K
+// best found anew, the latter took 393 us.  The gradient, 4096 x 32000 bf16, 117 us (4.5 TB/s).
 #include <algorithm>
 
 #include "sequence.h"
@@ -44,24 +45,30 @@ constexpr uint32_t kInfKey = 0xff800000u;
 __device__ __forceinline__ uint64_t pair_of(uint32_t key, int place) { return (uint64_t)key << 32 | ~(uint32_t)place; }
 __device__ __forceinline__ int place_of(uint64_t pair) { return (int)~(uint32_t)pair; }
 
+// With t = (z - m) c, c = log2(e) / tau: s = sum 2^t, u = sum 2^t t.
 struct Sums {
   float m, s, u;
+  // s and u relative to t + by
+  __device__ __forceinline__ void shift(float by) {
+    const float f = exp2_fast(by);
+    s *= f;
+    u = fmaf(s, by, u * f);  // the sum scaled first: segments of the type's lowest value
+  }
 };
-// u is in units of z: sum exp(d) (z - m).
-__device__ __forceinline__ void add(Sums &a, const Sums &b, float c) {
-  if (b.s == 0.f) return;  // nothing but -inf: (m - M) 0 would be NaN
+// (from - to) c as a number.
+__device__ __forceinline__ float distance(float from, float to, float c) {
+  return from == to ? 0.f : fmaxf((from - to) * c, kLowest);
+}
+__device__ __forceinline__ void add(Sums &a, Sums b, float c) {
+  if (b.s == 0.f) return;  // nothing but -inf
   if (a.s == 0.f) {
     a = b;
     return;
   }
   const float m = fmaxf(a.m, b.m);
-  // the differences as numbers, the sums scaled before they are multiplied with them: segments of the type's lowest value
-  const float da = a.m == m ? 0.f : fmaxf(a.m - m, kLowest), db = b.m == m ? 0.f : fmaxf(b.m - m, kLowest);
-  const float fa = exp2_fast(da * c), fb = exp2_fast(db * c);
-  const float sa = a.s * fa, sb = b.s * fb;
-  a.u = fmaf(sa, da, a.u * fa) + fmaf(sb, db, b.u * fb);
-  a.s = sa + sb;
-  a.m = m;
+  a.shift(distance(a.m, m, c));
+  b.shift(distance(b.m, m, c));
+  a = {m, a.s + b.s, a.u + b.u};
 }
 
 // The largest logits that a first bound is found from: of every thread, or of four adjacent ones.
@@ -153,7 +160,14 @@ __device__ __forceinline__ int add_top(TopScratch<TH> &t, int set, int kept, uin
   // bisection: K or more logits of the chunk are not below lo, fewer than K not below hi
   const int most = kMost - kept;
   n -= kept;
-  uint64_t lo = bound, hi = 1ull << 32;
+  uint32_t most_key = odd ? 0xffffffffu : key_of(largest);
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) most_key = max(most_key, (uint32_t)__shfl_xor((int)most_key, off, 64));
+  if ((threadIdx.x & 63) == 0) t.red[1][threadIdx.x >> 6] = (int)most_key;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < TH / 64; ++i) most_key = max(most_key, (uint32_t)t.red[1][i]);
+  uint64_t lo = bound, hi = (uint64_t)most_key + 1;
   int turn = 0;
   auto count = [&](const Bound &b) {
     int c = 0;
@@ -194,6 +208,7 @@ __device__ __forceinline__ void rank_top(const uint64_t *found, int n, int K, Pu
   for (int i = threadIdx.x; i < n; i += TH) {
     const uint64_t mine = found[i];
     int rank = 0;
+#pragma unroll 4
     for (int j = 0; j < n; ++j) rank += found[j] > mine;
     if (rank < K) put(rank, mine);
   }
@@ -212,7 +227,7 @@ template <class T>
 __device__ __forceinline__ void row_result(const fdc_token_logprobs_args &a, int64_t row, const Sums &x, float *logp,
                                            float *entropy, float *stats) {
   const Result r(x, a.tau);
-  const float h = r.log_s - x.u / x.s * r.per;
+  const float h = r.log_s - x.u / x.s * kLn2;
   if (logp != nullptr) {
     const int v = a.tokens[row];
     logp[row] = v < 0 ? 0.f : v >= a.V ? NAN : r.logp((float)static_cast<const T *>(a.z)[row * a.z_stride + v]);
@@ -239,9 +254,13 @@ __device__ __forceinline__ void keep_packed(Pack<T, V> &x) {
   asm volatile("" : "+v"(x.w[0]), "+v"(x.w[1]), "+v"(x.w[2]), "+v"(x.w[3]));
 }
 
+// Rows of many chunks want as many waves as there are; float16 with alternatives has 57 registers spilled at eight.
+template <class T, int TH, int NV, bool Top>
+constexpr int kWavesASimd = NV == 1 ? 1 : TH == 256 && Top && std::is_same_v<T, _Float16> ? 6 : 8;
+
 // A workgroup a segment (of `seg` logits, `segs` a row).
 template <class T, int TH, int NV, bool Top>
-__global__ __launch_bounds__(TH, NV > 1 ? 8 : 1) void k_logprobs(fdc_token_logprobs_args a, Out out, int seg, int segs) {
+__global__ __launch_bounds__(TH, (kWavesASimd<T, TH, NV, Top>)) void k_logprobs(fdc_token_logprobs_args a, Out out, int seg, int segs) {
   constexpr int V = kLogitV<T>, W = TH / 64, CHUNK = TH * NV * V;
   __shared__ float rmax[W], rs[W], ru[W];
   __shared__ std::conditional_t<Top, TopScratch<TH>, int> scratch;
@@ -281,16 +300,28 @@ __global__ __launch_bounds__(TH, NV > 1 ? 8 : 1) void k_logprobs(fdc_token_logpr
   Pack<T, V> x[NV], next[NV];
   load(x, begin);
   Sums t{-INFINITY, 0.f, 0.f};
+  // As long as a wave's logits are numbers and its maxima's m c at most 2^20, t is fma(z, c, -mc), with mc the rounded m c: off
+  // by its rounding of at most 2^-5, which all of the thread's terms have in common and which is made good at the end.  Else
+  // (z - m) c, held above -inf.
+  float mc = -INFINITY;
+  const float near = 0x1p20f / c;
+  bool careful = false;  // the same in every lane
+  auto to_exact = [&] {
+    if (t.s != 0.f) t.shift(fmaf(-t.m, c, mc));
+  };
   int kept = 0, set = 0;
   uint32_t bound = 0;
   for (int from = begin; from < end; from += CHUNK) {
     const bool more = from + CHUNK < end;
     if (more) load(next, from + CHUNK);
-    float largest = -INFINITY;
+    float best[NV], largest = -INFINITY;  // of each piece, and of all
 #pragma unroll
-    for (int k = 0; k < NV; ++k)
+    for (int k = 0; k < NV; ++k) {
+      best[k] = x[k].at(0);
 #pragma unroll
-      for (int i = 0; i < V; ++i) largest = fmaxf(largest, x[k].at(i));
+      for (int i = 1; i < V; ++i) best[k] = fmaxf(best[k], x[k].at(i));
+      largest = fmaxf(largest, best[k]);
+    }
     if constexpr (Top) {
       if (from == begin) {
         if constexpr (TH == 1024) {
@@ -308,24 +339,48 @@ __global__ __launch_bounds__(TH, NV > 1 ? 8 : 1) void k_logprobs(fdc_token_logpr
         }
       }
     }
-    if (largest > t.m) {
-      const float d = t.m == -INFINITY ? 0.f : fmaxf(t.m - largest, kLowest), f = exp2_fast(d * c);
-      t.s *= f;
-      t.u = fmaf(t.s, d, t.u * f);
-      t.m = largest;
+    if (!careful && __any(fabsf(largest) > near)) {
+      to_exact();
+      careful = true;
     }
-    // of -inf alone so far (or with NaN): each term is 0 (or NaN)
-    const float base = t.m == -INFINITY ? 0.f : t.m;
+    if (largest > t.m) {
+      const float to = largest * c;
+      if (t.s != 0.f) t.shift(careful ? distance(t.m, largest, c) : mc - to);
+      t.m = largest, mc = to;
+    }
+    if (!careful) {
+      const Sums before = t;
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      keep_packed(x[k]);
+      for (int k = 0; k < NV; ++k) {
+        keep_packed(x[k]);
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const float d = x[k].at(i) - base, e = exp2_fast(d * c);
-        t.s += e;
-        t.u = fmaf(e, fmaxf(d, kLowest), t.u);  // a place of -inf: 0 times a number
+        for (int i = 0; i < V; ++i) {
+          const float d = fmaf(x[k].at(i), c, -mc), e = exp2_fast(d);
+          t.s += e;
+          t.u = fmaf(e, d, t.u);
+        }
+        asm volatile("" : "+v"(t.s), "+v"(t.u));  // a piece at a time: its floats die with it
       }
-      asm volatile("" : "+v"(t.s), "+v"(t.u));  // a piece at a time: its floats die with it
+      if (__any(t.u != t.u && t.s == t.s)) {  // 0 times -inf
+        t = before;
+        to_exact();
+        careful = true;
+      }
+    }
+    if (careful) {
+      // of -inf alone so far (or with NaN): each term is 0 (or NaN)
+      const float base = t.m == -INFINITY ? 0.f : t.m;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        keep_packed(x[k]);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          const float d = (x[k].at(i) - base) * c, e = exp2_fast(d);
+          t.s += e;
+          t.u = fmaf(e, fmaxf(d, kLowest), t.u);
+        }
+        asm volatile("" : "+v"(t.s), "+v"(t.u));
+      }
     }
     if constexpr (Top) {
       if (from == begin) {
@@ -333,26 +388,19 @@ __global__ __launch_bounds__(TH, NV > 1 ? 8 : 1) void k_logprobs(fdc_token_logpr
         bound = scratch.bound;
       }
       const bool odd = t.s != t.s;
-      if (__syncthreads_or(odd || key_of(largest) >= bound)) {
-        // a bit a logit, 32 at a time; the few that are set find their logits in memory again, not in registers by number
+      if (__syncthreads_or(odd || largest >= Bound(bound, 0).f)) {
+        // the few pieces that have one are read again (their registers cannot be chosen by number)
         auto above = [&](float f, auto &&put) {
-          constexpr int GROUP = 32 / V < NV ? 32 / V : NV;
+          uint32_t pieces = 0;
 #pragma unroll
-          for (int k0 = 0; k0 < NV; k0 += GROUP) {
-            uint32_t bits = 0;
+          for (int k = 0; k < NV; ++k) pieces |= odd || best[k] >= f ? 1u << k : 0u;
+          while (pieces != 0) {
+            const int at = from + (__builtin_ctz(pieces) * TH + tid) * V, base = place_of_piece(at);
+            pieces &= pieces - 1;
+            const Pack<T, V> y = TH == 64 ? load_some<T, V>(z + base, end - base, -INFINITY) : load_pack<T, V>(z + base);
 #pragma unroll
-            for (int k = k0; k < k0 + GROUP; ++k) {
-              keep_packed(x[k]);
-#pragma unroll
-              for (int i = 0; i < V; ++i) bits |= !(x[k].at(i) < f) ? 1u << ((k - k0) * V + i) : 0u;
-              asm volatile("" : "+v"(bits));
-            }
-            while (bits != 0) {
-              const int bit = __builtin_ctz(bits);
-              bits &= bits - 1;
-              const int place = place_of_piece(from + ((k0 + bit / V) * TH + tid) * V) + bit % V;
-              put((float)z[place], place);
-            }
+            for (int i = 0; i < V; ++i)
+              if (!(y.at(i) < f) && base + i >= at && base + i < end) put(y.at(i), base + i);
           }
         };
         const int n = add_top<T, TH>(scratch, set, kept, bound, a.K, largest, odd, z, from, min(end, from + CHUNK), above);
@@ -378,17 +426,14 @@ __global__ __launch_bounds__(TH, NV > 1 ? 8 : 1) void k_logprobs(fdc_token_logpr
     for (int k = 0; k < NV; ++k) x[k] = next[k];
   }
   // the threads' sums, relative to the largest of all
+  if (!careful) to_exact();
   float m = wave_max(t.m);
   if (lane == 0) rmax[wave] = m;
   __syncthreads();
   m = rmax[0];
 #pragma unroll
   for (int w = 1; w < W; ++w) m = fmaxf(m, rmax[w]);
-  if (t.m != m && !(t.s == 0.f)) {
-    const float d = t.m == -INFINITY ? 0.f : fmaxf(t.m - m, kLowest), f = exp2_fast(d * c);
-    t.s *= f;
-    t.u = fmaf(t.s, d, t.u * f);
-  }
+  if (t.m != m && !(t.s == 0.f)) t.shift(t.m == -INFINITY ? 0.f : distance(t.m, m, c));
   t.m = m;
   t.s = wave_sum(t.s);
   t.u = wave_sum(t.u);

@@ -519,6 +519,21 @@ def test_logprobs_values_at_the_edge(V, dtype):
     assert not seq.token_logprobs_backward(r.stats, z, tokens, glogp=g, gentropy=g).any()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("V", [40, 3000, 40000, 140000])
+def test_logprobs_far_from_zero(V, dtype):
+    # the products of logits and log2(e) lose bits, and more than a binade's worth past 2^24; the differences do not.  The last
+    # two rows go that far from chunk to chunk, up and down.
+    m, most = Make(V, dtype), 15 if dtype == "f16" else 70
+    far = [2.0 ** 10, -(2.0 ** 13), 2.0 ** min(19, most), 2.0 ** min(24, most), -(2.0 ** min(34, most)), 2.0 ** most]
+    grow = 2.0 ** (torch.arange(V, device="cuda") * (most / V))
+    rows = [(m.f32(V) * 2 + f).clamp(-65000.0, 65000.0) if dtype == "f16" else m.f32(V) * 2 + f for f in far] + [grow, -grow]
+    z = torch.stack(rows).to(DTYPES[dtype])
+    print(f"far from zero V={V} {dtype}", flush=True)
+    logprobs_check(z, i32([0, V - 1, 2, 3, 4, V - 1, V - 1, 0]), 20, 1.0, m.f32(8), m.f32(8), m.f32(8, 20))
+    logprobs_check(z, i32([0, V - 1, 2, 3, 4, V - 1, V - 1, 0]), 0, 0.125, m.f32(8), m.f32(8))
+
+
 def test_logprobs_parts():
     m = Make(2, "bf16")
     z = m.act(6, 500)
