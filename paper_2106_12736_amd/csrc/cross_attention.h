@@ -422,8 +422,8 @@ inline Cut cut(long long heads, long long own, long long through, int tile, bool
   c.splits = (int)ceil_div(steps, c.run);
   return c;
 }
-// Waves of a workgroup of the form for few rows: as many as their registers allow (two a SIMD, four with 16-bit heads of at
-// most 64 channels, one with wide float32 ones).
+// Waves of a workgroup of the form for few rows: two a SIMD, and one with float32 heads of more than 32 channels, whose
+// registers allow no more.
 template <class T>
 constexpr int few_waves(int DP) {
   return sizeof(T) == 2 ? 8 : DP <= 32 ? 8 : 4;
