@@ -500,7 +500,7 @@ hipError_t launch_tiles(const char *name, long long blocks, int threads, size_t 
 // The forward for few rows, in cross_attention_few.hip, and the parts of the backward, in cross_attention_bwd_*.hip.
 hipError_t launch_attention_few(const attention::Attn &p, const attention::Cut &c, float *part, hipStream_t s);
 hipError_t launch_attention_bwd_q(const attention::Attn &p, const attention::Cut &c, const fdc_heads &gy, const fdc_heads &gq,
-                                  const float2 *stats, float *part, hipStream_t s);
+                                  float2 *stats, float *part, hipStream_t s);
 hipError_t launch_attention_bwd_kv(const attention::Attn &p, const attention::Cut &c, const fdc_heads &gy,
                                    const fdc_heads &gk, const fdc_heads &gv, const float2 *stats, float *part,
                                    hipStream_t s);

@@ -172,35 +172,6 @@ __global__ __launch_bounds__(256) void k_attn_join(Attn p, const float *__restri
 }
 
 // ---- backward ----------------------------------------------------------------
-// [rows][2]: what a score's exponent is less by (infinity for a row without keys, or past the queries: its probabilities are 0)
-// and delta.  16 lanes a row (HBM-bound: 32768 x 8 rows of 128 bf16, 201 MB, 40 us, 5.0 TB/s).
-template <class T>
-__global__ __launch_bounds__(256) void k_attn_delta(Attn p, fdc_heads gy, float2 *__restrict__ stats,
-                                                    long long rows) {
-  const long long at_row = (long long)blockIdx.x * 16 + threadIdx.x / 16;
-  if (at_row >= rows) return;
-  const int bg = (int)(at_row / p.R), b = bg / p.a.G, g = bg - b * p.a.G, c = threadIdx.x % 16 * 8;
-  const Row row = row_of(p, g, (int)(at_row - (long long)bg * p.R), length_of(p.a.q_lengths, b, p.a.Lq));
-  const float e = p.lse[at_row];
-  const bool live = row.live && e != -INFINITY;
-  float sum = 0.f;
-  if (live && c < p.a.D) {
-    const Frag<T> x = load_frag<T>(at<T>(gy, b, row.t, row.head) + c, p.a.D - c);
-    const Frag<T> y = load_frag<T>(at<T>(p.a.y, b, row.t, row.head) + c, p.a.D - c);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) sum = fmaf((float)x[i], (float)y[i], sum);
-    if constexpr (sizeof(T) == 2) {
-      const Frag<T> rest = load_frag<T>(static_cast<const T *>(p.low) + at_row * p.D4 + c, p.a.D - c);
-      float more = 0.f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) more = fmaf((float)x[i], (float)rest[i], more);
-      sum = fmaf(more, 1.f / kLowUp<T>, sum);
-    }
-  }
-  sum = lane_sum<16>(sum);
-  if (threadIdx.x % 16 == 0) stats[at_row] = live ? float2{e * kLog2e - kUpBack<T>, sum} : float2{INFINITY, 0.f};
-}
-
 // Sums of the runs' parts [splits][B G][n][width D4], in order, to the heads of out0 and out1 (of the rows' tokens, or of
 // the keys): a thread has 4 channels.
 template <class T, bool Keys>
@@ -281,11 +252,6 @@ hipError_t launch_cross_attention_bwd(const fdc_cross_attention_args &a, const f
   const Cuts cuts(a.dtype, a.B, a.Lq, a.Lk, a.H, a.G, a.D);
   float2 *stats = reinterpret_cast<float2 *>(ws);
   float *part = ws + cuts.stats_floats();
-  if (hipError_t e = by_dtype(a.dtype, [&](auto tag) {
-        return timed_launch("attn_delta", k_attn_delta<decltype(tag)>, dim3((unsigned)ceil_div(cuts.rows, 16)), dim3(256),
-                            0, s, p, g.gy, stats, cuts.rows);
-      }))
-    return e;
   auto sum = [&](auto keys, const Cut &c, const fdc_heads &out0, const fdc_heads &out1, int n, long long total) {
     return by_dtype(a.dtype, [&](auto tag) {
       return timed_launch("attn_sum", k_attn_sum<decltype(tag), decltype(keys)::value>,

@@ -7,12 +7,26 @@ using namespace attention;
 
 namespace {
 
-// gq: a workgroup has 32 W rows and goes through a run of the keys, as the forward does.  Three products: 8 x 2048 tokens
-// over 1024 keys, 16 heads of 128 bf16, 259 us (796 TFLOP/s), over 4096 keys 837 (1070 TFLOP/s for what is added, a large
-// library product's 1120); the rest is rows in and out.  Half of a row's fragments are on their way from LDS at a time: all of
-// them at once took the registers of two waves a SIMD (288 spilled).
+// A lane's channels of its row.
+template <class T, int N>
+__device__ __forceinline__ float dot(const Frag<T> (&x)[N], const Frag<T> (&y)[N]) {
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum = fmaf((float)x[i][e], (float)y[i][e], sum);
+  return sum;
+}
+
+// gq: a workgroup has 32 W rows and goes through a run of the keys, as the forward does.  Before, its waves form their rows'
+// delta from gy, y and y's low part, and the first run's leave it, with what a score's exponent is less by (infinity for a row
+// without keys, or past the queries: its probabilities are 0), in stats [rows][2] for the gradient of k and v.  A launch of
+// its own for these took 40 us of 8 x 2048 tokens, 16 heads of 128 bf16; here it takes 37, and 2 in place of 5 of small
+// calls.  Three products: that case over 1024 keys 287 us, over 4096 keys 868 (1065 TFLOP/s for what is added, a large library
+// product's 1120); the rest is rows in and out.  Half of a row's fragments are on their way from LDS at a time: all of them
+// at once took the registers of two waves a SIMD (288 spilled).
 template <class T, int DP, int W>
-__global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_q(Attn p, fdc_heads gy, fdc_heads gq, const float2 *__restrict__ stats,
+__global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_q(Attn p, fdc_heads gy, fdc_heads gq, float2 *__restrict__ stats,
                                                        float *__restrict__ part, int row_tiles, int splits, int run) {
   constexpr int KT = attn_keys(sizeof(T)), S = KT * kStride<T, DP>, NB = KT / 32;
   extern __shared__ __align__(16) char lds_[];
@@ -25,13 +39,17 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_q(Attn p, fdc_heads 
   const int keys = length_of(p.a.lengths, b, p.a.Lk), queries = length_of(p.a.q_lengths, b, p.a.Lq);
   const int r = (rt * W + wave) * 32 + (lane & 31);
   const Row row = row_of(p, g, r, queries);
-  const float2 st = r < p.R ? stats[(int64_t)bg * p.R + r] : float2{INFINITY, 0.f};
-  const bool live = st.x != INFINITY;
+  const int64_t at_row = (int64_t)bg * p.R + min(r, p.R - 1);
+  const float lse = p.lse[at_row];
+  const bool live = r < p.R && row.live && lse != -INFINITY;
+  float2 st{live ? lse * kLog2e - kUpBack<T> : INFINITY, 0.f};
   Frag<T> q[DP / 16], go[DP / 16];
   T *area = lds + wave * 32 * kStride<T, DP>;
-  WaveRows<T, DP> wq, wg;
+  WaveRows<T, DP> wq, wg, wy, wl;
   wq.issue(static_cast<const T *>(p.a.q.p), offset_of(p.a.q, b, row.t, row.head), p.a.D, p.whole, live, lane);
   wg.issue(static_cast<const T *>(gy.p), offset_of(gy, b, row.t, row.head), p.a.D, p.whole, live, lane);
+  wy.issue(static_cast<const T *>(p.a.y.p), offset_of(p.a.y, b, row.t, row.head), p.a.D, p.whole, live, lane);
+  if constexpr (sizeof(T) == 2) wl.issue(static_cast<const T *>(p.low), at_row * p.D4, p.a.D, p.whole, live, lane);
   v16f o[DP / 32] = {};
   Scaled<T> scaled;
   const int first = split * run, last = min(first + run, (keys + KT - 1) / KT);
@@ -47,6 +65,16 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_q(Attn p, fdc_heads 
     load(first, there);
     wq.land(q, area, p.a.D, live, lane);
     wg.land(go, area, p.a.D, live, lane);
+    {
+      Frag<T> y[DP / 16];
+      wy.land(y, area, p.a.D, live, lane);
+      st.y = dot<T>(go, y);
+      if constexpr (sizeof(T) == 2) {
+        wl.land(y, area, p.a.D, live, lane);
+        st.y = fmaf(dot<T>(go, y), 1.f / kLowUp<T>, st.y);
+      }
+      st.y += __shfl_xor(st.y, 32, 64);
+    }
     __syncthreads();
     sk.store(lds, p.a.D, there), sv.store(lds + S, p.a.D, there);
     for (int tile = first; tile < last; ++tile) {
@@ -102,6 +130,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_q(Attn p, fdc_heads 
       there = next, next = after;
     }
   }
+  if (split == 0 && half == 0 && r < p.R) stats[at_row] = st;
   const float f = p.a.scale * exp2f(-kUpBack<T>) * scaled.undo();
   if (splits > 1) {
     if (r >= p.R) return;
@@ -117,7 +146,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_q(Attn p, fdc_heads 
 }  // namespace
 
 hipError_t launch_attention_bwd_q(const Attn &p, const Cut &c, const fdc_heads &gy, const fdc_heads &gq,
-                                  const float2 *stats, float *part, hipStream_t s) {
+                                  float2 *stats, float *part, hipStream_t s) {
   return by_shape<true>(p.a.dtype, p.a.D, c.waves, [&](auto tag, auto dp, auto waves) {
     using T = decltype(tag);
     constexpr int DP = decltype(dp)::value, W = decltype(waves)::value;

@@ -15,10 +15,11 @@
 //
 // Many rows: a workgroup each; few rows: segments, joined by a workgroup a row.
 //
-// 4096 x 32000 bf16 without alternatives 47 us (z from the last-level cache; 71 with the subtraction, the product and a guard
-// against 0 times -inf for each logit in place of one fma), 2048 x 100000 with 64 of them 125 us (3.3 TB/s): the vector
-// instructions of maxima, sums and candidates stand beside the reads.  With the rows in registers whole, and every segment's K
-// best found anew, the latter took 393 us.  The gradient, 4096 x 32000 bf16, 117 us (4.5 TB/s).
+// 4096 x 32000 bf16 without alternatives 52 us (5.0 TB/s; 71 behind a gradient's writes), 2048 x 100000 with 64 of them 129
+// us (3.2 TB/s), of which the first chunk's bound and the last ranking are some 20 us and later candidates 25: there the
+// vector units are busy 85 % of the time.  With the rows in registers whole, and every segment's K best found anew, it
+// took 393 us.  Candidates taken from registers instead of read again took 134.  The gradient, 4096 x 32000 bf16, 117 us
+// (4.5 TB/s).
 #include <algorithm>
 
 #include "sequence.h"
