@@ -53,17 +53,19 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_kv(
   const int in = min(key, p.a.Lk - 1);
   T *area = lds + wave * 32 * kStride<T, DP>;
   WaveRows<T, DP> wk, wv;
-  wk.issue(static_cast<const T *>(p.a.k.p), offset_of(p.a.k, b, in, g), p.a.D, p.whole, there, lane);
-  wv.issue(static_cast<const T *>(p.a.v.p), offset_of(p.a.v, b, in, g), p.a.D, p.whole, there, lane);
+  wk.issue(static_cast<const T *>(p.a.k.p), offset_of(p.a.k, b, in, g), p.a.D, p.wide, there, lane);
+  wv.issue(static_cast<const T *>(p.a.v.p), offset_of(p.a.v, b, in, g), p.a.D, p.wide, there, lane);
   v16f ok[DP / 32] = {}, ov[DP / 32] = {};
   Scaled<T> scaled;
   const int first = split * run, last = min(first + run, (p.R + QT - 1) / QT);
   const float2 *rows = stats + (int64_t)bg * p.R;
   const float2 none{INFINITY, 0.f};
   if (first < last && __syncthreads_or(there)) {
-    Staged<T, DP, 64 * W> sq, sg;
+    // 16-bit heads of 64 channels have no registers left for pieces that move (float16: 37 spilled, then 67; 329 us, then 407)
+    using Tile = Staged<T, DP, 64 * W, !(DP == 64 && sizeof(T) == 2)>;
+    Tile sq, sg;
     // where the pieces' rows are: a tile further on, as long as that is within the head
-    constexpr int N = Staged<T, DP, 64 * W>::N;
+    constexpr int N = Tile::N;
     int token[N];
     int64_t q_at[N], g_at[N];
     auto locate = [&](int i, int r) {
@@ -74,8 +76,8 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_kv(
 #pragma unroll
     for (int i = 0; i < N; ++i) locate(i, first * QT + sq.row_of(i));
     auto load = [&](uint64_t live) {
-      sq.load([&](int i) { return static_cast<const T *>(p.a.q.p) + q_at[i]; }, p.a.D, p.whole, live);
-      sg.load([&](int i) { return static_cast<const T *>(gy.p) + g_at[i]; }, p.a.D, p.whole, live);
+      sq.load([&](int i) { return static_cast<const T *>(p.a.q.p) + q_at[i]; }, p.a.D, p.wide, live);
+      sg.load([&](int i) { return static_cast<const T *>(gy.p) + g_at[i]; }, p.a.D, p.wide, live);
     };
     auto advance = [&](int tile) {
 #pragma unroll

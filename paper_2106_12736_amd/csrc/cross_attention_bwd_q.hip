@@ -46,10 +46,10 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_q(Attn p, fdc_heads 
   Frag<T> q[DP / 16], go[DP / 16];
   T *area = lds + wave * 32 * kStride<T, DP>;
   WaveRows<T, DP> wq, wg, wy, wl;
-  wq.issue(static_cast<const T *>(p.a.q.p), offset_of(p.a.q, b, row.t, row.head), p.a.D, p.whole, live, lane);
-  wg.issue(static_cast<const T *>(gy.p), offset_of(gy, b, row.t, row.head), p.a.D, p.whole, live, lane);
-  wy.issue(static_cast<const T *>(p.a.y.p), offset_of(p.a.y, b, row.t, row.head), p.a.D, p.whole, live, lane);
-  if constexpr (sizeof(T) == 2) wl.issue(static_cast<const T *>(p.low), at_row * p.D4, p.a.D, p.whole, live, lane);
+  wq.issue(static_cast<const T *>(p.a.q.p), offset_of(p.a.q, b, row.t, row.head), p.a.D, p.wide, live, lane);
+  wg.issue(static_cast<const T *>(gy.p), offset_of(gy, b, row.t, row.head), p.a.D, p.wide, live, lane);
+  wy.issue(static_cast<const T *>(p.a.y.p), offset_of(p.a.y, b, row.t, row.head), p.a.D, p.wide, live, lane);
+  if constexpr (sizeof(T) == 2) wl.issue(static_cast<const T *>(p.low), at_row * p.D4, p.a.D, p.wide, live, lane);
   v16f o[DP / 32] = {};
   Scaled<T> scaled;
   const int first = split * run, last = min(first + run, (keys + KT - 1) / KT);
@@ -58,8 +58,8 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_q(Attn p, fdc_heads 
     auto load = [&](int tile, uint64_t there) {
       const T *k0 = at<T>(p.a.k, b, (int64_t)tile * KT, g), *v0 = at<T>(p.a.v, b, (int64_t)tile * KT, g);
       const int most = p.a.Lk - 1 - tile * KT;
-      sk.load([&](int i) { return k0 + min(sk.row_of(i), most) * p.a.k.token_stride; }, p.a.D, p.whole, there);
-      sv.load([&](int i) { return v0 + min(sv.row_of(i), most) * p.a.v.token_stride; }, p.a.D, p.whole, there);
+      sk.load([&](int i) { return k0 + min(sk.row_of(i), most) * p.a.k.token_stride; }, p.a.D, p.wide, there);
+      sv.load([&](int i) { return v0 + min(sv.row_of(i), most) * p.a.v.token_stride; }, p.a.D, p.wide, there);
     };
     uint64_t there = keys_there(p, b, first * KT, keys, lane, KT), next = keys_there(p, b, (first + 1) * KT, keys, lane, KT);
     load(first, there);

@@ -27,7 +27,7 @@ __global__ __launch_bounds__(64 * W) void k_attn_few(Attn p, float *__restrict__
   T *area = reinterpret_cast<T *>(lds_) + wave * 32 * S;
   const Row row = row_of(p, g, lane & 31, queries);
   WaveRows<T, DP> wq;
-  wq.issue(static_cast<const T *>(p.a.q.p), offset_of(p.a.q, b, row.t, row.head), p.a.D, p.whole, row.live, lane);
+  wq.issue(static_cast<const T *>(p.a.q.p), offset_of(p.a.q, b, row.t, row.head), p.a.D, p.wide, row.live, lane);
   v16f o[DP / 32] = {};
   float m = -INFINITY, l = 0.f, w = 0.f;  // the sum, and that of the rounded probabilities
   const int first = split * run, last = min(first + run, (keys + 31) / 32);
@@ -35,11 +35,11 @@ __global__ __launch_bounds__(64 * W) void k_attn_few(Attn p, float *__restrict__
   auto load = [&](Pack<T, V>(&x)[N], const fdc_heads &h, int block, uint64_t there) {
     const T *base = at<T>(h, b, (int64_t)block * 32, g);
     const int most = p.a.Lk - 1 - block * 32;
-    if (p.whole) {
+    if (p.wide) {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const int r = (lane + 64 * i) / PR, c = (lane + 64 * i) % PR * V;
-        x[i] = load_pack<T, V>(base + min(r, most) * h.token_stride + (c < p.a.D ? c : 0));
+        x[i] = load_pack<T, V>(base + min(r, most) * h.token_stride + first_of<T>(c, p.a.D));
       }
     } else {
 #pragma unroll
@@ -51,6 +51,7 @@ __global__ __launch_bounds__(64 * W) void k_attn_few(Attn p, float *__restrict__
     }
   };
   auto put = [&](Pack<T, V>(&x)[N], uint64_t there) {
+    move_pieces(x, p.a.D, [&](int i) { return (lane + 64 * i) % PR * V; });
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int r = (lane + 64 * i) / PR, c = (lane + 64 * i) % PR * V;

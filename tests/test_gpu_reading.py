@@ -237,6 +237,14 @@ def test_attention_widths(D, dtype):
     attention_case(2, 9, 70, 2, 1, D, dtype, seed=D)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("D", [3, 5, 9, 13, 30, 47, 63, 73, 83, 94, 103, 126])
+def test_attention_widths_between_pieces(D, dtype):
+    # several tiles of rows and keys, and few rows, of widths that are not a number of 16-byte pieces
+    attention_case(2, 150, 140, 4, 2, D, dtype, q_lengths=[150, 33], lengths=[77, 140], seed=D)
+    attention_case(2, 1, 333, 4, 2, D, dtype, lengths=[333, 40], seed=D)
+
+
 @pytest.mark.parametrize("Lk", [1, 2, 3, 31, 32, 33, 63, 64, 65, 127, 128, 129, 200])
 def test_attention_numbers_of_keys(Lk):
     attention_case(2, 5, Lk, 2, 2, 48, "bf16", seed=Lk)
