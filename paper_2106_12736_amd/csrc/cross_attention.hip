@@ -13,8 +13,8 @@ namespace {
 // y is divided by the sum of the rounded probabilities, so that its weights add up to 1: for a row that reads one key
 // almost alone, y then is off by a rounding of the others' part only, and so is delta.  lse is of the sum before rounding.
 // Bound by the matrix units and what stands between their products: 8 x 2048 tokens over 1024 keys, 16 heads of 128 bf16,
-// 187 us (735 TFLOP/s), of which some 45 are rows in and out (201 MB, workgroups in step); over 4096 keys 645 us, 910
-// TFLOP/s for what is added, where a large library product runs at 1120.  Eight waves a workgroup share a tile's way through
+// 187 to 194 us between runs (720 TFLOP/s), of which some 45 are rows in and out (201 MB, workgroups in step); over 4096 keys
+// 658 us, 890 TFLOP/s for what is added, where a large library product runs at 1120.  Eight waves a workgroup share a tile's way through
 // LDS (128 bytes a cycle feed the matrix units just in time).  Tried: tiles of 32 keys in workgroups of four waves, two on a
 // compute unit (221 us).
 // The running maximum of a row is raised, and its sums rescaled, only when a score is 2^8 past it.

@@ -10,8 +10,8 @@ namespace {
 // gk and gv: a workgroup has 32 W keys and goes through a run of the rows (of every query head that shares them),
 // whose q and gy pass through LDS.  k, v and both sums are in registers: 192 of a wave's for 16-bit keys of 128 channels, so that
 // it has a SIMD to itself; the blocks of a tile are independent up to the sums, and the scores of one are formed
-// among the products of another.  Four products: 8 x 2048 tokens over 1024 keys, 16 heads of 128 bf16, 381 us (721
-// TFLOP/s), over 4096 keys 1445 (775 for what is added).  Bound by one wave's own latencies: with the blocks one after
+// among the products of another.  Four products: 8 x 2048 tokens over 1024 keys, 16 heads of 128 bf16, 390 to 412 us between
+// runs (690 TFLOP/s), over 4096 keys 1435 (790 for what is added).  Bound by one wave's own latencies: with the blocks one after
 // another 463 us, with both blocks' scores first 434, with the vector work set among the products 392.  Tried: v in LDS and
 // eight waves of 256 registers (180 spilled); a branch around tiles without live rows, which has every sum copied
 // between the two kinds of registers in each tile (253 moves for 64 products).

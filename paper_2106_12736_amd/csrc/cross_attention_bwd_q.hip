@@ -22,7 +22,7 @@ __device__ __forceinline__ float dot(const Frag<T> (&x)[N], const Frag<T> (&y)[N
 // delta from gy, y and y's low part, and the first run's leave it, with what a score's exponent is less by (infinity for a row
 // without keys, or past the queries: its probabilities are 0), in stats [rows][2] for the gradient of k and v.  A launch of
 // its own for these took 40 us of 8 x 2048 tokens, 16 heads of 128 bf16; here it takes 37, and 2 in place of 5 of small
-// calls.  Three products: that case over 1024 keys 287 us, over 4096 keys 868 (1065 TFLOP/s for what is added, a large library
+// calls.  Three products: that case over 1024 keys 289 us, over 4096 keys 865 (1073 TFLOP/s for what is added, a large library
 // product's 1120); the rest is rows in and out.  Half of a row's fragments are on their way from LDS at a time: all of them
 // at once took the registers of two waves a SIMD (288 spilled).
 template <class T, int DP, int W>
