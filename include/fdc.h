@@ -630,7 +630,7 @@ fdc_status fdc_cross_attention_backward(const fdc_cross_attention_args *a, const
                                         const fdc_cross_attention_grads *g, void *ws, size_t ws_bytes,
                                         hipStream_t stream);
 
-/* Log probabilities of R rows of V logits z at a temperature tau > 0 (at least 1e-38), with l = log softmax(z / tau):
+/* Log probabilities of R rows of V logits z at a temperature tau > 0 (1e-38 to 8e37), with l = log softmax(z / tau):
  *   logp[r] = l[tokens[r]],   entropy[r] = -sum_v exp(l[v]) l[v],   idx[r][k], top[r][k]: the K largest logits' places
  * and l there, from high to low, equal logits by rising place (0 <= K <= 128, K <= V; a NaN counts as the largest).
  * z [R][V] with row stride z_stride.  tokens [R] int32 (NULL: no logp): a row with tokens < 0 has logp 0 (and no gradient

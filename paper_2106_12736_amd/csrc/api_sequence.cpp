@@ -371,8 +371,8 @@ fdc_status check_logprobs_sizes(int dtype, int64_t R, int V, int K) {
 fdc_status check_logprobs(const fdc_token_logprobs_args *a) {
   if (a == nullptr) return fail(FDC_EINVAL, "arguments are NULL");
   FDC_TRY(check_logprobs_sizes(a->dtype, a->R, a->V, a->K));
-  if (!(a->tau > 0.f) || !std::isfinite(a->tau) || !std::isfinite(1.5f / a->tau))  // log2(e) / tau enters the kernels
-    return fail(FDC_EINVAL, "tau must be positive, with 1.5 / tau in float32's range (got %g)", (double)a->tau);
+  if (!(a->tau > 0.f) || !std::isnormal(1.f / a->tau) || !std::isfinite(1.5f / a->tau))  // log2(e) / tau enters the kernels
+    return fail(FDC_EINVAL, "tau must be positive, with 1 / tau among float32's normal numbers (got %g)", (double)a->tau);
   if (!a->z) return fail(FDC_EINVAL, "z is NULL");
   return check_row_stride(a->z_stride, a->R, a->V, "z", false);
 }

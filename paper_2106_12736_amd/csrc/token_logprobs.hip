@@ -305,7 +305,7 @@ __global__ __launch_bounds__(TH, (kWavesASimd<T, TH, NV, Top>)) void k_logprobs(
   // by its rounding of at most 2^-5, which all of the thread's terms have in common and which is made good at the end.  Else
   // (z - m) c, held above -inf.
   float mc = -INFINITY;
-  const float near = 0x1p20f / c;
+  const float near = fminf(0x1p20f / c, -kLowest);
   bool careful = false;  // the same in every lane
   auto to_exact = [&] {
     if (t.s != 0.f) t.shift(fmaf(-t.m, c, mc));

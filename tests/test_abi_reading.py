@@ -162,7 +162,7 @@ def test_rotary_over_its_input():
 @pytest.mark.parametrize("change,want", [
     ({"dtype": 9}, FDC_EINVAL), ({"R": 0}, FDC_EINVAL), ({"V": 0}, FDC_EINVAL), ({"K": -1}, FDC_EINVAL), ({"K": 51}, FDC_EINVAL),
     ({"V": 1000, "K": 129, "z_stride": 1000}, FDC_EUNSUPPORTED), ({"tau": 0.0}, FDC_EINVAL), ({"tau": float("nan")}, FDC_EINVAL),
-    ({"tau": float("inf")}, FDC_EINVAL), ({"tau": 4e-39}, FDC_EINVAL), ({"z": None}, FDC_EINVAL), ({"z_stride": -1}, FDC_EINVAL),
+    ({"tau": float("inf")}, FDC_EINVAL), ({"tau": 4e-39}, FDC_EINVAL), ({"tau": 2e38}, FDC_EINVAL), ({"z": None}, FDC_EINVAL), ({"z_stride": -1}, FDC_EINVAL),
     ({"V": (1 << 24) + 1}, FDC_EUNSUPPORTED), ({"R": 1 << 26}, FDC_EUNSUPPORTED), ({"R": 1 << 25, "V": 1 << 20}, FDC_EUNSUPPORTED),
 ])
 def test_logprobs_refuses(change, want):

@@ -542,6 +542,19 @@ def test_logprobs_far_from_zero(V, dtype):
     logprobs_check(z, i32([0, V - 1, 2, 3, 4, V - 1, V - 1, 0]), 0, 0.125, m.f32(8), m.f32(8))
 
 
+@pytest.mark.parametrize("V", [40, 3000, 40000])
+def test_logprobs_extreme_temperatures(V):
+    # the hottest is a uniform distribution over the places that are there, the coldest one of the largest logits
+    m = Make(V)
+    z = m.act(4, V)
+    z[1, ::2] = -float("inf")
+    z[2, :V // 2] = -float("inf")
+    z[3, 1:] = -float("inf")
+    print(f"extreme temperatures V={V}", flush=True)
+    for temperature in (8e37, 1e33, 2e-38):
+        logprobs_check(z, i32([0, 1, V - 1, 0]), 5, temperature)
+
+
 def test_logprobs_parts():
     m = Make(2, "bf16")
     z = m.act(6, 500)
