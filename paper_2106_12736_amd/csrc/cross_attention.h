@@ -373,9 +373,10 @@ template <class T>
 __device__ __forceinline__ void store_row_part(const Attn &p, int g, int b, int64_t at_row, int r, int queries, int c,
                                                float (&o)[4], float m, float l, float w) {
   const Row row = row_of(p, g, r, queries);
-  const float f = !row.live || l == 0.f ? 0.f : 1.f / w;
+  const bool none = !row.live || l == 0.f;
+  const float f = 1.f / w;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) o[j] *= f;
+  for (int j = 0; j < 4; ++j) o[j] = none ? 0.f : o[j] * f;  // not by a product: o is NaN where a key it sees is
   store_some<T, 4>(at<T>(p.a.y, b, row.t, row.head) + c, o, p.a.D - c);
   if constexpr (sizeof(T) == 2) {
     if (p.low != nullptr) {
@@ -384,7 +385,7 @@ __device__ __forceinline__ void store_row_part(const Attn &p, int g, int b, int6
     }
   }
   if (p.lse != nullptr && c == 0)
-    p.lse[at_row] = !row.live || l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l) - kUp<T>) * kLn2;
+    p.lse[at_row] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l) - kUp<T>) * kLn2;
 }
 
 // float16's probabilities times 2^15 (at most 2^15): 2^-14 is its least normal number.

@@ -128,7 +128,12 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_fwd(Attn p, float *__res
     if (half == 0) to[p.D4] = m, to[p.D4 + 1] = l, to[p.D4 + 2] = w;
     return;
   }
-  const float f = !row.live || l == 0.f ? 0.f : 1.f / w;
+  const bool none = !row.live || l == 0.f;
+  const float f = none ? 0.f : 1.f / w;
+  if (none) {  // not by a product: they are NaN where a key that the sequence has is, or infinite
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) o[d] = v16f{};
+  }
   const int64_t at_row = (int64_t)bg * p.R + r;
   __syncthreads();
   WaveRows<T, DP>::store(area, static_cast<T *>(p.a.y.p), offset_of(p.a.y, b, row.t, row.head), p.a.D, r < p.R, lane,
@@ -141,7 +146,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_fwd(Attn p, float *__res
       });
   }
   if (p.lse != nullptr && half == 0 && r < p.R)
-    p.lse[at_row] = !row.live || l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l) - kUp<T>) * kLn2;
+    p.lse[at_row] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l) - kUp<T>) * kLn2;
 }
 
 // The runs' results of a row, in order: a thread has 4 channels, and several runs' loads under way (HBM-bound; 42 runs of 1232

@@ -1,0 +1,72 @@
+"""The reading operators at values and sizes that could go wrong without another test's seeing it.
+
+Infinities and NaN in keys and values that a sequence's queries see, beside rows past its queries: those rows' outputs and
+gradients are 0, and so are the gradients of keys that no query reads.  What the rows that read them get is the oracle's,
+NaN and infinities at the same places; tolerances are those of the tests of finite values.
+"""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import reading as oracle
+from paper_2106_12736_amd import sequence as seq
+from test_gpu_reading import UNIT, Make, bounds, host, i32, within
+
+pytestmark = pytest.mark.gpu
+
+INF, NAN = float("inf"), float("nan")
+
+FORMS = {"tiles": (3, 77, 130, 2, 2, 40), "keys in runs": (3, 40, 1500, 1, 1, 64), "wide": (3, 300, 70, 4, 2, 128),
+         "few rows": (3, 4, 200, 4, 2, 32), "few rows in runs": (3, 4, 9000, 2, 1, 40), "rows in runs": (3, 700, 20, 2, 1, 24),
+         "odd width": (3, 150, 65, 1, 1, 63)}
+
+
+class Seen:
+    """A call whose key Lk / 2 holds `value` in its last channel, in k or v; its sequences have no, some and all queries."""
+
+    def __init__(self, form, dtype, where, value):
+        B, Lq, Lk, H, G, D = FORMS[form]
+        print(f"seen {form} {dtype} {where} {value}", flush=True)
+        m = Make(Lq + D, dtype)
+        self.q, self.k, self.v, self.gy = m.act(B, Lq, H, D), m.act(B, Lk, G, D), m.act(B, Lk, G, D), m.act(B, Lq, H, D)
+        self.q[..., -1] = self.q[..., -1].abs() + 0.5  # a key of -inf there has a score of -inf with every query
+        (self.k if where == "k" else self.v)[:, Lk // 2, :, -1] = value
+        self.n = [0, Lq // 2 + 1, Lq]
+        for b, n in enumerate(self.n):
+            self.q[b, n:], self.gy[b, n:] = NAN, INF
+        self.kw = dict(q_lengths=i32(self.n))
+        self.y, self.saved = seq.cross_attention_forward(self.q, self.k, self.v, save=True, **self.kw)
+
+    def hosts(self):
+        return host(self.q), host(self.k), host(self.v)
+
+    def bounds(self, y):
+        with np.errstate(all="ignore"):
+            return bounds(host(self.gy), *self.hosts(), y, self.q.shape[-1] ** -0.5, self.n, None, None)
+
+    def wanted(self):
+        with np.errstate(all="ignore"):
+            return oracle.cross_attention(*self.hosts(), q_lengths=self.n)
+
+    def factor(self):
+        """Half a step of what a 16-bit factor of a sum is rounded to."""
+        return UNIT[self.y.dtype] if self.y.dtype != torch.float32 else 0.0
+
+
+SEEN = [("k", NAN), ("k", -INF), ("v", INF), ("v", NAN)]
+
+
+@pytest.mark.parametrize("where,value", SEEN)
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("form", FORMS)
+def test_rows_past_the_queries_are_zero(form, dtype, where, value):
+    s = Seen(form, dtype, where, value)
+    for b, n in enumerate(s.n):
+        assert (s.y[b, n:] == 0).all(), b
+    ry, rlse = s.wanted()
+    (ay, _, _, _), _ = s.bounds(ry)
+    within(s.y, ry, (s.factor() + 2e-5) * ay, "y")
+    within(s.saved[:rlse.size].view(rlse.shape), rlse, 2e-5 * (1 + np.abs(np.where(np.isfinite(rlse), rlse, 0))), "lse")
+    again, _ = seq.cross_attention_forward(s.q, s.k, s.v, **s.kw)
+    assert torch.equal(again.nan_to_num(7.0), s.y.nan_to_num(7.0))
