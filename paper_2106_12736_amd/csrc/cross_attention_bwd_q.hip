@@ -130,6 +130,10 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_q(Attn p, fdc_heads 
       there = next, next = after;
     }
   }
+  if (!live) {  // whatever NaN or infinities among the keys and values have led to
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) o[d] = v16f{};
+  }
   if (split == 0 && half == 0 && r < p.R) stats[at_row] = st;
   const float f = p.a.scale * exp2f(-kUpBack<T>) * scaled.undo();
   if (splits > 1) {

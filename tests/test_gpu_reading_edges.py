@@ -70,3 +70,19 @@ def test_rows_past_the_queries_are_zero(form, dtype, where, value):
     within(s.saved[:rlse.size].view(rlse.shape), rlse, 2e-5 * (1 + np.abs(np.where(np.isfinite(rlse), rlse, 0))), "lse")
     again, _ = seq.cross_attention_forward(s.q, s.k, s.v, **s.kw)
     assert torch.equal(again.nan_to_num(7.0), s.y.nan_to_num(7.0))
+
+
+# the gradient of the queries
+@pytest.mark.parametrize("where,value", SEEN)
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("form", FORMS)
+def test_gradients_past_the_queries_are_zero(form, dtype, where, value):
+    s = Seen(form, dtype, where, value)
+    g = seq.cross_attention_backward(s.gy, s.y, s.saved, s.q, s.k, s.v, **s.kw)
+    for b, n in enumerate(s.n):
+        assert (g.q[b, n:] == 0).all(), b
+    ry, _ = s.wanted()
+    (_, aq, _, _), (pq, _) = s.bounds(ry)
+    with np.errstate(all="ignore"):
+        want = oracle.cross_attention_backward(host(s.gy), *s.hosts(), q_lengths=s.n)[0]
+        within(g.q, want, s.factor() * aq + 4e-5 * pq, "gq")
