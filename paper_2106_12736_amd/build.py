@@ -23,6 +23,9 @@ COMMON = [
     "-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
     # packed fp32 instructions stay off (hipcc would otherwise form them from float2 code)
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+    # spilled vector registers go to scratch, not to accumulator registers: where one word of a product's factor went to
+    # the last free one and the others to scratch, the factor came back without that word
+    "-mllvm", "-amdgpu-spill-vgpr-to-agpr=0",
     "-I", os.path.join(ROOT, "include"),
     "-Wall", "-Wno-unused-function",
 ]

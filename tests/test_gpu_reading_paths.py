@@ -90,3 +90,13 @@ def test_types():
         seq.cross_attention_forward(q, q.half(), q)
     with pytest.raises(ValueError, match="must be float32, bfloat16 or float16"):
         seq.cross_attention_forward(q.double(), q.double(), q.double())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("D", [32, 64, 96, 128])
+@pytest.mark.parametrize("Lk", [60, 150, 300])
+def test_every_workgroup_of_attention(Lk, D, dtype):
+    # two, four and eight waves, of rows and of keys, over several tiles in one run and in several
+    attention_case(2, 150, Lk, 4, 2, D, dtype, lengths=[Lk, Lk - 7], seed=D)
+    attention_case(40, 130, Lk, 8, 8, D, dtype, seed=Lk)
+    attention_case(2, 60, Lk, 2, 2, D, dtype, [60, 31], seed=D + Lk)
