@@ -277,19 +277,27 @@ struct Staged {
   static __device__ __forceinline__ int channel_of(int i) { return ((int)threadIdx.x + i * TH) % PR * V; }
   // at(i): where the row of piece i begins (memory whether the row is there or not)
   template <class At>
-  __device__ __forceinline__ void load(At &&at, int D, bool wide, uint64_t there) {
-    if (Move ? wide : D % V == 0) {
+  __device__ __forceinline__ void load_whole(At &&at, int D) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) x[i] = load_pack<T, V>(at(i) + first_of<T>(channel_of(i), D));
-    } else {
+    for (int i = 0; i < N; ++i) x[i] = load_pack<T, V>(at(i) + first_of<T>(channel_of(i), D));
+  }
+  template <class At>
+  __device__ __forceinline__ void load_parts(At &&at, int D, uint64_t there) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const int c = channel_of(i);
-        x[i] = Pack<T, V>{};
-        if ((COUNT % TH == 0 || row_of(i) < COUNT / PR) && c < D && (there >> row_of(i) & 1))
-          x[i] = load_some<T, V>(at(i) + c, D - c);
-      }
+    for (int i = 0; i < N; ++i) {
+      const int c = channel_of(i);
+      x[i] = Pack<T, V>{};
+      if ((COUNT % TH == 0 || row_of(i) < COUNT / PR) && c < D && (there >> row_of(i) & 1))
+        x[i] = load_some<T, V>(at(i) + c, D - c);
     }
+  }
+  static __device__ __forceinline__ bool in_whole(int D, bool wide) { return Move ? wide : D % V == 0; }
+  template <class At>
+  __device__ __forceinline__ void load(At &&at, int D, bool wide, uint64_t there) {
+    if (in_whole(D, wide))
+      load_whole(at, D);
+    else
+      load_parts(at, D, there);
   }
   __device__ __forceinline__ void store(T *tile, int D, uint64_t there) {
     if constexpr (Move) move_pieces(x, D, [&](int i) { return channel_of(i); });

@@ -29,6 +29,24 @@ __device__ __forceinline__ void between() {
   }
 }
 
+// Whether one of row l % 32's values is NaN or an infinity: its exponent's bits, all set, carry into the sign's place.
+template <class T, int N>
+__device__ __forceinline__ bool odd_row(const Frag<T> (&x)[N]) {
+  constexpr unsigned exponent = sizeof(T) == 4 ? 0x7f800000u : std::is_same_v<T, _Float16> ? 0x7c007c00u : 0x7f807f80u;
+  constexpr unsigned one = sizeof(T) == 4 ? 0x00800000u : std::is_same_v<T, _Float16> ? 0x04000400u : 0x00800080u;
+  constexpr int words = sizeof(Frag<T>) / 4;
+  typedef unsigned Words __attribute__((ext_vector_type(words)));
+  unsigned carry = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const Words w = __builtin_bit_cast(Words, x[i]);
+#pragma unroll
+    for (int j = 0; j < words; ++j) carry |= (w[j] & exponent) + one;
+  }
+  const uint64_t lanes = __ballot((carry & (sizeof(T) == 4 ? 0x80000000u : 0x80008000u)) != 0);
+  return (lanes | lanes >> 32 | lanes << 32) >> (threadIdx.x & 63) & 1;
+}
+
 template <class T, int DP, int W>
 constexpr size_t bwd_kv_lds() {
   return tiles_bytes<T, DP, W>() + 2 * attn_keys(sizeof(T)) * sizeof(float2);
@@ -57,6 +75,8 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_kv(
   wv.issue(static_cast<const T *>(p.a.v.p), offset_of(p.a.v, b, in, g), p.a.D, p.wide, there, lane);
   v16f ok[DP / 32] = {}, ov[DP / 32] = {};
   Scaled<T> scaled;
+  bool has_gk = there, has_gv = there;  // else they are 0
+  uint64_t seen = 0;                    // whether there are rows
   const int first = split * run, last = min(first + run, (p.R + QT - 1) / QT);
   const float2 *rows = stats + (int64_t)bg * p.R;
   const float2 none{INFINITY, 0.f};
@@ -76,8 +96,14 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_kv(
 #pragma unroll
     for (int i = 0; i < N; ++i) locate(i, first * QT + sq.row_of(i));
     auto load = [&](uint64_t live) {
-      sq.load([&](int i) { return static_cast<const T *>(p.a.q.p) + q_at[i]; }, p.a.D, p.wide, live);
-      sg.load([&](int i) { return static_cast<const T *>(gy.p) + g_at[i]; }, p.a.D, p.wide, live);
+      auto q_row = [&](int i) { return static_cast<const T *>(p.a.q.p) + q_at[i]; };
+      auto g_row = [&](int i) { return static_cast<const T *>(gy.p) + g_at[i]; };
+      // one branch for both: with one each, registers that the first loads were on their way to held addresses of the second,
+      // which then waited for them (431 us in place of 390)
+      if (Tile::in_whole(p.a.D, p.wide))
+        sq.load_whole(q_row, p.a.D), sg.load_whole(g_row, p.a.D);
+      else
+        sq.load_parts(q_row, p.a.D, live), sg.load_parts(g_row, p.a.D, live);
     };
     auto advance = [&](int tile) {
 #pragma unroll
@@ -99,6 +125,20 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_kv(
     __syncthreads();
     sq.store(lds, p.a.D, live), sg.store(lds + S, p.a.D, live);
     if (wave == 0 && lane < QT) lst[lane] = st.x, lst[QT + lane] = st.y;
+    // The product of a key that holds NaN or an infinity with the zeros in the place of a row that is not there is NaN.  With a
+    // row that is there its score is -inf, which adds nothing but what is NaN of delta (to gk), or has made the row's lse
+    // NaN, and with it all.  So what is 0 is known here: the loop has no registers for it (scores that begin at -inf there: 436
+    // us in place of 393 of the case above), and after it the lookup has the loop spill (float16's heads of 64: 204 in place of 126).
+    const bool odd = odd_row<T>(k);
+    if (__any(odd)) {
+      bool no_lse = false, no_delta = false;
+      for (int r = first * QT + lane; r < min(last * QT, p.R); r += 64) {
+        no_lse |= rows[r].x != rows[r].x;
+        no_delta |= !(fabsf(rows[r].y) < INFINITY);
+      }
+      no_lse = __any(no_lse), no_delta = __any(no_delta);
+      if (odd) has_gv = no_lse, has_gk = no_lse || no_delta;
+    }
     for (int tile = first; tile < last; ++tile) {
       const int buf = tile - first & 1;
       const T *qt = lds + buf * 2 * S, *gt = qt + S;
@@ -106,6 +146,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_kv(
       __syncthreads();
       const bool more = tile + 1 < last;
       const uint64_t live_next = __ballot(next.x != INFINITY);
+      seen |= live;
       float2 after = none;
       if (more) {
         advance(tile + 1);
@@ -183,9 +224,14 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_kv(
       live = live_next, next = after;
     }
   }
-  if (!there) {  // whatever its zeros for k and v have led to
+  // whatever zeros in the place of the key, or of the rows, have led to
+  if (!has_gk || seen == 0) {
 #pragma unroll
-    for (int d = 0; d < DP / 32; ++d) ok[d] = ov[d] = v16f{};
+    for (int d = 0; d < DP / 32; ++d) ok[d] = v16f{};
+  }
+  if (!has_gv || seen == 0) {
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) ov[d] = v16f{};
   }
   const float fv = exp2f(-kUpBack<T>), fk = p.a.scale * fv * scaled.undo();
   if (splits > 1) {

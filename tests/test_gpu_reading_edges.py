@@ -23,7 +23,8 @@ FORMS = {"tiles": (3, 77, 130, 2, 2, 40), "keys in runs": (3, 40, 1500, 1, 1, 64
 
 
 class Seen:
-    """A call whose key Lk / 2 holds `value` in its last channel, in k or v; its sequences have no, some and all queries."""
+    """A call whose key Lk / 2 holds `value` in its last channel, in k or v (or k, and the next key's v -value); its sequences
+    have no, some and all queries."""
 
     def __init__(self, form, dtype, where, value):
         B, Lq, Lk, H, G, D = FORMS[form]
@@ -31,7 +32,10 @@ class Seen:
         m = Make(Lq + D, dtype)
         self.q, self.k, self.v, self.gy = m.act(B, Lq, H, D), m.act(B, Lk, G, D), m.act(B, Lk, G, D), m.act(B, Lq, H, D)
         self.q[..., -1] = self.q[..., -1].abs() + 0.5  # a key of -inf there has a score of -inf with every query
-        (self.k if where == "k" else self.v)[:, Lk // 2, :, -1] = value
+        if where == "both":
+            self.k[:, Lk // 2, :, -1], self.v[:, Lk // 2 + 1, :, -1] = value, -value
+        else:
+            (self.k if where == "k" else self.v)[:, Lk // 2, :, -1] = value
         self.n = [0, Lq // 2 + 1, Lq]
         for b, n in enumerate(self.n):
             self.q[b, n:], self.gy[b, n:] = NAN, INF
@@ -54,7 +58,7 @@ class Seen:
         return UNIT[self.y.dtype] if self.y.dtype != torch.float32 else 0.0
 
 
-SEEN = [("k", NAN), ("k", -INF), ("v", INF), ("v", NAN)]
+SEEN = [("k", NAN), ("k", -INF), ("v", INF), ("v", NAN), ("both", -INF)]
 
 
 @pytest.mark.parametrize("where,value", SEEN)
@@ -86,3 +90,22 @@ def test_gradients_past_the_queries_are_zero(form, dtype, where, value):
     with np.errstate(all="ignore"):
         want = oracle.cross_attention_backward(host(s.gy), *s.hosts(), q_lengths=s.n)[0]
         within(g.q, want, s.factor() * aq + 4e-5 * pq, "gq")
+
+
+# the gradients of the keys and values
+@pytest.mark.parametrize("where,value", SEEN)
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("form", FORMS)
+def test_gradients_of_keys_are_those_of_the_queries_there(form, dtype, where, value):
+    s = Seen(form, dtype, where, value)
+    g = seq.cross_attention_backward(s.gy, s.y, s.saved, s.q, s.k, s.v, **s.kw)
+    assert (g.k[0] == 0).all() and (g.v[0] == 0).all()
+    ry, _ = s.wanted()
+    (_, _, ak, av), (_, pk) = s.bounds(ry)
+    with np.errstate(all="ignore"):
+        _, gk, gv = oracle.cross_attention_backward(host(s.gy), *s.hosts(), q_lengths=s.n)
+        within(g.v, gv, (s.factor() + 2e-5) * av, "gv")
+        if where == "k":
+            within(g.k, gk, s.factor() * ak + 4e-5 * pk, "gk")
+        else:  # infinite or NaN: a sum of infinities of both signs, and of what y's infinity leaves of delta
+            assert not np.isfinite(gk[1:]).any() and not torch.isfinite(g.k[1:]).any()
