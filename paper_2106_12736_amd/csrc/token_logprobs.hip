@@ -594,14 +594,15 @@ __global__ __launch_bounds__(kGradThreads) void k_logprobs_grad(fdc_token_logpro
     return;
   }
   const float *p = stats + kLogprobStats * row;
-  const float per = 1.f / a.tau, c = kLog2e / a.tau, m = p[0], f = over ? NAN : per / p[1];
-  // p (l + entropy) with l = (z - m) / tau - log s
+  // 1 / tau as a factor of p where it is large, and of the upstream gradients where it is small: 1 / (tau s) is not among
+  // float32's normal numbers at the hottest temperatures, and the gradients over tau are too large at the coldest
+  const float per = 1.f / a.tau, c = kLog2e / a.tau, m = p[0], f = over ? NAN : fmaxf(per, 1.f) / p[1], g = fminf(per, 1.f);
+  // p (l + entropy) with l = t log(2) - log s, t = (z - m) log2(e) / tau
   const float shift = p[2] - __builtin_amdgcn_logf(p[1]) * kLn2;
-  const float c0 = fmaf(gh, shift, alike), c1 = gh * per;
-  const float none = -300.f / c;  // from here on the exponential is 0: what it is multiplied with stays finite
+  const float c0 = fmaf(gh, shift, alike) * g, c1 = gh * kLn2 * g;
   auto grad = [&](float x) {
-    const float d = x - m;
-    return -f * exp2_fast(d * c) * fmaf(c1, fmaxf(d, none), c0);
+    const float t = (x - m) * c;
+    return -f * exp2_fast(t) * fmaf(c1, fmaxf(t, -300.f), c0);  // past -300 the exponential is 0, and its factor finite
   };
   for (int at = begin + tid * V; at < end; at += kGradThreads * V) {
     const int n = min(V, end - at);

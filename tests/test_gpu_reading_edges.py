@@ -109,3 +109,26 @@ def test_gradients_of_keys_are_those_of_the_queries_there(form, dtype, where, va
             within(g.k, gk, s.factor() * ak + 4e-5 * pk, "gk")
         else:  # infinite or NaN: a sum of infinities of both signs, and of what y's infinity leaves of delta
             assert not np.isfinite(gk[1:]).any() and not torch.isfinite(g.k[1:]).any()
+
+
+# ----------------------------------------------------------------------------
+# token log probabilities
+# ----------------------------------------------------------------------------
+from test_gpu_reading import logprobs_check  # noqa: E402
+
+
+@pytest.mark.parametrize("temperature,up", [(8e37, 1e30), (2e36, 1e30), (1e33, 1.0), (2e-38, 1e-3)])
+@pytest.mark.parametrize("V", [40, 3000, 40000])
+def test_gradients_at_extreme_temperatures(V, temperature, up):
+    # upstream gradients that leave results among float32's normal numbers
+    m = Make(V)
+    z = m.act(4, V)
+    z[1, ::2] = -INF
+    z[2, :V // 2] = -INF
+    z[3, 1:] = -INF
+    print(f"extreme temperatures V={V} {temperature}", flush=True)
+    tokens, g = i32([0, 1, V - 1, 0]), [m.f32(4, scale=up), m.f32(4, scale=up), m.f32(4, 5, scale=up)]
+    logprobs_check(z, tokens, 5, temperature, *g)
+    logprobs_check(z, tokens, 5, temperature, g[0])
+    logprobs_check(z, tokens, 5, temperature, gentropy=g[1])
+    logprobs_check(z, None, 5, temperature, gtop=g[2])
