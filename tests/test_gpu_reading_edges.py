@@ -132,3 +132,20 @@ def test_gradients_at_extreme_temperatures(V, temperature, up):
     logprobs_check(z, tokens, 5, temperature, g[0])
     logprobs_check(z, tokens, 5, temperature, gentropy=g[1])
     logprobs_check(z, None, 5, temperature, gtop=g[2])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("V", [40, 3000, 40000, 140000])
+def test_gradients_of_rows_with_holes(V, dtype):
+    # each place's gradient against its own terms
+    m = Make(V, dtype)
+    z = m.act(5, V)
+    z[0, 1:] = -INF
+    z[1, ::2] = -INF
+    z[2, V // 2:] = -INF
+    z[3, torch.randperm(V, generator=m.g)[:V - V // 8].cuda()] = -INF
+    print(f"holes V={V} {dtype}", flush=True)
+    tokens, K = i32([0, 1, V - 1, -1, V // 2]), 20
+    logprobs_check(z, tokens, K, 1.0, m.f32(5), m.f32(5), m.f32(5, K))
+    logprobs_check(z, tokens, K, 0.7, m.f32(5), m.f32(5))
+    logprobs_check(z, None, 0, 1.0, gentropy=m.f32(5))
