@@ -336,6 +336,18 @@ fdc_status check_attention_sizes(int dtype, int B, int Lq, int Lk, int H, int G,
   return FDC_OK;
 }
 
+// What the sizes of the queries alone say: their rows are the forward's, in whatever groups.
+fdc_status check_attention_rows(int dtype, int B, int Lq, int H, int D) {
+  FDC_TRY(check_dtype(dtype));
+  FDC_TRY(check_sizes(B, Lq, D));
+  if (H < 1) return fail(FDC_EINVAL, "H must be positive (got %d)", H);
+  if (H > 65535) return fail(FDC_EUNSUPPORTED, "H = %d exceeds 65535", H);
+  if (D > fdc::kAttentionMaxWidth) return fail(FDC_EUNSUPPORTED, "D = %d: at most %d", D, fdc::kAttentionMaxWidth);
+  if (!fdc::cross_attention_rows_fit((int64_t)B * Lq * H, D))
+    return fail(FDC_EUNSUPPORTED, "B = %d, Lq = %d, H = %d exceed the launch limit", B, Lq, H);
+  return FDC_OK;
+}
+
 fdc_status check_attention(const fdc_cross_attention_args *a, bool y_is_output) {
   if (a == nullptr) return fail(FDC_EINVAL, "arguments are NULL");
   FDC_TRY(check_attention_sizes(a->dtype, a->B, a->Lq, a->Lk, a->H, a->G, a->D));
@@ -574,7 +586,7 @@ fdc_status fdc_cross_attention_workspace_size(int dtype, int B, int Lq, int Lk, 
 }
 
 fdc_status fdc_cross_attention_saved_size(int dtype, int B, int Lq, int H, int D, size_t *bytes) {
-  FDC_TRY(check_attention_sizes(dtype, B, Lq, 1, H, H, D));
+  FDC_TRY(check_attention_rows(dtype, B, Lq, H, D));
   if (!bytes) return fail(FDC_EINVAL, "bytes is NULL");
   *bytes = fdc::cross_attention_saved(dtype, B, Lq, H, D);
   return FDC_OK;

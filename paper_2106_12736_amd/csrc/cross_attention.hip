@@ -208,13 +208,16 @@ __global__ __launch_bounds__(256) void k_attn_sum(Attn p, const float *__restric
 
 }  // namespace
 
+// The rows of a call, of any grouping: a thread for 4 channels where they are joined.
+bool cross_attention_rows_fit(int64_t rows, int D) { return rows < 1LL << 36 && rows * ceil_div(D, 4) < (1LL << 32) - 256; }
+
 // The largest number of workgroups of a launch: below 2^31, and below 2^32 threads.
 bool cross_attention_fits(int dtype, int B, int Lq, int Lk, int H, int G, int D) {
   const Cuts c(dtype, B, Lq, Lk, H, G, D);
   const long long most = (1LL << 32) / 1024 - 1, heads = (long long)B * G;
-  if (c.rows >= 1LL << 36 || c.keys >= 1LL << 36) return false;
+  if (!cross_attention_rows_fit(c.rows, D) || c.keys >= 1LL << 36) return false;
   return heads * c.fwd.tiles * c.fwd.splits <= most && heads * c.kv.tiles * c.kv.splits <= most &&
-         c.rows * c.D4 / 4 < (1LL << 32) - 256 && c.keys * 2 * c.D4 / 4 < (1LL << 32) - 256;
+         c.keys * 2 * c.D4 / 4 < (1LL << 32) - 256;
 }
 
 size_t cross_attention_saved(int dtype, int B, int Lq, int H, int D) {

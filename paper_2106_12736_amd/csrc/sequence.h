@@ -54,6 +54,7 @@ hipError_t launch_distill_bwd(const fdc_distill_args &a, const float *stats, con
 
 hipError_t launch_rotary(const fdc_rotary_args &a, hipStream_t s);
 
+bool cross_attention_rows_fit(int64_t rows, int D);
 bool cross_attention_fits(int dtype, int B, int Lq, int Lk, int H, int G, int D);
 size_t cross_attention_saved(int dtype, int B, int Lq, int H, int D);  // bytes
 size_t cross_attention_fwd_ws(int dtype, int B, int Lq, int Lk, int H, int G, int D);  // bytes

@@ -220,3 +220,24 @@ def test_under_host_sanitizers():
                        cwd=ROOT, env=env, capture_output=True, text=True, timeout=600)
     assert r.returncode == 0, r.stdout[-4000:] + r.stderr[-4000:]
     assert "passed" in r.stdout
+
+
+@pytest.mark.parametrize("B,Lq,Lk,H,G,D", [(65535, 1, 256, 65, 1, 128), (32768, 1, 64, 128, 2, 64), (65535, 4, 9, 60, 4, 32),
+                                           (1, 1 << 20, 40, 64, 1, 64)])
+@pytest.mark.parametrize("dtype", [0, 1, 2])
+def test_what_attends_can_be_saved(dtype, B, Lq, Lk, H, G, D):
+    # the size of what is saved has no number of key heads: that of the call decides
+    n = ctypes.c_size_t()
+    assert _lib.status("fdc_cross_attention_workspace_size", dtype, B, Lq, Lk, H, G, D, None, None) == FDC_OK
+    assert _lib.status("fdc_cross_attention_saved_size", dtype, B, Lq, H, D, ctypes.byref(n)) == FDC_OK, _lib.last_error()
+    rows, pieces = B * Lq * H, lambda n: (n + 15) // 16 * 16  # each part in pieces of 16 bytes
+    assert n.value == pieces(4 * rows) + (0 if dtype == 0 else pieces(2 * rows * D))
+
+
+def test_what_is_too_large_cannot_be_saved():
+    n = ctypes.c_size_t()
+    size = lambda *a: _lib.status("fdc_cross_attention_saved_size", *a, ctypes.byref(n))  # noqa: E731
+    assert size(1, 65535, 1 << 20, 1, 128) == FDC_EUNSUPPORTED and size(1, 65535, 1 << 28, 65535, 128) == FDC_EUNSUPPORTED
+    assert size(1, 1, 1, 65536, 8) == FDC_EUNSUPPORTED and size(1, 1, 1, 0, 8) == FDC_EINVAL
+    assert size(1, 0, 1, 1, 8) == FDC_EINVAL and size(3, 1, 1, 1, 8) == FDC_EINVAL
+    assert _lib.status("fdc_cross_attention_saved_size", 1, 1, 1, 1, 8, None) == FDC_EINVAL
