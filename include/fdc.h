@@ -602,7 +602,7 @@ fdc_status fdc_rotary(const fdc_rotary_args *a, hipStream_t stream);
  *   s[j] = scale q[b][t][h] . k[b][j][h / (H / G)],   y[b][t][h] = sum_j softmax(s)[j] v[b][j][h / (H / G)]
  * over the keys j that sequence b has: j < lengths[b] and mask[b * mask_stride + j] != 0 (either NULL: no such limit).
  * What k and v hold at other keys is never used, NaN included.  A row without keys has y = 0.
- * q, y [B][Lq][H][D]; k, v [B][Lk][G][D]; 1 <= D <= 128; scale > 0.  q_lengths [B] (NULL: Lq): the queries' lengths.
+ * q, y [B][Lq][H][D]; k, v [B][Lk][G][D]; 1 <= D <= 128; 0 < scale <= 2e38.  q_lengths [B] (NULL: Lq): the queries' lengths.
  * saved (NULL: no backward follows): fdc_cross_attention_saved_size bytes, 16-byte aligned, for the backward.  It begins
  * with lse [B][H][Lq] float32: log sum_j exp(s[j]), -inf without keys and past a sequence's queries (the rest: what
  * y's rounding lost).

@@ -351,8 +351,8 @@ fdc_status check_attention_rows(int dtype, int B, int Lq, int H, int D) {
 fdc_status check_attention(const fdc_cross_attention_args *a, bool y_is_output) {
   if (a == nullptr) return fail(FDC_EINVAL, "arguments are NULL");
   FDC_TRY(check_attention_sizes(a->dtype, a->B, a->Lq, a->Lk, a->H, a->G, a->D));
-  if (!(a->scale > 0.f) || !std::isfinite(a->scale))
-    return fail(FDC_EINVAL, "scale must be positive (got %g)", (double)a->scale);
+  if (!(a->scale > 0.f) || !std::isfinite(1.5f * a->scale))  // scale log2(e) enters the kernels
+    return fail(FDC_EINVAL, "scale must be positive, with 1.5 scale in float32's range (got %g)", (double)a->scale);
   FDC_TRY(check_heads(a->q, "q", a->B, a->Lq, a->H, a->D, false));
   FDC_TRY(check_heads(a->k, "k", a->B, a->Lk, a->G, a->D, false));
   FDC_TRY(check_heads(a->v, "v", a->B, a->Lk, a->G, a->D, false));

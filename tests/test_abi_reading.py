@@ -241,3 +241,17 @@ def test_what_is_too_large_cannot_be_saved():
     assert size(1, 1, 1, 65536, 8) == FDC_EUNSUPPORTED and size(1, 1, 1, 0, 8) == FDC_EINVAL
     assert size(1, 0, 1, 1, 8) == FDC_EINVAL and size(3, 1, 1, 1, 8) == FDC_EINVAL
     assert _lib.status("fdc_cross_attention_saved_size", 1, 1, 1, 1, 8, None) == FDC_EINVAL
+
+
+@pytest.mark.parametrize("scale", [2.5e38, 3.4e38])
+def test_scales_whose_exponents_leave_float32_are_refused(scale):
+    # scale log2(e) enters the kernels; an unaligned `saved` is what the call is refused for otherwise
+    a = _with(CrossAttentionArgs, ATT, scale=scale)
+    assert _lib.status("fdc_cross_attention_forward", a, P + 8, P, 1 << 40, None) == FDC_EINVAL
+    assert "scale" in _lib.last_error()
+    g = CrossAttentionGrads(*(_heads(5 + i, 2, 6 if i < 2 else 9, 4 if i < 2 else 2, 16) for i in range(4)))
+    assert _lib.status("fdc_cross_attention_backward", a, P + 8, g, P, 1 << 40, None) == FDC_EINVAL
+    assert "scale" in _lib.last_error()
+    a.scale = 2.2e38
+    assert _lib.status("fdc_cross_attention_forward", a, P + 8, P, 1 << 40, None) == FDC_EINVAL
+    assert "saved" in _lib.last_error()
