@@ -22,4 +22,15 @@ Err in_launches(long long total, int threads, Err none, F &&launch) {
   return err;
 }
 
+// Heads a thread of rotary positions goes through, with `threads` threads for a head: up to 4 (32768 tokens of 16 heads of
+// 128 bf16: 64 us, with 16 heads 78, with 2 63), fewer for what would not fill the chip's 256 compute units with 16 waves
+// each, and more where a launch of the whole could not be counted.
+constexpr int rotary_heads(long long threads, int H) {
+  int heads = H < 4 ? H : 4;
+  auto total = [&] { return threads * ((H + heads - 1) / heads); };
+  while (heads > 1 && total() < 256 * 16 * 64) heads = (heads + 1) / 2;
+  while (heads < H && total() > (1LL << 32) - 256) heads = 2 * heads < H ? 2 * heads : H;
+  return heads;
+}
+
 }  // namespace fdc

@@ -4,8 +4,7 @@
 //
 // A pass over x and y (HBM-bound: 32768 tokens of 16 heads of 128 bf16, 268 MB, 64 us, 4.2 TB/s).  The angle of a pair is that of every head of the token, so a thread holds the
 // cosines and sines of VP pairs (a 16-byte piece of either half) and goes through the heads with them.
-#include <algorithm>
-
+#include "launch_limit.h"
 #include "sequence.h"
 
 namespace fdc {
@@ -119,10 +118,7 @@ hipError_t launch_rotary(const fdc_rotary_args &a, hipStream_t s) {
     int P = 0;
     for (int i = 0; i < a.axes; ++i) P += a.pairs[i];
     const int turned = (int)ceil_div(P, VP), pieces = turned + (int)ceil_div(a.D - 2 * P, 2 * VP);
-    // up to 4 heads a thread (32768 tokens of 16 x 128 bf16: 64 us, with 16 heads 78, with 2 63), fewer for what would not
-    // fill the chip's 256 compute units with 16 waves each
-    int heads = std::min(a.H, 4);
-    while (heads > 1 && (long long)a.B * a.L * pieces * ceil_div(a.H, heads) < 256 * 16 * 64) heads = (heads + 1) / 2;
+    const int heads = rotary_heads((long long)a.B * a.L * pieces, a.H);
     const int runs = (int)ceil_div(a.H, heads);
     const long long total = (long long)a.B * a.L * pieces * runs, blocks = ceil_div(total, kRotaryThreads);
     if (blocks * kRotaryThreads >= (1LL << 32)) return hipErrorInvalidConfiguration;

@@ -87,3 +87,18 @@ def test_logprobs_far_rows():
         assert float(gz[i, tokens[i]]) > 0.5
     gz[some] = 0
     assert torch.count_nonzero(gz) == 0
+
+
+def test_rotary_more_threads_than_a_launch_has():
+    # 2^31 tokens of 5 heads: with 4 heads a thread a launch of 2^32 threads, so all 5
+    B, L, H = 8, 1 << 28, 5
+    print(f"rotary {B * L * H * 2} elements", flush=True)
+    x = torch.zeros(B, L, H, 2, dtype=BF16, device="cuda")
+    at = torch.tensor([0, 1, L // 2 - 1, L // 2, L - 2, L - 1], device="cuda")
+    x[:, at] = torch.randn(B, len(at), H, 2, device="cuda").to(BF16)
+    pos = torch.arange(L, device="cuda", dtype=torch.int32)[:, None].contiguous()
+    f = torch.tensor([0.37], device="cuda")
+    want = oracle.rotary(host(x[:, at]), pos[at].cpu().numpy(), host(f))
+    assert seq.rotary_forward(x, pos, f, y=x) is x
+    # a rounding, and 1e-6 of the largest value
+    assert (np.abs(host(x[:, at]) - want) <= 2.0 ** -8 * np.abs(want) + 1e-5).all()

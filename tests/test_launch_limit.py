@@ -58,3 +58,34 @@ def test_large_grids_go_through_the_limit():
     full = open(os.path.join(CSRC, "full_fdc.hip")).read()
     launchers = full[full.index("hipError_t launch_full_contract("):]
     assert len(re.findall(r"\bin_launches\(", launchers)) == len(re.findall(r"\btimed_launch\(", launchers)) == 5
+
+
+ROTARY = r"""
+#include "launch_limit.h"
+#undef NDEBUG
+#include <cassert>
+
+int main() {
+  // the accepted sizes: B L pieces below 2^32 - 2^20
+  const long long sizes[] = {1, 8, 1000, 65535, 1 << 20, (1LL << 24) + 1, 1LL << 26, (1LL << 30) - 1, 1LL << 30, 1LL << 31,
+                             (1LL << 32) - (1LL << 20) - 1};
+  for (long long threads : sizes)
+    for (int H : {1, 2, 3, 4, 5, 7, 8, 16, 33, 256, 65535}) {
+      const int heads = fdc::rotary_heads(threads, H);
+      assert(heads >= 1 && heads <= H);
+      const long long total = threads * ((H + heads - 1) / heads), blocks = (total + 255) / 256;
+      assert(blocks < (1LL << 32) && fdc::launch_counts((std::uint32_t)blocks, 256));
+      if (threads * ((H + 3) / 4) <= (1LL << 32) - 256) assert(heads <= 4);
+    }
+  assert(fdc::rotary_heads(1 << 26, 256) == 8 && fdc::rotary_heads(32768 * 16, 16) == 4 && fdc::rotary_heads(16, 16) == 1);
+  return 0;
+}
+"""
+
+
+@pytest.mark.skipif(shutil.which("g++") is None, reason="g++ is needed")
+def test_rotary_launches_fit_the_thread_count(tmp_path):
+    src, exe = tmp_path / "rotary.cpp", tmp_path / "rotary"
+    src.write_text(ROTARY)
+    subprocess.run(["g++", "-std=c++17", "-I", CSRC, str(src), "-o", str(exe)], check=True, timeout=120)
+    subprocess.run([str(exe)], check=True, timeout=60)
