@@ -383,16 +383,12 @@ def _rotary(x, positions, freqs, sections, interleaved, lengths, y, inverse):
     else:
         raise ValueError(f"x must be [B, L, H, D] or [B, H, D] (got {tuple(shape)})")
     axes, pairs = _pairs(sections if sections is None else tuple(sections), freqs.shape)
-    got, s = positions.shape, positions.stride()
-    want = (B, L, axes) if len(shape) == 4 else (B, axes)
-    if len(shape) == 3:
-        batch, token = s[0], 0
-    elif len(got) == 2:  # the same for every sequence
-        want, batch, token = (L, axes), 0, s[0]
-    else:
-        batch, token = s[0], s[1] if len(s) > 1 else 0
-    if got != want or positions.dtype != torch.int32 or positions.get_device() != x.get_device():
+    # [L, axes] of [B, L, H, D]: the same for every sequence
+    want = (B, axes) if len(shape) == 3 else (L, axes) if positions.dim() == 2 else (B, L, axes)
+    if positions.shape != want or positions.dtype != torch.int32 or positions.get_device() != x.get_device():
         _wrong(positions, torch.int32, x.device, want, "positions")
+    s = positions.stride()
+    batch, token = (s[0], 0) if len(shape) == 3 else (0, s[0]) if len(want) == 2 else (s[0], s[1])
     if s[-1] != 1 and axes > 1:
         raise ValueError("positions' last dimension must be dense")
     y = _like(x) if y is None else y

@@ -149,3 +149,15 @@ def test_gradients_of_rows_with_holes(V, dtype):
     logprobs_check(z, tokens, K, 1.0, m.f32(5), m.f32(5), m.f32(5, K))
     logprobs_check(z, tokens, K, 0.7, m.f32(5), m.f32(5))
     logprobs_check(z, None, 0, 1.0, gentropy=m.f32(5))
+
+
+# ----------------------------------------------------------------------------
+# refusals
+# ----------------------------------------------------------------------------
+def test_positions_without_axes_are_refused():
+    m = Make(1)
+    x, f = m.act(2, 3, 4, 16), m.f32(8)
+    for t, positions in ((x, torch.tensor(3, dtype=torch.int32, device="cuda")), (x[:, 0], m.ints(0, 9, 2)),
+                         (x[:, 0], torch.tensor(3, dtype=torch.int32, device="cuda")), (x, m.ints(0, 9, 3))):
+        with pytest.raises(ValueError, match="positions"):
+            seq.rotary_forward(t, positions, f)
