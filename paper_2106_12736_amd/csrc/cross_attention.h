@@ -65,9 +65,11 @@ __device__ __forceinline__ float halves_sum(float v) {
 }
 
 constexpr int attn_keys(size_t size) { return size == 2 ? 64 : 32; }  // rows of an LDS tile
-// A tile's rows are longer than their channels, so that what is read at once lies in different ones of LDS's 64 banks: for
-// 16-byte reads of a row a lane an odd number of 4 words (at 72 words instead of 76 they take 1.8 times as long), for the
-// transposed reads 4 rows' 8 words apart.
+// A tile's rows are longer than their channels.  16-bit rows are an odd number of 4 words, so that 16-byte reads of a row a
+// lane have no conflicts in LDS's banks (4 cycles; at 72 words instead of 76 they take 1.8 times as long).  The transposed
+// reads take 4 cycles, of which half are counted as conflicts, and are what the kernels' conflicts come from (20 to 29 % of
+// LDS's cycles); 16-byte writes of a tile take 8 (96 channels 10.6, 32 channels 15.9).  float32: the two reads of a row's 8
+// values take 8 cycles each, half of them conflicts, columns 4 without.
 template <class T, int DP>
 constexpr int kStride = DP + (sizeof(T) == 4 ? 8 : DP == 32 || DP == 128 ? 24 : 8);
 // LDS: two buffers of two tiles, and at its beginning and end 32 rows for each wave.
@@ -456,7 +458,11 @@ constexpr int few_waves(int DP) {
 }
 constexpr int kFewRows = 32;
 // Runs of blocks of 32 keys: one launch where a workgroup's keys are at most 512 KB or there are two workgroups for every
-// compute unit, else runs of at least two blocks a wave.
+// compute unit, else runs of at least two blocks a wave.  A call in one launch and in runs, in a captured graph, us: bf16 of
+// 512 KB a head, 16 heads of 64 channels 15.6 and 11.5, 64 of 128 15.9 and 16.3, 256 of 128 27.9 and 35.7; of 1 MB 26.1 and
+// 10.9, 23.8 and 22.9, 45.6 and 55.1.  float32 of 256 KB, 16 heads of 64 18.6 and 14.6; of 512 KB 31.8 and 15.7, 64 of 128
+// 31.2 and 22.9, 256 of 128 34.9 and 45.9; of 1 MB 58.4 and 15.0, 54.9 and 27.5, 58.8 and 70.2.  So few heads of float32 would
+// have runs from 256 KB on, and 256 heads none at all.
 inline Cut cut_few(int dtype, long long heads, long long keys, int D) {
   Cut c;
   const int DP = D <= 32 ? 32 : D <= 64 ? 64 : D <= 96 ? 96 : 128;

@@ -14,7 +14,9 @@ namespace {
 // runs (690 TFLOP/s), over 4096 keys 1435 (790 for what is added).  Bound by one wave's own latencies: with the blocks one after
 // another 463 us, with both blocks' scores first 434, with the vector work set among the products 392.  Tried: v in LDS and
 // eight waves of 256 registers (180 spilled); a branch around tiles without live rows, which has every sum copied
-// between the two kinds of registers in each tile (253 moves for 64 products).
+// between the two kinds of registers in each tile (253 moves for 64 products).  Registers spilled: float16's heads of 128 77
+// (179 in workgroups of two waves), of 96 in two waves 62, bf16's of 128 in two waves 53; heads of 64 in eight waves bf16 18,
+// float16 33.
 // An order for COUNT products and the vector work that they are independent of: some instructions after each product, which
 // the matrix unit takes 32 cycles for.
 template <class T, int COUNT>
@@ -81,7 +83,8 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_kv(
   const float2 *rows = stats + (int64_t)bg * p.R;
   const float2 none{INFINITY, 0.f};
   if (first < last && __syncthreads_or(there)) {
-    // 16-bit heads of 64 channels have no registers left for pieces that move (float16: 37 spilled, then 67; 329 us, then 407)
+    // 16-bit heads of 33 to 64 channels have no registers left for pieces that move (8 x 2048 rows on 1024 keys, 16 heads of 64
+    // bf16 177 us, with them 192; of 63 channels, read by elements, 261, and 208 with them; float16 230 and 230, 300 and 256)
     using Tile = Staged<T, DP, 64 * W, !(DP == 64 && sizeof(T) == 2)>;
     Tile sq, sg;
     // where the pieces' rows are: a tile further on, as long as that is within the head

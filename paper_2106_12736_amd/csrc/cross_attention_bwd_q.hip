@@ -24,7 +24,8 @@ __device__ __forceinline__ float dot(const Frag<T> (&x)[N], const Frag<T> (&y)[N
 // its own for these took 40 us of 8 x 2048 tokens, 16 heads of 128 bf16; here it takes 37, and 2 in place of 5 of small
 // calls.  Three products: that case over 1024 keys 289 us, over 4096 keys 865 (1073 TFLOP/s for what is added, a large library
 // product's 1120); the rest is rows in and out.  Half of a row's fragments are on their way from LDS at a time: all of them
-// at once took the registers of two waves a SIMD (288 spilled).
+// at once took the registers of two waves a SIMD (288 spilled; as it is 33 with 16-bit heads of 128 channels, 34 in
+// float16, and 8 with those of 96; one is read back in a tile).
 template <class T, int DP, int W>
 __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_q(Attn p, fdc_heads gy, fdc_heads gq, float2 *__restrict__ stats,
                                                        float *__restrict__ part, int row_tiles, int splits, int run) {

@@ -11,7 +11,8 @@ namespace {
 // its own: k and v are read once, a block ahead of the products (HBM-bound: 64 x 4096 keys of 8 heads of 128 f16, 1.07 GB in
 // 215 us, 5.0 TB/s; 1024 keys of 16 heads of 64 bf16 take 10.7 us, latencies alone, in one launch where runs and their join took
 // 13.8 in two), and pass through the wave's own rows of LDS without barriers.  At the end the waves' maxima, sums and outputs are joined in LDS,
-// in wave order, so that a call is one launch where there are sequences enough or keys few enough.
+// in wave order, so that a call is one launch where there are sequences enough or keys few enough.  16-bit heads of 128
+// channels have 29 registers spilled, those of 96 8.
 template <class T, int DP, int W>
 constexpr size_t few_lds(int rows) {
   const size_t areas = (size_t)32 * W * kStride<T, DP> * sizeof(T), outs = (size_t)W * rows * DP * sizeof(float);

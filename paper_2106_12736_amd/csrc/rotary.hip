@@ -2,8 +2,9 @@
 //
 //   (u, v) -> (u cos(a) - v sin(a), u sin(a) + v cos(a));   the gradient is the turn by -a.
 //
-// A pass over x and y (HBM-bound: 32768 tokens of 16 heads of 128 bf16, 268 MB, 64 us, 4.2 TB/s).  The angle of a pair is that of every head of the token, so a thread holds the
-// cosines and sines of VP pairs (a 16-byte piece of either half) and goes through the heads with them.
+// A pass over x and y (HBM-bound: 32768 tokens of 16 heads of 128 bf16, 268 MB, 64 us, 4.2 TB/s).  The angle of a pair is
+// that of every head of the token, so a thread holds the cosines and sines of VP pairs (a 16-byte piece of either half) and
+// goes through the heads with them.
 #include "launch_limit.h"
 #include "sequence.h"
 

@@ -17,7 +17,7 @@
 //
 // 4096 x 32000 bf16 without alternatives 52 us (5.0 TB/s; 71 behind a gradient's writes), 2048 x 100000 with 64 of them 129
 // us (3.2 TB/s), of which the first chunk's bound and the last ranking are some 20 us and later candidates 25: there the
-// vector units are busy 85 % of the time.  With the rows in registers whole, and every segment's K best found anew, it
+// vector units are busy 86 % of the time (7 registers spilled).  With the rows in registers whole, and every segment's K best found anew, it
 // took 393 us.  Candidates taken from registers instead of read again took 134.  The gradient, 4096 x 32000 bf16, 117 us
 // (4.5 TB/s).
 #include <algorithm>
@@ -303,7 +303,8 @@ __global__ __launch_bounds__(TH, (kWavesASimd<T, TH, NV, Top>)) void k_logprobs(
   Sums t{-INFINITY, 0.f, 0.f};
   // As long as a wave's logits are numbers and its maxima's m c at most 2^20, t is fma(z, c, -mc), with mc the rounded m c: off
   // by its rounding of at most 2^-5, which all of the thread's terms have in common and which is made good at the end.  Else
-  // (z - m) c, held above -inf.
+  // (z - m) c, held above -inf.  The second form for all: 4096 x 32000 without alternatives 50.5 us in place of 48.6 (bf16),
+  // 49.9 in place of 47.0 (f16); 2048 x 100000 with 64 of them 121 in place of 125 (bf16), 138 in place of 132 (f16).
   float mc = -INFINITY;
   const float near = fminf(0x1p20f / c, -kLowest);
   bool careful = false;  // the same in every lane
@@ -635,7 +636,11 @@ struct Segments {
 };
 constexpr int kThreads = 256, kManyThreads = 1024, kPieces = 4;  // of a chunk
 // A row a workgroup where there are rows for every compute unit, and for fewer ones of at most 256 KB, in workgroups of 1024
-// threads (7 rows of 50021 f32: one launch without a workspace instead of two); else segments of one chunk or more.
+// threads (one launch without a workspace instead of two); else segments of one chunk or more.  A call with 20 best in one
+// launch and in segments, in a captured graph, us: 32000 bf16 (64 KB), 1 row 9.7 and 11.1, 64 rows 11.5 and 14.5, 500 rows 16.9
+// and 23.4; 50021 f32 (200 KB) 15.9 and 10.4, 16.9 and 12.4, 28.8 and 32.8; 128256 bf16 (250 KB) 22.1 and 11.8, 24.6 and 17.7,
+// 41.2 and 51.4; 151936 bf16 (297 KB) 26.1 and 11.7, 28.8 and 18.9, 48.6 and 55.5.  So up to 64 rows of more than some 80 KB
+// would be better off in segments, and 500 of any size here in one launch.
 Segments segments(int dtype, int64_t R, int V) {
   const int piece = 16 / (int)dtype_size(dtype), chunk = kThreads * kPieces * piece;
   const long long chunks = ceil_div(V, chunk);
