@@ -14,8 +14,8 @@ namespace {
 // runs (690 TFLOP/s), over 4096 keys 1435 (790 for what is added).  Bound by one wave's own latencies: with the blocks one after
 // another 463 us, with both blocks' scores first 434, with the vector work set among the products 392.  Tried: v in LDS and
 // eight waves of 256 registers (180 spilled); a branch around tiles without live rows, which has every sum copied
-// between the two kinds of registers in each tile (253 moves for 64 products).  Registers spilled: float16's heads of 128 77
-// (179 in workgroups of two waves), of 96 in two waves 62, bf16's of 128 in two waves 53; heads of 64 in eight waves bf16 18,
+// between the two kinds of registers in each tile (253 moves for 64 products).  Registers spilled: float16's heads of 128 81
+// (172 in workgroups of two waves), of 96 in two waves 36, bf16's of 128 in two waves 40; heads of 64 in eight waves bf16 18,
 // float16 33.
 // An order for COUNT products and the vector work that they are independent of: some instructions after each product, which
 // the matrix unit takes 32 cycles for.
@@ -102,8 +102,8 @@ __global__ __launch_bounds__(64 * W, W / 4) void k_attn_bwd_kv(
       auto q_row = [&](int i) { return static_cast<const T *>(p.a.q.p) + q_at[i]; };
       auto g_row = [&](int i) { return static_cast<const T *>(gy.p) + g_at[i]; };
       // one branch for both: with one each, registers that the first loads were on their way to held addresses of the second,
-      // which then waited for them (431 us in place of 390)
-      if (Tile::in_whole(p.a.D, p.wide))
+      // which then waited for them (431 us in place of 390).  Heads of over 64 channels are more than a piece.
+      if (DP > 64 || Tile::in_whole(p.a.D, p.wide))
         sq.load_whole(q_row, p.a.D), sg.load_whole(g_row, p.a.D);
       else
         sq.load_parts(q_row, p.a.D, live), sg.load_parts(g_row, p.a.D, live);
