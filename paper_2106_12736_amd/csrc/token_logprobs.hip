@@ -17,7 +17,7 @@
 //
 // 4096 x 32000 bf16 without alternatives 52 us (5.0 TB/s; 71 behind a gradient's writes), 2048 x 100000 with 64 of them 129
 // us (3.2 TB/s), of which the first chunk's bound and the last ranking are some 20 us and later candidates 25: there the
-// vector units are busy 86 % of the time (7 registers spilled).  With the rows in registers whole, and every segment's K best found anew, it
+// vector units are busy 85 % of the time (7 registers spilled).  With the rows in registers whole, and every segment's K best found anew, it
 // took 393 us.  Candidates taken from registers instead of read again took 134.  The gradient, 4096 x 32000 bf16, 117 us
 // (4.5 TB/s).
 #include <algorithm>
